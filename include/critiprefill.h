@@ -9,6 +9,13 @@
  *   critiprefill_select_shared / critiprefill_sparse_attn_shared   the same two steps with one list per KV head
  *   critiprefill_dense_causal_attn Eq. 2 (O = softmax(Q K^T / sqrt(d)) V) with the prefill causal mask
  *
+ * and what a program does around a prefill and after it, on a cache of pages (second half of this file):
+ *
+ *   critiprefill_norm_rope         norms of queries and keys for each head and the position rotation, in one pass
+ *   critiprefill_norm_rope_write   the same, with keys and values going straight into the cache
+ *   critiprefill_cache_write / critiprefill_cache_read   keys and values into the cache and back, as they are or in 8 bits
+ *   critiprefill_paged_attn        attention of each sequence's new tokens, one or many, over its pages
+ *
  * Conventions common to all entry points
  * --------------------------------------
  * Pointers: every data pointer is DEVICE memory owned by the caller, 16-byte aligned.  Inputs are
@@ -39,10 +46,10 @@ enum {
     CP_OK = 0,
     CP_ERR_NULL = -1,        /* a required pointer is NULL */
     CP_ERR_SHAPE = -2,       /* non-positive size, n_q_heads % n_kv_heads != 0, block_size does not divide segment_size */
-    CP_ERR_UNSUPPORTED = -3, /* head_dim != 128, unknown dtype or softmax_domain, n2 > 8192, list longer than the API allows,
-                                bf16 estimate with batch * n_q_heads > 65535 */
+    CP_ERR_UNSUPPORTED = -3, /* head_dim != 128, unknown dtype, softmax_domain or cache_format, n2 > 8192, list longer than the API allows,
+                                bf16 estimate with batch * n_q_heads > 65535, sizes of the cache beyond the limits named below */
     CP_ERR_ALIGN = -4,       /* a pointer is not 16-byte aligned or a stride is not a multiple of 8 elements */
-    CP_ERR_WORKSPACE = -5,   /* workspace smaller than critiprefill_workspace_bytes() */
+    CP_ERR_WORKSPACE = -5,   /* workspace smaller than critiprefill_workspace_bytes(), critiprefill_paged_workspace_bytes() */
     CP_ERR_LAUNCH = -6       /* the HIP runtime refused a launch */
 };
 
@@ -140,6 +147,75 @@ int critiprefill_sparse_attn_shared(const critiprefill_params *p, const void *q,
 /* Eq. 2 with the causal mask u <= t: the dense baseline.  Same tensors as sparse_attn, no lists. */
 int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, const void *k, const void *v,
                                    void *out, float *lse, void *hip_stream);
+
+/*
+ * The cache
+ * ---------
+ * K and V of all sequences lie in pages of page_size tokens: k_cache and v_cache are [n_pages, n_kv_heads, page_size, row],
+ * contiguous, so that a head's tokens of a page are one piece.  A row is 128 elements of `dtype` (CP_CACHE_PLAIN), or 128
+ * OCP e4m3 elements with one power of two for each 32 channels (CP_CACHE_MXFP8): the bytes e of k_scale and v_scale, [n_pages,
+ * n_kv_heads, page_size, 4], stand for 2^(e - 127); 2^e is the smallest with max |x| <= 448 * 2^e, e in 1 .. 254.  Values that are not
+ * finite have no part in the maximum and are held as NaN.  With CP_CACHE_PLAIN the scales are not read and may be NULL.
+ * A token's place is its slot, page * page_size + offset; a token whose slot is not in 0 .. n_pages * page_size - 1 has no place: it is
+ * not written, and read as zeros.  Two tokens of one call with the same slot leave one of the two, which one is not said.
+ *
+ * Tensors are [tokens, heads, 128]: `tokens` rows, those of all sequences one after another, with strides of token and head in the
+ * parameter block (elements, multiples of 8; channels lie together), so that the parts of a joint projection are read where they are.
+ * Written tensors: strides of at least 128.  tokens == 0 (and n_seqs == 0) is no error: nothing is launched or looked at.
+ */
+enum { CP_CACHE_PLAIN = 0, CP_CACHE_MXFP8 = 1 };
+
+typedef struct critiprefill_cache_params {
+    int32_t n_q_heads, n_kv_heads, head_dim;  /* head_dim must be 128; n_q_heads is not read by cache_write and cache_read */
+    int32_t dtype;                            /* CP_DTYPE_*: of Q, K, V, the outputs, the weights and plain pages */
+    int32_t tokens;                           /* rows of the tensors */
+    int32_t cache_format;                     /* CP_CACHE_* */
+    int32_t page_size, n_pages;               /* page_size: a power of two, 16 or more; n_pages * page_size < 2^31 */
+    int32_t n_seqs, max_pages;                /* paged_attn: sequences, and the pitch of the page table */
+    int32_t max_q_len;                        /* paged_attn: new tokens that a sequence has at most, 0: not known.  Chooses the kernel; more are right too */
+    int32_t rotary_dim, rotary_interleaved;   /* norm_rope: channels that turn (0 .. 128, a multiple of 16), and how they pair */
+    float norm_eps, attn_scale;               /* attn_scale: 0 -> 1/sqrt(head_dim) */
+    int64_t q_stride[2], k_stride[2], v_stride[2]; /* token, head.  cache_read: k_stride, v_stride are the outputs' */
+    int64_t o_stride[2], ko_stride[2];        /* q_out or out; k_out */
+} critiprefill_cache_params;
+
+/*
+ * For every token and head, in fp32 and rounded once: y = x / sqrt(mean(x^2) + norm_eps) * weight over the head's 128 channels (q_weight,
+ * k_weight: 128 elements of dtype; NULL: y = x), then for c < rotary_dim / 2 the channels (c, c + rotary_dim / 2), or (2c, 2c + 1) with
+ * rotary_interleaved, turned by the angle positions[token] * inv_freq[c]: (y1 cos - y2 sin, y2 cos + y1 sin).  inv_freq: rotary_dim / 2
+ * doubles, radians for each position; the angle is worked out in fp64.  positions: int32[tokens], of any sign.  Both may be NULL with rotary_dim == 0.
+ * q_out may be q and k_out may be k, with the same strides; other overlaps are not allowed.
+ */
+int critiprefill_norm_rope(const critiprefill_cache_params *p, const void *q, const void *k, const void *q_weight, const void *k_weight,
+                           const double *inv_freq, const int32_t *positions, void *q_out, void *k_out, void *hip_stream);
+
+/* The same for q; k goes, and v as it is, to slots[token] of the cache (int32[tokens]).  With CP_CACHE_MXFP8 k is quantised from fp32. */
+int critiprefill_norm_rope_write(const critiprefill_cache_params *p, const void *q, const void *k, const void *v, const void *q_weight, const void *k_weight,
+                                 const double *inv_freq, const int32_t *positions, const int32_t *slots, void *q_out, void *k_cache, void *v_cache,
+                                 uint8_t *k_scale, uint8_t *v_scale, void *hip_stream);
+
+/* k, v of `tokens` tokens into the cache, and the values that the cache holds for `tokens` slots, in any order, back as tensors of dtype. */
+int critiprefill_cache_write(const critiprefill_cache_params *p, const void *k, const void *v, const int32_t *slots, void *k_cache, void *v_cache,
+                             uint8_t *k_scale, uint8_t *v_scale, void *hip_stream);
+int critiprefill_cache_read(const critiprefill_cache_params *p, const int32_t *slots, const void *k_cache, const void *v_cache, const uint8_t *k_scale,
+                            const uint8_t *v_scale, void *k, void *v, void *hip_stream);
+
+/* Bytes of scratch critiprefill_paged_attn needs: parts of results that several workgroups work on.  It depends on the sizes of heads, dtype and max_q_len
+ * (tokens where that is 0) alone, not on lengths.  Contents do not matter before a call; calls that may overlap need one each. */
+size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
+
+/*
+ * Attention of new tokens over the cache, which holds their own K and V already.  Sequence i has the rows q_start[i] .. q_start[i + 1] - 1 of q
+ * (q_start: int32[n_seqs + 1], ascending from 0 to tokens), kv_len[i] tokens in all, the new ones last, and token u of it lies in page
+ * page_table[i, u / page_size] (int32[n_seqs, max_pages]) at u % page_size.  The t-th of its n new tokens sees the tokens u <= kv_len[i] - n + t.
+ * out[tokens, n_q_heads, 128] has dtype and o_stride; lse (nullable, fp32 [tokens, n_q_heads]) receives log(sum exp(scaled logits)).  A
+ * row that sees nothing gets output 0 and lse -inf.  All four arrays are read on the device and the lengths never by the host: a captured call follows them.
+ * Whatever they hold, nothing outside the tensors is touched: rows and lengths are cut to the tensors' sizes, and tokens of a page outside the pool are seen
+ * by no row.  Rows of no sequence are not written.  At most 64 query heads for a KV head.
+ */
+int critiprefill_paged_attn(const critiprefill_cache_params *p, const void *q, const void *k_cache, const void *v_cache, const uint8_t *k_scale,
+                            const uint8_t *v_scale, const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len, void *out, float *lse,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *critiprefill_strerror(int status);
 int critiprefill_version(void);

@@ -15,10 +15,12 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcritipr
 _lib = None
 
 CP_DTYPE_FP32, CP_DTYPE_BF16 = 0, 1
+CP_CACHE_PLAIN, CP_CACHE_MXFP8 = 0, 1
 EXPORTS = ["critiprefill_list_len", "critiprefill_workspace_bytes", "critiprefill_estimate",
            "critiprefill_estimate_static", "critiprefill_select", "critiprefill_sparse_attn", "critiprefill_select_shared",
            "critiprefill_sparse_attn_shared", "critiprefill_dense_causal_attn",
-           "critiprefill_strerror", "critiprefill_version"]
+           "critiprefill_norm_rope", "critiprefill_norm_rope_write", "critiprefill_cache_write", "critiprefill_cache_read",
+           "critiprefill_paged_workspace_bytes", "critiprefill_paged_attn", "critiprefill_strerror", "critiprefill_version"]
 
 
 class Params(ctypes.Structure):
@@ -28,6 +30,13 @@ class Params(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("attn_scale", ctypes.c_float), ("score_scale", ctypes.c_float),
                 ("alpha", ctypes.c_float), ("softmax_domain", ctypes.c_int32),
                 ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
+
+
+class CacheParams(ctypes.Structure):
+    _fields_ = ([(x, ctypes.c_int32) for x in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "tokens", "cache_format", "page_size", "n_pages",
+                                               "n_seqs", "max_pages", "max_q_len", "rotary_dim", "rotary_interleaved")]
+                + [("norm_eps", ctypes.c_float), ("attn_scale", ctypes.c_float)]
+                + [(x, ctypes.c_int64 * 2) for x in ("q_stride", "k_stride", "v_stride", "o_stride", "ko_stride")])
 
 
 class CritiPrefillError(RuntimeError):
@@ -59,6 +68,12 @@ def load():
     lib.critiprefill_select_shared.argtypes = [P, vp, vp, vp, vp]; lib.critiprefill_select_shared.restype = ctypes.c_int
     lib.critiprefill_sparse_attn_shared.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp]; lib.critiprefill_sparse_attn_shared.restype = ctypes.c_int
     lib.critiprefill_dense_causal_attn.argtypes = [P, vp, vp, vp, vp, vp, vp]; lib.critiprefill_dense_causal_attn.restype = ctypes.c_int
+    C = ctypes.POINTER(CacheParams)
+    for name, pointers in (("norm_rope", 9), ("norm_rope_write", 14), ("cache_write", 8), ("cache_read", 8)):
+        f = getattr(lib, "critiprefill_" + name)
+        f.argtypes = [C] + [vp] * pointers; f.restype = ctypes.c_int
+    lib.critiprefill_paged_workspace_bytes.argtypes = [C]; lib.critiprefill_paged_workspace_bytes.restype = sz
+    lib.critiprefill_paged_attn.argtypes = [C] + [vp] * 11 + [sz, vp]; lib.critiprefill_paged_attn.restype = ctypes.c_int
     lib.critiprefill_strerror.argtypes = [ctypes.c_int]; lib.critiprefill_strerror.restype = ctypes.c_char_p
     lib.critiprefill_version.argtypes = []; lib.critiprefill_version.restype = ctypes.c_int
     _lib = lib
@@ -164,6 +179,98 @@ def critiprefill_dense_causal_attn(p, q, k, v, out, lse=None, stream=None):
                                                  _stream(stream)), "critiprefill_dense_causal_attn")
 
 
+# ---- the paged cache -----------------------------------------------------------------------------
+def _dtype_code(dtype: torch.dtype) -> int:
+    if dtype == torch.bfloat16:
+        return CP_DTYPE_BF16
+    if dtype == torch.float32:
+        return CP_DTYPE_FP32
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def make_cache_params(n_q_heads: int, n_kv_heads: int, dtype: torch.dtype, *, q=None, k=None, v=None, out=None, k_out=None, k_cache=None,
+                      mxfp8: bool = False, page_table=None, max_q_len: int = 0, rotary_dim: int = 0, interleaved: bool = False,
+                      norm_eps: float = 0.0, attn_scale: float = 0.0) -> CacheParams:
+    """Fill the parameter block from the tensors of a call: q, k, v, out (q_out or the attention's) and k_out are [tokens, heads, 128], each with
+    strides of its own; k_cache [n_pages, n_kv_heads, page_size, 128] says the pool's size, page_table [n_seqs, max_pages] the sequences."""
+    p = CacheParams()
+    p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype = n_q_heads, n_kv_heads, 128, _dtype_code(dtype)
+    p.cache_format = CP_CACHE_MXFP8 if mxfp8 else CP_CACHE_PLAIN
+    tokens = None
+    for t, heads, stride, name in ((q, n_q_heads, p.q_stride, "q"), (k, n_kv_heads, p.k_stride, "k"), (v, n_kv_heads, p.v_stride, "v"),
+                                   (out, n_q_heads, p.o_stride, "out"), (k_out, n_kv_heads, p.ko_stride, "k_out")):
+        if t is None:
+            continue
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128 or (tokens is not None and t.shape[0] != tokens):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({'tokens' if tokens is None else tokens}, {heads}, 128)")
+        if t.dtype != dtype:
+            raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: channel stride must be 1")
+        tokens = t.shape[0]
+        for i in range(2):
+            # the stride of an axis of one element is never used, and torch gives it any value
+            stride[i] = t.stride(i) if t.shape[i] > 1 else max(128, heads * 128 if i == 0 else 128)
+    p.tokens = tokens or 0
+    if k_cache is not None:
+        if k_cache.dim() != 4 or k_cache.shape[1] != n_kv_heads or k_cache.shape[3] != 128 or not k_cache.is_contiguous():
+            raise ValueError(f"k_cache: expected a contiguous [n_pages, {n_kv_heads}, page_size, 128], got {tuple(k_cache.shape)}")
+        if k_cache.dtype != (torch.uint8 if mxfp8 else dtype):
+            raise TypeError(f"k_cache: {k_cache.dtype}")
+        p.n_pages, p.page_size = k_cache.shape[0], k_cache.shape[2]
+    if page_table is not None:
+        if page_table.dim() != 2 or not page_table.is_contiguous():
+            raise ValueError("page_table: expected a contiguous [n_seqs, max_pages]")
+        p.n_seqs, p.max_pages = page_table.shape
+    p.max_q_len, p.rotary_dim, p.rotary_interleaved, p.norm_eps, p.attn_scale = max_q_len, rotary_dim, int(interleaved), norm_eps, attn_scale
+    return p
+
+
+def _check_args(tokens, *triples):
+    """(tensor, dtype, elements at least) of what the parameter block does not describe: the library sees only an address."""
+    for t, dtype, least in triples:
+        if t is not None and (t.dtype != dtype or t.numel() < least or not t.is_contiguous()):
+            raise ValueError(f"expected a contiguous tensor of {dtype} with {least} elements or more, got {t.dtype} {tuple(t.shape)}")
+
+
+def critiprefill_norm_rope(p, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream=None):
+    _check_args(p.tokens, (inv_freq, torch.float64, p.rotary_dim // 2), (positions, torch.int32, p.tokens))
+    _check(load().critiprefill_norm_rope(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), _ptr(positions),
+                                         _ptr(q_out), _ptr(k_out), _stream(stream)), "critiprefill_norm_rope")
+
+
+def critiprefill_norm_rope_write(p, q, k, v, q_weight, k_weight, inv_freq, positions, slots, q_out, k_cache, v_cache, k_scale=None, v_scale=None,
+                                 stream=None):
+    _check_args(p.tokens, (inv_freq, torch.float64, p.rotary_dim // 2), (positions, torch.int32, p.tokens), (slots, torch.int32, p.tokens))
+    _check(load().critiprefill_norm_rope_write(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                                               _ptr(positions), _ptr(slots), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                               _stream(stream)), "critiprefill_norm_rope_write")
+
+
+def critiprefill_cache_write(p, k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None):
+    _check_args(p.tokens, (slots, torch.int32, p.tokens))
+    _check(load().critiprefill_cache_write(ctypes.byref(p), _ptr(k), _ptr(v), _ptr(slots), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                           _ptr(v_scale), _stream(stream)), "critiprefill_cache_write")
+
+
+def critiprefill_cache_read(p, slots, k_cache, v_cache, k_scale, v_scale, k, v, stream=None):
+    _check_args(p.tokens, (slots, torch.int32, p.tokens))
+    _check(load().critiprefill_cache_read(ctypes.byref(p), _ptr(slots), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(k),
+                                          _ptr(v), _stream(stream)), "critiprefill_cache_read")
+
+
+def critiprefill_paged_workspace_bytes(p: CacheParams) -> int:
+    return load().critiprefill_paged_workspace_bytes(ctypes.byref(p))
+
+
+def critiprefill_paged_attn(p, q, k_cache, v_cache, k_scale, v_scale, page_table, q_start, kv_len, out, lse, workspace, stream=None):
+    _check_args(p.tokens, (page_table, torch.int32, p.n_seqs * p.max_pages), (q_start, torch.int32, p.n_seqs + 1), (kv_len, torch.int32, p.n_seqs),
+                (lse, torch.float32, p.tokens * p.n_q_heads))
+    _check(load().critiprefill_paged_attn(ctypes.byref(p), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(page_table),
+                                          _ptr(q_start), _ptr(kv_len), _ptr(out), _ptr(lse), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)), "critiprefill_paged_attn")
+
+
 # ---- buffer helpers (device memory only; no arithmetic) -----------------------------------------
 def n_segments(p: Params) -> int:
     return -(-p.seq_len // p.segment_size)
@@ -194,3 +301,20 @@ def alloc_shared_lists(p: Params, device="cuda"):
 
 def alloc_workspace(p: Params, device="cuda") -> torch.Tensor:
     return torch.empty((max(16, critiprefill_workspace_bytes(p)),), dtype=torch.uint8, device=device)
+
+
+def alloc_cache(n_pages: int, n_kv_heads: int, page_size: int, dtype: torch.dtype = torch.bfloat16, mxfp8: bool = False, device="cuda"):
+    """(k_cache, v_cache, k_scale, v_scale) of a pool of pages; the scales are None without mxfp8."""
+    shape = (n_pages, n_kv_heads, page_size)
+    caches = [torch.empty((*shape, 128), dtype=torch.uint8 if mxfp8 else dtype, device=device) for _ in range(2)]
+    scales = [torch.empty((*shape, 4), dtype=torch.uint8, device=device) if mxfp8 else None for _ in range(2)]
+    return (*caches, *scales)
+
+
+def alloc_paged_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
+    return torch.empty((max(16, critiprefill_paged_workspace_bytes(p)),), dtype=torch.uint8, device=device)
+
+
+def rotary_frequencies(rotary_dim: int = 128, base: float = 500000.0, device="cuda") -> torch.Tensor:
+    """inv_freq of critiprefill_norm_rope for the usual base^(-2c / rotary_dim)."""
+    return base ** (-torch.arange(rotary_dim // 2, dtype=torch.float64, device=device) * 2 / rotary_dim)

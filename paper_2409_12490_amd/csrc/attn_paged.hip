@@ -1,0 +1,517 @@
+// Attention of the new tokens of each sequence over the pages of a cache, for few rows a KV head (single tokens above all) and for fp32:
+//
+//   o_t = sum_u p_tu v_u / sum_u p_tu,  p_tu = exp(q_t k_u scale - m_t),  u <= keys - tokens + t;  no such u: o_t = 0, lse_t = -inf
+//
+// A tile has up to 16 * NQ rows (a token's query heads of one KV head lie next to each other) and its keys are read once for all of them.  The four waves
+// of a workgroup split the keys: a step gives each wave 32 (bf16; fp32: 16) of its own, with a running maximum, sum and output of its own, merged
+// through LDS when the unit or the workgroup's run ends.  How the steps are dealt to workgroups: paged.h.
+//
+//   S^T[key][row]  = K . Q^T      16x16 MFMA, A = K straight from memory (a lane has one key's 32 neighbouring channels), B = Q in registers
+//   softmax                       one row per lane column
+//   O^T[ch][row]  += V^T . P^T    A = V straight from memory, 8 channels of a token to a lane (whole rows per instruction); the pairs of tokens that a bf16
+//                                 operand wants come from v_perm, and the channel that an operand row stands for is the lane's own choice: lane c, operand
+//                                 n is channel 8 c + n.  B = P^T, the S^T accumulators as they stand.
+// Nothing goes through LDS and no wave waits for another in the key loop: K and V of the next step are asked for before this one is multiplied.
+// 8-bit keys and values become bf16 (exact: their scales are powers of two) or fp32 in registers.
+#include "paged.h"
+
+#include <algorithm>
+
+namespace cp {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+typedef const __attribute__((address_space(4))) int32_t* scalar_list;   // read through scalar loads: wave-uniform addresses
+
+constexpr float kLazyLog2 = 8.0f;             // how far a row's max may outgrow its reference point before O is rescaled
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { union { u32x4 u; bf16x8 b; } c; c.u = v; return c.b; }
+__device__ __forceinline__ unsigned as_u32(bf16x2 v) { union { bf16x2 b; unsigned u; } c; c.b = v; return c.u; }
+
+// max and sum over the four lanes that share a column: l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float column_max(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ float mx_scale(unsigned byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ u32x2 widen4(unsigned w, float scale) {      // four e4m3 to bf16
+    u32x2 r;
+    r[0] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+    r[1] = as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
+    return r;
+}
+__device__ __forceinline__ f32x4 widen4f(unsigned w, float scale) {     // to fp32
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
+    return f32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// What a wave has of a step: K and V as they come from memory.
+template <bool F32, bool MX> struct Raw;
+template <> struct Raw<false, false> { u32x4 k[2][4]; u32x4 v[8]; };                           // [16 keys][64 bytes]; [token]
+template <> struct Raw<false, true> { u32x4 k[2][2]; u32x2 v[8]; unsigned ks[2]; u32x4 vs[2]; };
+template <> struct Raw<true, false> { f32x4 k[8]; f32x4 v[4][2]; };
+template <> struct Raw<true, true> { u32x4 k[2]; unsigned v[4][2]; unsigned ks; u32x4 vs; };
+
+template <bool F32, bool MX, int NQ>
+__global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
+    constexpr int kRows = 16 * NQ, kWaveKeys = F32 ? 16 : 32, kGroups = kWaveKeys / 16;
+    constexpr int kRowBytes = MX ? kHeadDim : (F32 ? 512 : 256);
+    extern __shared__ __attribute__((aligned(16))) float merge[];              // [wave][row][128], then (max, sum) [wave][row]
+    float* const wave_stats = merge + 4 * kRows * kHeadDim;
+
+    const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, kg = lane >> 4;
+    const int wave = first_lane(tid >> 6);
+    Run run;
+    const bool any = run.find(a, blockIdx.x, lane);
+    if (blockIdx.x == 0 && tid == 0) a.record[0] = any ? (int)run.used : 0;    // workgroup 0 is the first run's, if there is one
+    if (!any) return;
+    const unsigned home = run.logical;
+    if (tid == 0) a.record[4 + 4 * home + 3] = 0;
+    const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
+    const int page_mask = (1 << a.page_shift) - 1;
+
+    while (true) {
+        const Sequence seq = run.now;
+        const int tile_tokens = 1 << a.tile_shift, t0 = run.tile << a.tile_shift;
+        const int live = min(tile_tokens, seq.tokens - t0);                    // tokens of the tile
+        const unsigned unit = seq.steps_of(run.tile, a.tile_shift, a.step_shift), first = run.step, count = min(run.left, unit - first);
+        const int head = run.head;
+        const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)run.seq * a.max_pages);
+        const int past = seq.keys - seq.tokens;                                // position of the sequence's first new token
+        const int low = min(past + t0, seq.keys - 1), high = min(past + t0 + live, seq.keys) - 1;   // last keys that its first and its last row see
+
+        // ---- Q: lane's column is a row, 8 channels at 32 kg + 8 ks (fp32: 32 at 32 kg)
+        bf16x8 qf[F32 ? 1 : NQ][4];
+        f32x4 qw[F32 ? NQ : 1][8];
+        int last[NQ];                                                          // the last key that the row sees
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + c16, t = min(r / a.group, live - 1), g = r - r / a.group * a.group;
+            last[nq] = min(past + t0 + t, seq.keys - 1);
+            const int64_t at = (seq.start + t0 + t) * a.qs0 + (int64_t)(head * a.group + g) * a.qs1 + 32 * kg;
+            if (F32) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) qw[F32 ? nq : 0][x] = *(const f32x4*)((const float*)a.q + at + 4 * x);
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) qf[F32 ? 0 : nq][ks] = *(const bf16x8*)((const __bf16*)a.q + at + 8 * ks);
+            }
+        }
+
+        f32x4 o[NQ][8];
+        float m_run[NQ], l_run[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            m_run[nq] = -INFINITY; l_run[nq] = 0.f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) o[nq][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // ---- loads.  Pages are looked up a step ahead; one that is not in the pool holds nothing: its keys are hidden, and read from page 0
+        int entry[kGroups];
+        auto key_of = [&](unsigned step) { return (int)(step << a.step_shift) + wave * kWaveKeys; };
+        auto look_up = [&](unsigned step) __attribute__((always_inline)) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int u = key_of(step) + 16 * g;
+                entry[g] = u <= high && step < first + count ? table[u >> a.page_shift] : -1;
+            }
+        };
+        auto load = [&](Raw<F32, MX>& raw, int (&seen)[kGroups], unsigned step) __attribute__((always_inline)) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int u = key_of(step) + 16 * g;
+                const bool there = (unsigned)entry[g] < (unsigned)a.n_pages;
+                seen[g] = there ? seq.keys - u : 0;                            // keys of the group that exist
+                const int64_t row = (((int64_t)(there ? entry[g] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
+                const char* kp = (const char*)a.cache.k + row * kRowBytes;
+                const char* vp = (const char*)a.cache.v + row * kRowBytes;
+                if constexpr (!F32) {
+                    const int per = MX ? 32 : 64;
+#pragma unroll
+                    for (int x = 0; x < (MX ? 2 : 4); ++x) raw.k[g][x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * per + 16 * x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (MX) raw.v[4 * g + i] = *(const u32x2*)(vp + (4 * kg + i) * kRowBytes + 8 * c16);
+                        else raw.v[4 * g + i] = *(const u32x4*)(vp + (4 * kg + i) * kRowBytes + 16 * c16);
+                    }
+                    if constexpr (MX) {
+                        raw.ks[g] = (a.cache.ks + row * 4)[c16 * 4 + kg];
+                        raw.vs[g] = *(const u32x4*)(a.cache.vs + row * 4 + 16 * kg);   // of four tokens
+                    }
+                } else if constexpr (MX) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) raw.k[x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * 32 + 16 * x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) raw.v[i][x] = *(const unsigned*)(vp + (4 * kg + i) * kRowBytes + 4 * c16 + 64 * x);
+                    raw.ks = (a.cache.ks + row * 4)[c16 * 4 + kg];
+                    raw.vs = *(const u32x4*)(a.cache.vs + row * 4 + 16 * kg);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) raw.k[x] = *(const f32x4*)(kp + c16 * kRowBytes + kg * 128 + 16 * x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) raw.v[i][x] = *(const f32x4*)(vp + (4 * kg + i) * kRowBytes + 16 * c16 + 256 * x);
+                }
+            }
+        };
+        // ---- one step: the wave's keys u0 .. u0 + kWaveKeys - 1
+        auto multiply = [&](Raw<F32, MX>& raw, const int (&seen)[kGroups], unsigned step) __attribute__((always_inline)) {
+            const int u0 = key_of(step);
+            if (u0 > high) return;                                             // uniform: no row sees any of them
+            f32x4 s[NQ][kGroups];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) s[nq][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (!F32) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        u32x4 kw;
+                        if constexpr (MX) {
+                            const float scale = mx_scale(raw.ks[g]);
+                            const u32x2 lo = widen4(raw.k[g][ks >> 1][2 * (ks & 1)], scale), hi = widen4(raw.k[g][ks >> 1][2 * (ks & 1) + 1], scale);
+                            kw = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                        } else kw = raw.k[g][ks];
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) s[nq][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kw), qf[nq][ks], s[nq][g], 0, 0, 0);
+                    }
+            } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    f32x4 kw;
+                    if constexpr (MX) kw = widen4f(raw.k[x >> 2][x & 3], mx_scale(raw.ks));
+                    else kw = raw.k[x];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) s[nq][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kw[e], qw[nq][x][e], s[nq][0], 0, 0, 0);
+                }
+            }
+            // hidden keys: behind the row's own, or without a page.  Their values may hold anything, NaN included, and a weight of 0 does not stop that:
+            // rows of V that no row of the tile sees become 0
+            bool whole = u0 + kWaveKeys - 1 <= low;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) whole = whole && seen[g] > 0;
+            if (!whole) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        const int lim = seen[g] > 0 ? last[nq] - u0 - 16 * g - 4 * kg : -1;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[nq][g][i] = i > lim ? -INFINITY : s[nq][g][i];
+                    }
+                    const int lim = seen[g] > 0 ? high - u0 - 16 * g - 4 * kg : -1;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (!F32 && MX) { if (i > lim) { raw.v[4 * g + i] = u32x2{0, 0}; raw.vs[g][i] = 0x7f7f7f7fu; } }
+                        else if constexpr (!F32) { if (i > lim) raw.v[4 * g + i] = u32x4{0, 0, 0, 0}; }
+                        else if constexpr (MX) { if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; raw.vs[i] = 0x7f7f7f7fu; } }
+                        else { if (i > lim) raw.v[i][0] = raw.v[i][1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+                    }
+                }
+            }
+            bf16x8 pf[F32 ? 1 : NQ];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                float mx = fmaxf(fmaxf(s[nq][0][0], s[nq][0][1]), fmaxf(s[nq][0][2], s[nq][0][3]));
+                if constexpr (!F32) mx = fmaxf(fmaxf(fmaxf(s[nq][1][0], s[nq][1][1]), fmaxf(s[nq][1][2], s[nq][1][3])), mx);
+                mx = column_max(mx);
+                // the reference point moves only when the maximum has outgrown it by 2^kLazyLog2: P <= 2^8 meanwhile, the same factor in O and l
+                const float m_new = mx > m_run[nq] + lazy_raw ? mx : m_run[nq];
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = __builtin_amdgcn_exp2f((m_run[nq] - m_safe) * c);
+                const float ms = m_safe * c;
+                m_run[nq] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[nq][g][i], c, -ms));
+                        sum += p;                                              // before P is rounded for the product: lse is as exact as fp32 allows
+                        if constexpr (F32) s[nq][g][i] = p;
+                        else pf[nq][4 * g + i] = (__bf16)p;
+                    }
+                l_run[nq] = l_run[nq] * alpha + sum;
+                if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) o[nq][n] *= alpha;
+                }
+            }
+            if constexpr (!F32) {
+                u32x4 v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (MX) {
+                        const float scale = mx_scale((raw.vs[j >> 2][j & 3] >> (8 * (c16 >> 2))) & 0xff);
+                        const u32x2 lo = widen4(raw.v[j][0], scale), hi = widen4(raw.v[j][1], scale);
+                        v[j] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    } else v[j] = raw.v[j];
+                }
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    u32x4 w;                                                   // channel n of the lane's 8 tokens
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(v[2 * e + 1][n >> 1], v[2 * e][n >> 1], n & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pf[nq], o[nq][n], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 v[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if constexpr (MX) v[x] = widen4f(raw.v[i][x], mx_scale((raw.vs[i] >> (16 * x + 8 * (c16 >> 3))) & 0xff));
+                        else v[x] = raw.v[i][x];
+                    }
+#pragma unroll
+                    for (int n = 0; n < 8; ++n)
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[n >> 2][n & 3], s[nq][0][i], o[nq][n], 0, 0, 0);
+                }
+            }
+        };
+
+        Raw<F32, MX> one, two;
+        int seen_one[kGroups], seen_two[kGroups];
+        look_up(first); load(one, seen_one, first);
+        look_up(first + 1);
+        for (unsigned x = 0; x < count; x += 2) {
+            if (x + 1 < count) { load(two, seen_two, first + x + 1); look_up(first + x + 2); }
+            multiply(one, seen_one, first + x);
+            if (x + 1 < count) {
+                if (x + 2 < count) { load(one, seen_one, first + x + 2); look_up(first + x + 3); }
+                multiply(two, seen_two, first + x + 1);
+            }
+        }
+
+        // ---- merge the four waves: sum_w 2^(c (m_w - M)) O_w; 16-byte pieces of a row swizzled by the row
+        __syncthreads();                                                       // the unit before has been read
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + c16;
+            const float l = column_sum(l_run[nq]);
+            if (kg == 0) { wave_stats[2 * (wave * kRows + r)] = m_run[nq]; wave_stats[2 * (wave * kRows + r) + 1] = l; }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {                         // channels 8 (4 kg + i) + 4 half ..; fp32: 64 half + 4 (4 kg + i) ..
+                    const int piece = F32 ? 16 * half + 4 * kg + i : 2 * (4 * kg + i) + half;
+                    f32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = o[nq][4 * half + e][i];
+                    *(f32x4*)(merge + (wave * kRows + r) * kHeadDim + 4 * (piece ^ c16)) = w;
+                }
+        }
+        __syncthreads();
+        const bool began = first == 0, ended = first + count == unit;
+        const int64_t slot = 2 * (int64_t)home + (began ? 1 : 0);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + (tid >> 4), piece = tid & 15;              // 8 channels
+            const int t = r / a.group, g = r - t * a.group;
+            if (t >= live) continue;
+            float M = -INFINITY, L = 0.f, sum[8];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) M = fmaxf(M, wave_stats[2 * (w * kRows + r)]);
+            const float M_safe = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f((wave_stats[2 * (w * kRows + r)] - M_safe) * c);
+                L = fmaf(f, wave_stats[2 * (w * kRows + r) + 1], L);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const f32x4 v = *(const f32x4*)(merge + (w * kRows + r) * kHeadDim + 4 * ((2 * piece + half) ^ (r & 15)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[4 * half + e] = fmaf(f, v[e], sum[4 * half + e]);
+                }
+            }
+            if (began && ended) {
+                const float inv = L == 0.f ? 0.f : 1.0f / L;
+                const int64_t row = seq.start + t0 + t;
+                const int h = head * a.group + g;
+                const int64_t at = row * a.os0 + h * a.os1 + 8 * piece;
+                if (F32) {
+                    *(f32x4*)((float*)a.out + at) = f32x4{sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+                    *(f32x4*)((float*)a.out + at + 4) = f32x4{sum[4] * inv, sum[5] * inv, sum[6] * inv, sum[7] * inv};
+                } else {
+                    bf16x8 w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = (__bf16)(sum[e] * inv);
+                    *(bf16x8*)((__bf16*)a.out + at) = w;
+                }
+                if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
+            } else {
+                float* to = a.parts + (slot * kRows + r) * kHeadDim + 8 * piece;
+                *(f32x4*)to = f32x4{sum[0], sum[1], sum[2], sum[3]};
+                *(f32x4*)(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+                if (piece == 0) *(f32x2*)(a.stats + 2 * (slot * kRows + r)) = f32x2{M, L};
+            }
+        }
+        if (began && !ended && tid == 0) {
+            const unsigned rest = unit - first - count;                        // of whole runs, the last perhaps not whole
+            int32_t* rec = a.record + 4 + 4 * home;
+            rec[0] = seq.start + t0; rec[1] = live; rec[2] = head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
+        }
+        run.left -= count;
+        if (run.left == 0 || !run.next(a)) break;
+    }
+}
+
+// Adds up the parts of units that more than one workgroup worked on.  PG groups of threads take every PG-th part of a row.
+template <typename T, int PG>
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
+    __shared__ __attribute__((aligned(16))) float rest[PG > 1 ? 16 * 128 : 4];
+    __shared__ float rest_l[16];
+    const unsigned w = blockIdx.x;
+    if (w >= (unsigned)a.record[0]) return;
+    const int32_t* rec = a.record + 4 + 4 * w;
+    const int parts = rec[3];
+    if (parts < 2) return;
+    constexpr int kPer = 16 / PG;
+    const int tid = threadIdx.x, piece = tid & 15, pg = (tid >> 4) / kPer, local = (tid >> 4) % kPer;
+    const int r = blockIdx.y * kPer + local, t = r / a.group, g = r - t * a.group;
+    const bool live = t < rec[1];
+    if (blockIdx.y * kPer >= rec[1] * a.group) return;
+    const float c = a.scale_log2e;
+    float M = -INFINITY, L = 0.f;
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    if (live) {
+        auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
+        for (int x = 0; x < parts; ++x) M = fmaxf(M, a.stats[2 * (slot(x) * rows + r)]);
+        const float M_safe = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+        for (int x = pg; x < parts; x += PG) {
+            const f32x2 ml = *(const f32x2*)(a.stats + 2 * (slot(x) * rows + r));
+            const float* from = a.parts + (slot(x) * rows + r) * kHeadDim + 8 * piece;
+            const f32x4 v0 = *(const f32x4*)from, v1 = *(const f32x4*)(from + 4);
+            const float f = __builtin_amdgcn_exp2f((ml[0] - M_safe) * c);
+            L = fmaf(f, ml[1], L);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { lo[e] = fmaf(f, v0[e], lo[e]); hi[e] = fmaf(f, v1[e], hi[e]); }
+        }
+    }
+    if (PG > 1) {
+        float* mine = rest + (tid >> 4) * 128 + 8 * piece;
+        *(f32x4*)mine = lo; *(f32x4*)(mine + 4) = hi;
+        if (piece == 0) rest_l[tid >> 4] = L;
+        __syncthreads();
+        if (pg != 0) return;
+#pragma unroll
+        for (int x = 1; x < PG; ++x) {
+            lo += *(const f32x4*)(mine + x * kPer * 128); hi += *(const f32x4*)(mine + x * kPer * 128 + 4);
+            L += rest_l[local + x * kPer];
+        }
+    }
+    if (!live) return;
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const int64_t row = rec[0] + t;
+    const int h = rec[2] * a.group + g;
+    const int64_t at = row * a.os0 + h * a.os1 + 8 * piece;
+    lo *= inv; hi *= inv;
+    if constexpr (sizeof(T) == 4) {
+        *(f32x4*)((float*)a.out + at) = lo; *(f32x4*)((float*)a.out + at + 4) = hi;
+    } else {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = (__bf16)lo[e]; v[4 + e] = (__bf16)hi[e]; }
+        *(bf16x8*)((__bf16*)a.out + at) = v;
+    }
+    if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
+}
+
+template <bool F32, bool MX, int NQ>
+hipError_t launch(const PagedArgs& a, hipStream_t st) {
+    constexpr int smem = 4 * 16 * NQ * (kHeadDim + 2) * 4;
+    const hipError_t e = hipFuncSetAttribute((const void*)paged_rows_kernel<F32, MX, NQ>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((paged_rows_kernel<F32, MX, NQ>), dim3(a.workgroups), dim3(kThreads), smem, st, a);
+    return hipGetLastError();
+}
+
+int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        // rounded down
+
+}  // namespace
+
+PagedRoute paged_route(const CacheShape& sh) {
+    PagedRoute r;
+    const bool f32 = sh.dtype == 0;
+    r.chunk = 0;
+    int nq = 1;
+    while (nq < (f32 ? 2 : 4) && (16 * nq / sh.group < 1 || (1 << log2_of(16 * nq / sh.group)) < sh.max_q)) nq *= 2;
+    while (16 * nq < sh.group) nq *= 2;
+    r.rows = 16 * nq;
+    r.tile_shift = log2_of(r.rows / sh.group);
+    r.step_shift = f32 ? 6 : 7;
+    r.workgroups = nq == 1 ? 512 : 256;
+    r.least = 1;
+    return r;
+}
+
+size_t paged_workspace(const CacheShape& sh) {
+    const PagedRoute r = paged_route(sh);
+    return (size_t)r.workgroups * 2 * r.rows * (kHeadDim + 2) * 4 + (4 + 4 * (size_t)r.workgroups) * 4;
+}
+
+hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st) {
+    const int nq = route.rows / 16;
+    if (sh.dtype == 0) {
+        if (sh.mxfp8) return nq == 1 ? launch<true, true, 1>(a, st) : nq == 2 ? launch<true, true, 2>(a, st) : launch<true, true, 4>(a, st);
+        return nq == 1 ? launch<true, false, 1>(a, st) : nq == 2 ? launch<true, false, 2>(a, st) : launch<true, false, 4>(a, st);
+    }
+    if (sh.mxfp8) return nq == 1 ? launch<false, true, 1>(a, st) : nq == 2 ? launch<false, true, 2>(a, st) : launch<false, true, 4>(a, st);
+    return nq == 1 ? launch<false, false, 1>(a, st) : nq == 2 ? launch<false, false, 2>(a, st) : launch<false, false, 4>(a, st);
+}
+
+hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
+                             float* lse, void* workspace, hipStream_t st) {
+    const PagedRoute route = paged_route(sh);
+    PagedArgs a;
+    a.q = q; a.cache = cache; a.table = table; a.q_start = q_start; a.kv_len = kv_len; a.out = out; a.lse = lse;
+    a.parts = (float*)workspace;
+    a.stats = a.parts + (size_t)route.workgroups * 2 * route.rows * kHeadDim;
+    a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
+    a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
+    a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
+    a.workgroups = route.workgroups; a.least = route.least;
+    a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
+    a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
+    hipError_t e = launch_paged_rows(sh, route, a, st);
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)route.workgroups, (unsigned)(route.rows == 16 ? 4 : route.rows / 16));
+    if (sh.dtype == 0) {
+        if (route.rows == 16) hipLaunchKernelGGL((join_kernel<float, 4>), grid, dim3(256), 0, st, a, route.rows);
+        else hipLaunchKernelGGL((join_kernel<float, 1>), grid, dim3(256), 0, st, a, route.rows);
+    } else {
+        if (route.rows == 16) hipLaunchKernelGGL((join_kernel<__bf16, 4>), grid, dim3(256), 0, st, a, route.rows);
+        else hipLaunchKernelGGL((join_kernel<__bf16, 1>), grid, dim3(256), 0, st, a, route.rows);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace cp

@@ -1,0 +1,92 @@
+"""Shared plumbing of the tests of the cache operators: pools, page tables, calls through the binding.  No arithmetic of the operators lives here."""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from oracle import cache_oracle as O
+from paper_2409_12490_amd import binding as B
+
+DEV = "cuda"
+DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+HALF_STEP = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
+
+
+def f64(t):
+    return t.detach().to("cpu").to(torch.float64).numpy()
+
+
+def randn(gen, *shape, dtype="bf16", scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(DTYPES[dtype])
+
+
+def side_by_side(gen, tokens, heads, dtype, extra=0, scale=1.0):
+    """Tensors [tokens, h, 128] for h in heads that lie in one [tokens, sum(heads) + extra, 128], on the GPU."""
+    wide = randn(gen, tokens, sum(heads) + extra, 128, dtype=dtype, scale=scale).to(DEV)
+    return wide.split(list(heads) + [extra], 1)[:len(heads)]
+
+
+class Pool:
+    """Pages for sequences of given lengths, in random order, everything that no token lies in filled with NaN."""
+
+    def __init__(self, gen, lengths, hkv, page, dtype="bf16", mxfp8=False, spare=3, scale=1.0):
+        self.page, self.mxfp8, self.hkv, self.dtype = page, mxfp8, hkv, dtype
+        counts = [-(-n // page) for n in lengths]
+        self.n_pages = sum(counts) + spare
+        order = torch.randperm(self.n_pages, generator=gen)
+        self.table = torch.full((len(lengths), max(counts + [1]) + 1), 0, dtype=torch.int32)
+        self.table[:] = torch.tensor([-1, 2 ** 30, -2 ** 31])[torch.arange(self.table.shape[1]) % 3].int()    # what no token lies in may be anything
+        at = 0
+        for i, c in enumerate(counts):
+            self.table[i, :c] = order[at:at + c].int()
+            at += c
+        self.slots = [(self.table[i, torch.arange(n) // page] * page + torch.arange(n) % page).int() for i, n in enumerate(lengths)]
+        shape = (self.n_pages, hkv, page, 128)
+        self.k, self.v = randn(gen, *shape, dtype=dtype, scale=scale), randn(gen, *shape, dtype=dtype)
+        used = torch.zeros(self.n_pages * page, dtype=torch.bool)
+        for s in self.slots:
+            used[s.long()] = True
+        used = used.view(self.n_pages, 1, page, 1)
+        if mxfp8:
+            (kc, ks), (vc, vs) = (O.mx_quantise(f64(x)) for x in (self.k, self.v))
+            fill = lambda x, w: torch.where(used, torch.from_numpy(x), torch.tensor(w, dtype=torch.uint8))   # noqa: E731
+            self.held_k, self.held_v = (torch.where(used, torch.from_numpy(O.mx_values(c, s)), float("nan")).numpy() for c, s in ((kc, ks), (vc, vs)))
+            self.cache = [fill(kc, 0x7f).to(DEV), fill(vc, 0xff).to(DEV), fill(ks, 0xff).to(DEV), fill(vs, 0xff).to(DEV)]
+        else:
+            k, v = (x.masked_fill(~used, float("nan")) for x in (self.k, self.v))
+            self.held_k, self.held_v = f64(k), f64(v)
+            self.cache = [k.to(DEV), v.to(DEV), None, None]
+
+
+def attend(pool, q, q_start, kv_len, table=None, max_q_len=0, out=None, scale=0.0, workspace=None):
+    table = (pool.table if table is None else table).to(DEV)
+    out = torch.full((q.shape[0], q.shape[1], 128), float("nan"), dtype=q.dtype, device=DEV) if out is None else out
+    lse = torch.full(q.shape[:2], float("nan"), device=DEV)
+    p = B.make_cache_params(q.shape[1], pool.hkv, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp8=pool.mxfp8, page_table=table, max_q_len=max_q_len,
+                            attn_scale=scale)
+    ws = B.alloc_paged_workspace(p) if workspace is None else workspace
+    ws.fill_(0xff)                                                   # whatever it holds
+    start, lens = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (q_start, kv_len))
+    B.critiprefill_paged_attn(p, q, *pool.cache, table, start, lens, out, lse, ws)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def check_attention(pool, q, q_start, kv_len, out, lse, table=None, scale=128 ** -0.5):
+    """Against fp64.  A logit's error: each product and sum in fp32, 2^-24 of its terms a rounding, fewer than 16 deep, and as much again for scaling and
+    exp2; out: twice that times the largest |v| for each of numerator and denominator, the rounding of P to bf16 (not fp32), sums of
+    fp32, and its own rounding."""
+    table = pool.table if table is None else table
+    dtype = pool.dtype
+    want, want_lse, size, logit = O.paged_attention(f64(q), pool.held_k, pool.held_v, pool.page, table.numpy(), q_start, kv_len, scale)
+    delta = 2.0 ** -20 * (logit + np.maximum(np.abs(np.where(np.isfinite(want_lse), want_lse, 0.0)), 1.0)) + 2.0 ** -20
+    got, got_lse = f64(out), f64(lse)
+    rounding = HALF_STEP["bf16"] * size * (dtype == "bf16") + HALF_STEP[dtype] * np.abs(want)
+    bound = rounding * 1.01 + 4 * delta[..., None] * size.max(-1, keepdims=True) + 1e-30
+    assert np.isfinite(got).all(), f"{(~np.isfinite(got)).sum()} values are not finite"
+    worst = np.max(np.abs(got - want) / bound) if got.size else 0.0
+    assert worst <= 1.0, f"out: {worst:.2f} of the bound, at {np.unravel_index(np.argmax(np.abs(got - want) / bound), got.shape)}"
+    empty = ~np.isfinite(want_lse)
+    assert (got_lse[empty] == -np.inf).all() and (got[empty] == 0).all()
+    err = np.abs(np.where(empty, 0.0, got_lse) - np.where(empty, 0.0, want_lse))
+    assert (err <= 2 * delta).all(), f"lse: {np.max(err / delta) / 2:.2f} of the bound"

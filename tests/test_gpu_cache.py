@@ -1,0 +1,207 @@
+"""Head norms with the position rotation, as tensors and into the cache, and the cache written and read, against fp64."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2409_12490_amd import binding as B
+from tests.cache_helpers import DEV, DTYPES, HALF_STEP, f64, randn, side_by_side
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(got, want, size, dtype):
+    """fp32 products and sums (a norm's sum of 128, an angle to 2^-23 of a turn, sine and cosine): under 32 roundings of the terms; then the output's own."""
+    bound = HALF_STEP[dtype] * np.abs(want) * 1.01 + 32 * 2.0 ** -24 * size + 1e-37
+    assert np.isfinite(got).all()
+    worst = np.max(np.abs(got - want) / bound)
+    assert worst <= 1.0, f"{worst:.2f} of the bound"
+
+
+#       dtype  hq hkv tokens rotary interleaved norm  positions
+ROPES = [
+    ("bf16", 32, 8, 1, 128, False, True, "far"),
+    ("bf16", 32, 8, 67, 128, False, True, "run"),
+    ("bf16", 3, 1, 130, 64, False, True, "far"),
+    ("bf16", 8, 2, 45, 96, False, False, "far"),
+    ("bf16", 5, 5, 33, 128, True, True, "negative"),
+    ("bf16", 4, 4, 20, 32, True, False, "far"),
+    ("bf16", 28, 4, 9, 0, False, True, "none"),
+    ("fp32", 8, 2, 259, 128, False, True, "far"),
+    ("fp32", 2, 1, 1, 16, False, True, "far"),
+    ("fp32", 1, 1, 2000, 64, True, True, "run"),
+    ("bf16", 8, 2, 4999, 128, False, True, "far"),
+]
+
+
+def _rope_inputs(case, extra=0):
+    dtype, hq, hkv, tokens, rotary, inter, norm, where = case
+    gen = torch.Generator().manual_seed(tokens * 131 + hq)
+    q, k, v = side_by_side(gen, tokens, (hq, hkv, hkv), dtype, extra=extra, scale=2.0)
+    pos = {"far": torch.randint(0, 1 << 20, (tokens,), generator=gen), "run": torch.arange(5000, 5000 + tokens),
+           "negative": torch.randint(-1 << 30, 0, (tokens,), generator=gen), "none": torch.zeros(tokens)}[where].int().to(DEV)
+    w = [(1 + 0.3 * torch.randn(128, generator=gen)).to(DTYPES[dtype]).to(DEV) if norm else None for _ in range(2)]
+    freq = B.rotary_frequencies(rotary) if rotary else None
+    return q, k, v, w, pos, freq
+
+
+def _wanted(case, x, w, pos, freq):
+    _, _, _, _, rotary, inter, _, _ = case
+    return O.norm_rope(f64(x), None if w is None else f64(w), pos.cpu().numpy(), None if freq is None else f64(freq), rotary, inter, 1e-5)
+
+
+@pytest.mark.parametrize("case", ROPES, ids=lambda c: "x".join(map(str, c)))
+def test_norm_rope(case):
+    dtype, hq, hkv, tokens, rotary, inter, _, _ = case
+    q, k, _, w, pos, freq = _rope_inputs(case, extra=1)
+    q_out = torch.full((tokens, hq + 2, 128), float("nan"), dtype=q.dtype, device=DEV)      # with a gap behind the heads
+    k_out = torch.full((hkv, tokens, 128), float("nan"), dtype=q.dtype, device=DEV).transpose(0, 1)   # head-major, as estimate may take it
+    p = B.make_cache_params(hq, hkv, q.dtype, q=q, k=k, out=q_out[:, :hq], k_out=k_out, rotary_dim=rotary, interleaved=inter, norm_eps=1e-5)
+    B.critiprefill_norm_rope(p, q, k, *w, freq, pos if rotary else None, q_out[:, :hq], k_out)
+    torch.cuda.synchronize()
+    _check(f64(q_out[:, :hq]), *_wanted(case, q, w[0], pos, freq), dtype)
+    _check(f64(k_out), *_wanted(case, k, w[1], pos, freq), dtype)
+    assert torch.isnan(q_out[:, hq:]).all()
+    # in place
+    qi, ki = q.clone(), k.clone()
+    p = B.make_cache_params(hq, hkv, q.dtype, q=qi, k=ki, out=qi, k_out=ki, rotary_dim=rotary, interleaved=inter, norm_eps=1e-5)
+    B.critiprefill_norm_rope(p, qi, ki, *w, freq, pos if rotary else None, qi, ki)
+    assert torch.equal(qi, q_out[:, :hq]) and torch.equal(ki, k_out)
+
+
+def _check_held(got, want, size, dtype, mxfp8):
+    """got: held values of a cache.  8 bits: half a step of e4m3 (2^-4 of the value, 2^-10 of the scale below its normal range) from a value that is
+    itself off as above; the scale can be the next one where the maximum is that near to 448 of its units."""
+    if not mxfp8:
+        return _check(got, want, size, dtype)
+    e = O.mx_scale(want * (1 + 2.0 ** -16))
+    step = (2.0 ** (e.astype(np.float64) - 127.0) * 2.0 ** -10)[..., None] * np.ones(32)
+    bound = 2.0 ** -4 * np.abs(want) * 1.01 + step.reshape(want.shape) + 32 * 2.0 ** -24 * size
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= bound).all(), f"{np.max(np.abs(got - want) / bound):.2f} of the bound"
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("case", ROPES, ids=lambda c: "x".join(map(str, c)))
+def test_norm_rope_write(case, mxfp8):
+    dtype, hq, hkv, tokens, rotary, inter, _, _ = case
+    q, k, v, w, pos, freq = _rope_inputs(case)
+    page, n_pages = 16, tokens // 16 + 3
+    gen = torch.Generator().manual_seed(3)
+    slots = torch.randperm(n_pages * page, generator=gen)[:tokens].int()
+    outside = torch.rand(tokens, generator=gen) < 0.1
+    slots = torch.where(outside, torch.tensor([-1, n_pages * page, -2 ** 31, 2 ** 31 - 1])[torch.arange(tokens) % 4].int(), slots).to(DEV)
+    cache = B.alloc_cache(n_pages, hkv, page, q.dtype, mxfp8)
+    for c in cache:
+        if c is not None:
+            c.fill_(3)
+    q_out = torch.full((tokens, hq, 128), float("nan"), dtype=q.dtype, device=DEV)
+    p = B.make_cache_params(hq, hkv, q.dtype, q=q, k=k, v=v, out=q_out, k_cache=cache[0], mxfp8=mxfp8, rotary_dim=rotary, interleaved=inter, norm_eps=1e-5)
+    B.critiprefill_norm_rope_write(p, q, k, v, *w, freq, pos if rotary else None, slots, q_out, *cache)
+    torch.cuda.synchronize()
+    _check(f64(q_out), *_wanted(case, q, w[0], pos, freq), dtype)
+    flat = [None if c is None else c.transpose(1, 2).flatten(0, 1).cpu() for c in cache]      # [slots, heads, row]
+    kept = (~outside).nonzero()[:, 0]
+    at = slots.cpu()[kept].long()
+    rest = torch.ones(n_pages * page, dtype=torch.bool)
+    rest[at] = False
+    assert all((c[rest] == 3).all() for c in flat if c is not None)                           # nothing else is written
+    wk, sk = _wanted(case, k, w[1], pos, freq)
+    for c, s, want, size in ((flat[0], flat[2], wk, sk), (flat[1], flat[3], f64(v), np.zeros(v.shape))):
+        held = O.mx_values(c[at].numpy(), s[at].numpy()) if mxfp8 else f64(c[at])
+        _check_held(held, want[kept.numpy()], size[kept.numpy()], dtype, mxfp8)
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("dtype,hkv,page,tokens,fused", [("bf16", 8, 64, 1, True), ("bf16", 1, 16, 777, False), ("fp32", 3, 32, 130, True), ("bf16", 4, 256, 5000, True)])
+def test_write_and_read(dtype, hkv, page, tokens, fused, mxfp8):
+    gen = torch.Generator().manual_seed(tokens)
+    k, v = side_by_side(gen, tokens, (hkv, hkv), dtype, extra=3 if fused else 0)
+    k = (k * 2.0 ** torch.randint(-30, 30, (tokens, hkv, 1), generator=gen).to(DEV)).to(v.dtype)
+    if fused:
+        wide = torch.cat([k, v, v], 1)
+        k, v = wide[:, :hkv], wide[:, hkv:2 * hkv]
+    n_pages = tokens // page + 2
+    slots = torch.randperm(n_pages * page, generator=gen)[:tokens].int().to(DEV)
+    cache = B.alloc_cache(n_pages, hkv, page, k.dtype, mxfp8)
+    p = B.make_cache_params(hkv, hkv, k.dtype, k=k, v=v, k_cache=cache[0], mxfp8=mxfp8)
+    B.critiprefill_cache_write(p, k, v, slots, *cache)
+    ko, vo = (torch.full((tokens, hkv + 1, 128), float("nan"), dtype=k.dtype, device=DEV)[:, :hkv] for _ in range(2))
+    back = torch.cat([slots, torch.tensor([-1, n_pages * page], dtype=torch.int32, device=DEV)])
+    p = B.make_cache_params(hkv, hkv, k.dtype, k=ko, v=vo, k_cache=cache[0], mxfp8=mxfp8)
+    B.critiprefill_cache_read(p, slots, *cache, ko, vo)
+    torch.cuda.synchronize()
+    for x, y in ((k, ko), (v, vo)):
+        want = f64(x)
+        if mxfp8:
+            want = O.mx_values(*O.mx_quantise(want))                # whole powers of two: nothing else is rounded
+        assert np.array_equal(f64(y), want)
+    two = [torch.full((tokens + 2, hkv, 128), 7.0, dtype=k.dtype, device=DEV) for _ in range(2)]
+    p = B.make_cache_params(hkv, hkv, k.dtype, k=two[0], v=two[1], k_cache=cache[0], mxfp8=mxfp8)
+    B.critiprefill_cache_read(p, back, *cache, *two)
+    assert torch.equal(two[0][:tokens], ko) and torch.equal(two[1][:tokens], vo) and not two[0][tokens:].any() and not two[1][tokens:].any()
+
+
+def test_borders_of_the_8_bit_format():
+    rows = []
+    grid = O._GRID
+    ties = (grid[1:] + grid[:-1]) / 2
+    for top in (448.0, 449.0, 447.0, 300.0, 256.0, 255.0):          # the block's maximum decides the scale
+        for part in np.array_split(np.concatenate([grid, ties, -ties, ties * (1 + 2.0 ** -12)]), 20):
+            b = np.zeros(32)
+            b[:min(31, len(part))] = part[:31]
+            b[31] = top
+            rows.append(b)
+    rows += [np.zeros(32), np.full(32, 2.0 ** -149), np.full(32, -2.0 ** -126), np.full(32, 3.4e38), np.array([3.4e38] + [1e-38] * 31)]
+    x = np.concatenate(rows + [np.zeros(32)] * (-len(rows) % 4)).reshape(-1, 1, 128).astype(np.float32)
+    x = torch.from_numpy(x).to(DEV)
+    n = x.shape[0]
+    cache = B.alloc_cache(n // 16 + 1, 1, 16, torch.float32, True)
+    slots = torch.arange(n, dtype=torch.int32, device=DEV)
+    p = B.make_cache_params(1, 1, torch.float32, k=x, v=x, k_cache=cache[0], mxfp8=True)
+    B.critiprefill_cache_write(p, x, x, slots, *cache)
+    torch.cuda.synchronize()
+    codes, e = O.mx_quantise(f64(x))
+    for c, s in (cache[::2], cache[1::2]):
+        assert np.array_equal(s.cpu().numpy()[:, 0].reshape(-1, 4)[:n], e[:, 0])
+        assert np.array_equal(c.cpu().numpy()[:, 0].reshape(-1, 128)[:n], codes[:, 0])
+
+
+def test_values_that_are_not_finite():
+    x = torch.ones((3, 1, 128), device=DEV)
+    x[0, 0, 5], x[1, 0, 40], x[2, 0, 127] = float("inf"), float("nan"), float("-inf")
+    cache = B.alloc_cache(1, 1, 16, torch.float32, True)
+    slots = torch.arange(3, dtype=torch.int32, device=DEV)
+    p = B.make_cache_params(1, 1, torch.float32, k=x, v=x, k_cache=cache[0], mxfp8=True)
+    B.critiprefill_cache_write(p, x, x, slots, *cache)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    B.critiprefill_cache_read(p, slots, *cache, y, z)
+    assert torch.equal(torch.isnan(y), ~torch.isfinite(x)) and (y[torch.isfinite(x)] == 1).all() and torch.equal(torch.isnan(z), torch.isnan(y))
+
+
+def test_places_beyond_32_bits_of_offset():
+    hkv, page, n_pages = 8, 64, 36000                               # 4.7 GB of K
+    cache = B.alloc_cache(n_pages, hkv, page)
+    gen = torch.Generator().manual_seed(1)
+    k, v = side_by_side(gen, 100, (hkv, hkv), "bf16")
+    slots = (torch.randperm(5000, generator=gen)[:100] + (n_pages * page - 5000)).int().to(DEV)
+    p = B.make_cache_params(hkv, hkv, k.dtype, k=k, v=v, k_cache=cache[0])
+    B.critiprefill_cache_write(p, k, v, slots, *cache)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    p = B.make_cache_params(hkv, hkv, k.dtype, k=ko, v=vo, k_cache=cache[0])
+    B.critiprefill_cache_read(p, slots, *cache, ko, vo)
+    assert torch.equal(ko, k) and torch.equal(vo, v)
+
+
+def test_another_stream():
+    gen = torch.Generator().manual_seed(2)
+    q, k, v = (randn(gen, 4000, 4, 128).to(DEV) for _ in range(3))
+    pos, freq = torch.arange(4000, dtype=torch.int32, device=DEV), B.rotary_frequencies()
+    outs = [torch.zeros_like(q) for _ in range(4)]
+    p = B.make_cache_params(4, 4, q.dtype, q=q, k=k, out=outs[0], k_out=outs[1], rotary_dim=128)
+    B.critiprefill_norm_rope(p, q, k, None, None, freq, pos, outs[0], outs[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    B.critiprefill_norm_rope(p, q, k, None, None, freq, pos, outs[2], outs[3], stream=side)
+    side.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
