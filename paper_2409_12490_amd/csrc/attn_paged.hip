@@ -461,7 +461,12 @@ int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        //
 PagedRoute paged_route(const CacheShape& sh) {
     PagedRoute r;
     const bool f32 = sh.dtype == 0;
-    r.chunk = 0;
+    // More rows a KV head than the smaller tiles hold: tiles of 256 rows, whose keys are read once for all of them
+    r.chunk = !f32 && (long long)sh.max_q * sh.group > 64;
+    if (r.chunk) {
+        r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2;
+        return r;
+    }
     int nq = 1;
     while (nq < (f32 ? 2 : 4) && (16 * nq / sh.group < 1 || (1 << log2_of(16 * nq / sh.group)) < sh.max_q)) nq *= 2;
     while (16 * nq < sh.group) nq *= 2;
@@ -492,15 +497,17 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
                              float* lse, void* workspace, hipStream_t st) {
     const PagedRoute route = paged_route(sh);
     PagedArgs a;
-    a.q = q; a.cache = cache; a.table = table; a.q_start = q_start; a.kv_len = kv_len; a.out = out; a.lse = lse;
+    a.q = q; a.cache = cache; a.table = sh.max_pages ? table : kv_len; a.q_start = q_start; a.kv_len = kv_len; a.out = out; a.lse = lse;
     a.parts = (float*)workspace;
     a.stats = a.parts + (size_t)route.workgroups * 2 * route.rows * kHeadDim;
     a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
     a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
     a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
     a.workgroups = route.workgroups; a.least = route.least;
+    a.by_group = FastDiv(sh.group);
     a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
     a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
+    if (route.chunk) return launch_paged_chunk(sh, a, st);
     hipError_t e = launch_paged_rows(sh, route, a, st);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)route.workgroups, (unsigned)(route.rows == 16 ? 4 : route.rows / 16));

@@ -20,6 +20,7 @@ struct PagedArgs {
     int tokens, n_seqs, max_pages, n_pages, hq, hkv, group;
     int page_shift, tile_shift, step_shift;
     unsigned workgroups, least;
+    FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
 };
@@ -47,8 +48,10 @@ struct Sequence {                             // one sequence, checked: whatever
         if (j == tiles - 1) return max(1u, (unsigned)(keys + (1 << step_shift) - 1) >> step_shift);   // its last token sees all keys
         return ahead + ((unsigned)(((j + 1) << tile_shift) + (1 << step_shift) - 1) >> step_shift);
     }
-    __device__ __forceinline__ void load(const PagedArgs& a, int s) {
-        const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
+    // uniform: s is the same in all lanes, and so is what follows
+    __device__ __forceinline__ void load(const PagedArgs& a, int s, bool uniform) {
+        int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
+        if (uniform) { from = first_lane(from); to = first_lane(to); held = first_lane(held); }
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
@@ -69,15 +72,15 @@ struct Run {
         Sequence s;
         for (int base = 0; base < a.n_seqs; base += 64) {
             mine = 0;
-            if (base + lane < a.n_seqs) { s.load(a, base + lane); mine = s.steps * (unsigned)a.hkv; }
+            if (base + lane < a.n_seqs) { s.load(a, base + lane, false); mine = s.steps * (unsigned)a.hkv; }
             upto = mine;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(upto, d); if (lane >= d) upto += o; }
             total += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
         }
         if (total == 0) return false;
-        share = max(a.least, (total + a.workgroups - 1) / a.workgroups);
-        used = (total + share - 1) / share;
+        share = max(a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
+        used = (unsigned)first_lane((int)((total + share - 1) / share));
         // neighbouring runs share keys (tiles of one head) and go to one XCD (workgroup id mod 8)
         logical = (workgroup & 7) * ((used + 7) / 8) + (workgroup >> 3);
         if ((workgroup >> 3) >= (used + 7) / 8 || logical >= used) return false;
@@ -87,7 +90,7 @@ struct Run {
         for (int base = 0; base < a.n_seqs; base += 64) {
             if (a.n_seqs > 64) {
                 mine = 0;
-                if (base + lane < a.n_seqs) { s.load(a, base + lane); mine = s.steps * (unsigned)a.hkv; }
+                if (base + lane < a.n_seqs) { s.load(a, base + lane, false); mine = s.steps * (unsigned)a.hkv; }
                 upto = mine;
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(upto, d); if (lane >= d) upto += o; }
@@ -97,8 +100,8 @@ struct Run {
                 const int at = __builtin_ctzll(behind);
                 unsigned rest = begin - past - (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), at);
                 seq = base + at;
-                now.load(a, seq);
-                head = (int)(rest / now.steps);
+                now.load(a, seq, true);
+                head = first_lane((int)(rest / now.steps));
                 rest -= (unsigned)head * now.steps;
                 int lo = 0, hi = now.tiles - 1;                    // the last tile that begins at or before it
                 while (lo < hi) {
@@ -122,7 +125,7 @@ struct Run {
         head = 0;
         do {
             if (++seq >= a.n_seqs) return false;
-            now.load(a, seq);
+            now.load(a, seq, true);
         } while (now.tiles == 0);
         return true;
     }
@@ -131,6 +134,6 @@ struct Run {
 }  // namespace
 
 hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st);
-hipError_t launch_paged_chunk(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st);
+hipError_t launch_paged_chunk(const CacheShape& sh, const PagedArgs& a, hipStream_t st);
 
 }  // namespace cp
