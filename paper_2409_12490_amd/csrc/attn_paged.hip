@@ -82,6 +82,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
     if (!any) return;
     const unsigned home = run.logical;
     if (tid == 0) a.record[4 + 4 * home + 3] = 0;
+    if (!run.has_steps(a)) return;
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
     const int page_mask = (1 << a.page_shift) - 1;
 
@@ -89,7 +90,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
         const Sequence seq = run.now;
         const int tile_tokens = 1 << a.tile_shift, t0 = run.tile << a.tile_shift;
         const int live = min(tile_tokens, seq.tokens - t0);                    // tokens of the tile
-        const unsigned unit = seq.steps_of(run.tile, a.tile_shift, a.step_shift), first = run.step, count = min(run.left, unit - first);
+        unsigned first, count, unit;
+        run.piece(a, first, count, unit);
         const int head = run.head;
         const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)run.seq * a.max_pages);
         const int past = seq.keys - seq.tokens;                                // position of the sequence's first new token
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
         int last[NQ];                                                          // the last key that the row sees
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
-            const int r = 16 * nq + c16, t = min(r / a.group, live - 1), g = r - r / a.group * a.group;
+            const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, live - 1), g = r - of * a.group;
             last[nq] = min(past + t0 + t, seq.keys - 1);
             const int64_t at = (seq.start + t0 + t) * a.qs0 + (int64_t)(head * a.group + g) * a.qs1 + 32 * kg;
             if (F32) {
@@ -129,14 +131,14 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int u = key_of(step) + 16 * g;
-                entry[g] = u <= high && step < first + count ? table[u >> a.page_shift] : -1;
+                entry[g] = table[max(min(u, high), 0) >> a.page_shift];        // no branch; whether the keys are there is asked in load
             }
         };
         auto load = [&](Raw<F32, MX>& raw, int (&seen)[kGroups], unsigned step) __attribute__((always_inline)) {
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int u = key_of(step) + 16 * g;
-                const bool there = (unsigned)entry[g] < (unsigned)a.n_pages;
+                const bool there = (unsigned)entry[g] < (unsigned)a.n_pages && u <= high;
                 seen[g] = there ? seq.keys - u : 0;                            // keys of the group that exist
                 const int64_t row = (((int64_t)(there ? entry[g] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
                 const char* kp = (const char*)a.cache.k + row * kRowBytes;
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             const int r = 16 * nq + (tid >> 4), piece = tid & 15;              // 8 channels
-            const int t = r / a.group, g = r - t * a.group;
+            const int t = (int)a.by_group.div((unsigned)r), g = r - t * a.group;
             if (t >= live) continue;
             float M = -INFINITY, L = 0.f, sum[8];
 #pragma unroll
@@ -378,78 +380,17 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
             int32_t* rec = a.record + 4 + 4 * home;
             rec[0] = seq.start + t0; rec[1] = live; rec[2] = head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
         }
-        run.left -= count;
-        if (run.left == 0 || !run.next(a)) break;
+        if (!run.next_steps(a)) break;
     }
-}
-
-// Adds up the parts of units that more than one workgroup worked on.  PG groups of threads take every PG-th part of a row.
-template <typename T, int PG>
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    __shared__ __attribute__((aligned(16))) float rest[PG > 1 ? 16 * 128 : 4];
-    __shared__ float rest_l[16];
-    const unsigned w = blockIdx.x;
-    if (w >= (unsigned)a.record[0]) return;
-    const int32_t* rec = a.record + 4 + 4 * w;
-    const int parts = rec[3];
-    if (parts < 2) return;
-    constexpr int kPer = 16 / PG;
-    const int tid = threadIdx.x, piece = tid & 15, pg = (tid >> 4) / kPer, local = (tid >> 4) % kPer;
-    const int r = blockIdx.y * kPer + local, t = r / a.group, g = r - t * a.group;
-    const bool live = t < rec[1];
-    if (blockIdx.y * kPer >= rec[1] * a.group) return;
-    const float c = a.scale_log2e;
-    float M = -INFINITY, L = 0.f;
-    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-    if (live) {
-        auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-        for (int x = 0; x < parts; ++x) M = fmaxf(M, a.stats[2 * (slot(x) * rows + r)]);
-        const float M_safe = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-        for (int x = pg; x < parts; x += PG) {
-            const f32x2 ml = *(const f32x2*)(a.stats + 2 * (slot(x) * rows + r));
-            const float* from = a.parts + (slot(x) * rows + r) * kHeadDim + 8 * piece;
-            const f32x4 v0 = *(const f32x4*)from, v1 = *(const f32x4*)(from + 4);
-            const float f = __builtin_amdgcn_exp2f((ml[0] - M_safe) * c);
-            L = fmaf(f, ml[1], L);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { lo[e] = fmaf(f, v0[e], lo[e]); hi[e] = fmaf(f, v1[e], hi[e]); }
-        }
-    }
-    if (PG > 1) {
-        float* mine = rest + (tid >> 4) * 128 + 8 * piece;
-        *(f32x4*)mine = lo; *(f32x4*)(mine + 4) = hi;
-        if (piece == 0) rest_l[tid >> 4] = L;
-        __syncthreads();
-        if (pg != 0) return;
-#pragma unroll
-        for (int x = 1; x < PG; ++x) {
-            lo += *(const f32x4*)(mine + x * kPer * 128); hi += *(const f32x4*)(mine + x * kPer * 128 + 4);
-            L += rest_l[local + x * kPer];
-        }
-    }
-    if (!live) return;
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
-    const int64_t row = rec[0] + t;
-    const int h = rec[2] * a.group + g;
-    const int64_t at = row * a.os0 + h * a.os1 + 8 * piece;
-    lo *= inv; hi *= inv;
-    if constexpr (sizeof(T) == 4) {
-        *(f32x4*)((float*)a.out + at) = lo; *(f32x4*)((float*)a.out + at + 4) = hi;
-    } else {
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] = (__bf16)lo[e]; v[4 + e] = (__bf16)hi[e]; }
-        *(bf16x8*)((__bf16*)a.out + at) = v;
-    }
-    if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
 }
 
 template <bool F32, bool MX, int NQ>
 hipError_t launch(const PagedArgs& a, hipStream_t st) {
     constexpr int smem = 4 * 16 * NQ * (kHeadDim + 2) * 4;
-    const hipError_t e = hipFuncSetAttribute((const void*)paged_rows_kernel<F32, MX, NQ>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != hipSuccess) return e;
+    if (smem > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)paged_rows_kernel<F32, MX, NQ>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL((paged_rows_kernel<F32, MX, NQ>), dim3(a.workgroups), dim3(kThreads), smem, st, a);
     return hipGetLastError();
 }
@@ -464,7 +405,7 @@ PagedRoute paged_route(const CacheShape& sh) {
     // More rows a KV head than the smaller tiles hold: tiles of 256 rows, whose keys are read once for all of them
     r.chunk = !f32 && (long long)sh.max_q * sh.group > 64;
     if (r.chunk) {
-        r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2;
+        r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
         return r;
     }
     int nq = 1;
@@ -475,6 +416,7 @@ PagedRoute paged_route(const CacheShape& sh) {
     r.step_shift = f32 ? 6 : 7;
     r.workgroups = nq == 1 ? 512 : 256;
     r.least = 1;
+    r.setup = 1;
     return r;
 }
 
@@ -503,21 +445,17 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
     a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
     a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
-    a.workgroups = route.workgroups; a.least = route.least;
+    a.workgroups = route.workgroups; a.least = route.least; a.setup = route.setup;
     a.by_group = FastDiv(sh.group);
     a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
     a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
     if (route.chunk) return launch_paged_chunk(sh, a, st);
     hipError_t e = launch_paged_rows(sh, route, a, st);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)route.workgroups, (unsigned)(route.rows == 16 ? 4 : route.rows / 16));
-    if (sh.dtype == 0) {
-        if (route.rows == 16) hipLaunchKernelGGL((join_kernel<float, 4>), grid, dim3(256), 0, st, a, route.rows);
-        else hipLaunchKernelGGL((join_kernel<float, 1>), grid, dim3(256), 0, st, a, route.rows);
-    } else {
-        if (route.rows == 16) hipLaunchKernelGGL((join_kernel<__bf16, 4>), grid, dim3(256), 0, st, a, route.rows);
-        else hipLaunchKernelGGL((join_kernel<__bf16, 1>), grid, dim3(256), 0, st, a, route.rows);
-    }
+    // a workgroup of the join takes a row at a time; more rows than the grid has, where a chunk is longer than was said, come in turn
+    const dim3 grid((unsigned)route.workgroups, (unsigned)std::min<long long>(16, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group));
+    if (sh.dtype == 0) hipLaunchKernelGGL((join_kernel<float, 8, false>), grid, dim3(256), 0, st, a, route.rows);
+    else hipLaunchKernelGGL((join_kernel<__bf16, 8, false>), grid, dim3(256), 0, st, a, route.rows);
     return hipGetLastError();
 }
 

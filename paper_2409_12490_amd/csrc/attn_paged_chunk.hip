@@ -31,25 +31,17 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
     return r;
 }
 
-template <bool MX>
-__global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    Run run;
-    const bool any = run.find(a, workgroup_id(), thread_id() & 63);
-    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = any ? (int)run.used : 0;
-    if (!any) return;
-    const unsigned home = run.logical;
-    if (thread_id() == 0) a.record[4 + 4 * home + 3] = 0;
+// All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
+// around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
+template <bool MX, bool ROTATED>
+__device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home, unsigned lds0) {
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
-
     while (true) {
         // What follows from the thread's number is worked out for each unit: kept from one to the next it would be spilled, 60 registers of it.
         int tid = thread_id();
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63, l32 = lane & 31, hh = lane >> 5, r4 = lane >> 4, pch = lane & 15;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const bool rotated = wave >= 4;                              // shares its SIMD with wave - 4
         // ---- per-lane LDS addresses (bytes, ring slot 0), see attn_bf16.hip
         const unsigned k_base = (lds0 + kKOff + l32 * 256) | (unsigned)(((l32 & 15) ^ hh) << 4);
         const int i16 = lane & 15, gbit = (lane >> 4) & 1;
@@ -64,7 +56,8 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
 
         const Sequence seq = run.now;
         const int t0 = run.tile << a.tile_shift, live = min(1 << a.tile_shift, seq.tokens - t0), head = run.head;
-        const unsigned unit = seq.steps_of(run.tile, a.tile_shift, a.step_shift), first = run.step, count = min(run.left, unit - first);
+        unsigned first, count, unit;
+        run.piece(a, first, count, unit);
         const int ntiles = (int)count, base0 = (int)first * TK;
         const scalar_list table = (scalar_list)(unsigned long long)uniform_ptr(a.table + (int64_t)run.seq * a.max_pages);
         const int past = seq.keys - seq.tokens;
@@ -120,7 +113,10 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
             }
         };
         auto base = [&](int x) { return base0 + x * TK; };
-        auto bare = [&](int x, int bits) { return base(x) + TK - 1 > high || bits != 15; };   // it has rows that no row sees
+        int high_v = high;
+        asm("" : "+v"(high_v));                                      // like wq_lo
+        auto in_vector = [](int x) { asm("" : "+v"(x)); return x; };
+        auto bare = [&](int x, int bits) { return base(x) + TK - 1 > high_v || in_vector(bits) != 15; };   // it has rows that no row sees
         auto issue_k = [&](int slot) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -135,25 +131,25 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = 32 * i + 4 * wave + r4;
-                if (base(x) + row > high || !((bits >> (row >> 4)) & 1))
+                if (base(x) + row > high_v || !((bits >> (row >> 4)) & 1))
                     *LDS_PTR(u32x4, lds0 + kVOff + slot * kTileBytes + (32 * i + 4 * wave) * 256 + lane * 16) = u32x4{0, 0, 0, 0};
             }
         };
         // 8-bit: the tile in flight
         u32x4 raw_k, raw_v; unsigned scale_k = 0, scale_v = 0;
         auto load_raw = [&]() __attribute__((always_inline)) {       // of the tile described last
-            const int64_t row = at[0] + (xrow & 7);
-            raw_k = *(const u32x4*)((const char*)a.cache.k + row * 128 + 16 * xpiece);
-            raw_v = *(const u32x4*)((const char*)a.cache.v + row * 128 + 16 * xpiece);
-            scale_k = a.cache.ks[row * 4 + (xpiece >> 1)];
-            scale_v = a.cache.vs[row * 4 + (xpiece >> 1)];
+            const unsigned in_rows = (unsigned)lane * 16, in_scales = (unsigned)(lane >> 3) * 4 + (unsigned)((lane & 7) >> 1);   // eight rows of a wave
+            raw_k = *(const u32x4*)(uniform_ptr((const char*)a.cache.k + at[0] * 128) + in_rows);
+            raw_v = *(const u32x4*)(uniform_ptr((const char*)a.cache.v + at[0] * 128) + in_rows);
+            scale_k = (uniform_ptr(a.cache.ks + at[0] * 4))[in_scales];
+            scale_v = (uniform_ptr(a.cache.vs + at[0] * 4))[in_scales];
         };
         auto store_raw = [&](int x, int bits, int slot) __attribute__((always_inline)) {
             const float sk = __uint_as_float(scale_k << 23), sv = __uint_as_float(scale_v << 23);
             u32x4 k2[2] = {widen8(raw_k[0], raw_k[1], sk), widen8(raw_k[2], raw_k[3], sk)};
             u32x4 v2[2] = {widen8(raw_v[0], raw_v[1], sv), widen8(raw_v[2], raw_v[3], sv)};
             if (bare(x, bits)) {
-                if (base(x) + xrow > high || !((bits >> (xrow >> 4)) & 1)) v2[0] = v2[1] = u32x4{0, 0, 0, 0};
+                if (base(x) + xrow > high_v || !((bits >> (xrow >> 4)) & 1)) v2[0] = v2[1] = u32x4{0, 0, 0, 0};
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -246,7 +242,7 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
         auto pv = [&](const bf16x8 (&pf)[4]) __attribute__((always_inline)) { f32x16 no_s[2]; run_frags(1, no_s, pf); };
         auto mm_both = [&](f32x16 (&s)[2], const bf16x8 (&pf)[4]) __attribute__((always_inline)) { zero_s(s); run_frags(2, s, pf); };
         auto mask_if_needed = [&](f32x16 (&s)[2], int x, int bits) {
-            if (base(x) + TK - 1 <= wq_lo && bits == 15) return;
+            if (base(x) + TK - 1 <= wq_lo && in_vector(bits) == 15) return;
             int lim = qpos - base(x) - 4 * hh;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
@@ -315,17 +311,40 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
             return issued;
         };
 
-        // ---- prologue: tiles 0 to 3 are described, K and V of tiles 0 and 1 and K of tile 2 asked for (8-bit: 0 and 1 stored, 2 asked for)
+        // ---- prologue: the pages of tiles 0 to 3 are looked up at once; K and V of tiles 0 and 1 are asked for, then, when Q has left its place, K of tile 2
+        // (8-bit: 0 and 1 are stored, 2 asked for)
         at[0] = at[1] = 0;
-        look_up(0); describe(0);
-        if (MX) { load_raw(); }
-        else { issue_k(0); issue_v(0, true); }
+        int ahead[4][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            look_up(x);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) ahead[x][g] = entry[g];
+        }
+        auto describe_first = [&](int x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) entry[g] = ahead[x][g];
+            describe(x);
+        };
+        describe_first(0);
         const int bits0 = ok[3];
-        look_up(1);
-        if (MX) store_raw(0, bits0, 0);
-        describe(1);
-        if (MX) { if (ntiles > 1) { load_raw(); store_raw(1, ok[3], 1); } }
-        else issue_k(1);
+        if (MX) {
+            load_raw();
+            const u32x4 k0 = raw_k, v0 = raw_v;
+            const unsigned sk0 = scale_k, sv0 = scale_v;
+            describe_first(1);
+            load_raw();
+            const u32x4 k1 = raw_k, v1 = raw_v;
+            const unsigned sk1 = scale_k, sv1 = scale_v;
+            raw_k = k0; raw_v = v0; scale_k = sk0; scale_v = sv0;
+            store_raw(0, bits0, 0);
+            raw_k = k1; raw_v = v1; scale_k = sk1; scale_v = sv1;
+            store_raw(1, ok[3], 1);
+        } else {
+            issue_k(0); issue_v(0, true);
+            describe_first(1);
+            issue_k(1); issue_v(1, true);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (!MX && bare(0, bits0)) zero_v(0, bits0, 0);
 #pragma unroll
@@ -333,15 +352,15 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) pin(qf[ks]);
         __syncthreads();                                             // nobody reads Q in LDS any more
-        look_up(2); describe(2);
+        describe_first(2);
         if (MX) { if (ntiles > 2) load_raw(); }
-        else { issue_v(1, false); issue_k(2); }
-        look_up(3); describe(3);
+        else issue_k(2);
+        describe_first(3);
         // now ok[0 .. 3] are of tiles 0 .. 3, at of tile 3, v_at of tile 2
 
         f32x16 s[2]; bf16x8 pf[4];
         auto tile_active = [&](int x) { return x < ntiles && base(x) <= wq_last; };
-        if (!rotated) {
+        if constexpr (!ROTATED) {
             // step t: ka points into the slot of K(t), va into the slot of V(t-1)
             bool have_p = false, act = tile_active(0);
             va_slot = NBUF - 1;
@@ -440,47 +459,24 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
                 rec[0] = seq.start + t0; rec[1] = live; rec[2] = head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
             }
         }
-        run.left -= count;
-        if (run.left == 0 || !run.next(a)) break;
+        if (!run.next_steps(a)) break;
         __syncthreads();                                             // the staging has been read
     }
 }
 
-// Adds up the parts of units that more than one workgroup worked on: a thread takes 8 channels of a row, neighbouring threads neighbouring rows.
-__global__ __launch_bounds__(256) void chunk_join_kernel(PagedArgs a) {
-    const unsigned w = blockIdx.x;
-    if (w >= (unsigned)a.record[0]) return;
-    const int32_t* rec = a.record + 4 + 4 * w;
-    const int parts = rec[3];
-    if (parts < 2) return;
-    const int tid = threadIdx.x, r = blockIdx.y * 16 + (tid & 15), piece = tid >> 4;
-    if (r >= rec[1] * a.group) return;
-    const float c = a.scale_log2e;
-    auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-    float M = -INFINITY, L = 0.f;
-    for (int x = 0; x < parts; ++x) M = fmaxf(M, a.stats[2 * (slot(x) * kChunkRows + r)]);
-    const float M_safe = M == -INFINITY ? 0.f : M;
-    float sum[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-#pragma unroll 2
-    for (int x = 0; x < parts; ++x) {
-        const float* ml = a.stats + 2 * (slot(x) * kChunkRows + r);
-        const float f = __builtin_amdgcn_exp2f((ml[0] - M_safe) * c);
-        L = fmaf(f, ml[1], L);
-        const float* from = a.parts + slot(x) * kChunkRows * kHeadDim + (r >> 5) * (WQ * kHeadDim) + piece * 256 + (r & 31) * 4;
-        const float4 lo = *(const float4*)from, hi = *(const float4*)(from + 128);
-        sum[0] = fmaf(f, lo.x, sum[0]); sum[1] = fmaf(f, lo.y, sum[1]); sum[2] = fmaf(f, lo.z, sum[2]); sum[3] = fmaf(f, lo.w, sum[3]);
-        sum[4] = fmaf(f, hi.x, sum[4]); sum[5] = fmaf(f, hi.y, sum[5]); sum[6] = fmaf(f, hi.z, sum[6]); sum[7] = fmaf(f, hi.w, sum[7]);
-    }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
-    const int t = (int)a.by_group.div((unsigned)r), h = rec[2] * a.group + r - t * a.group;
-    const int64_t row = rec[0] + t;
-    bf16x8 v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (__bf16)(sum[e] * inv);
-    *(bf16x8*)((__bf16*)a.out + row * a.os0 + h * a.os1 + 8 * piece) = v;
-    if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + __logf(L);
+template <bool MX>
+__global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    Run run;
+    const bool any = run.find(a, workgroup_id(), thread_id() & 63);
+    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = any ? (int)run.used : 0;
+    if (!any) return;
+    const unsigned home = run.logical;
+    if (thread_id() == 0) a.record[4 + 4 * home + 3] = 0;
+    if (!run.has_steps(a)) return;
+    if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<MX, false>(a, run, home, lds0);
+    else work<MX, true>(a, run, home, lds0);
 }
 
 template <bool MX>
@@ -488,7 +484,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t st) {
     const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(paged_chunk_kernel<MX>, dim3(a.workgroups), dim3(512), kSmem, st, a);
-    hipLaunchKernelGGL(chunk_join_kernel, dim3(a.workgroups, kChunkRows / 16), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((join_kernel<__bf16, 1, true>), dim3(a.workgroups, kChunkRows / 32 * 4), dim3(256), 0, st, a, kChunkRows);
     return hipGetLastError();
 }
 

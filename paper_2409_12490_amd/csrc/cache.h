@@ -35,6 +35,7 @@ struct PagedRoute {
     int step_shift;                           // log2 of the keys of a step
     int workgroups;
     int least;                                // steps that a workgroup takes at least
+    int setup;                                // what a unit takes beside its steps, in steps
 };
 PagedRoute paged_route(const CacheShape& sh);
 size_t paged_workspace(const CacheShape& sh);

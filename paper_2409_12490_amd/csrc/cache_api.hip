@@ -44,7 +44,7 @@ int make_cache_shape(const critiprefill_cache_params* p, int uses, cp::CacheShap
         if (keys >= (1ll << 30)) return CP_ERR_UNSUPPORTED;
         // key steps are counted in 32 bits
         const cp::PagedRoute r = cp::paged_route(*sh);
-        const double tiles = (double)(sh->tokens >> r.tile_shift) + sh->n_seqs, steps = (double)(keys >> r.step_shift) + 2;
+        const double tiles = (double)(sh->tokens >> r.tile_shift) + sh->n_seqs, steps = (double)(keys >> r.step_shift) + 2 + r.setup;
         if (tiles * steps * sh->hkv >= 2147483648.0) return CP_ERR_UNSUPPORTED;
     }
     for (int i = 0; i < 2; ++i) {

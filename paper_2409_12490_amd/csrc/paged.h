@@ -1,10 +1,11 @@
 // What the two kernels of attention over pages share: how the work is cut, and what is left for the join.
 //
 // A unit is (sequence, KV head, tile of the sequence's new tokens); its rows are the tile's tokens times the KV head's query heads.  A unit takes as many
-// steps over its keys as its last token sees.  All steps of all units laid end to end, units in order of sequence, KV head, tile, are dealt to the
+// steps over its keys as its last token sees, and `setup` more for what a workgroup does around them (with none, workgroups whose run held twenty units of two steps each
+// took four times as long as the others).  All steps of all units laid end to end, units in order of sequence, KV head, tile, are dealt to the
 // workgroups in equal runs: no workgroup has more than its share, whatever the lengths, and the device alone reads the lengths.  A workgroup
 // finishes units that lie in its run; of one that began before it or goes on behind it, it leaves (sum, maximum, weighted V) in the workspace, and
-// join_kernel adds these up in order.
+// a second kernel adds these up in order.
 #pragma once
 #include "cache.h"
 
@@ -19,7 +20,7 @@ struct PagedArgs {
     int32_t* record;                          // [0]: workgroups with work; [4 + 4 w ..]: what the last unit of workgroup w needs, see Record
     int tokens, n_seqs, max_pages, n_pages, hq, hkv, group;
     int page_shift, tile_shift, step_shift;
-    unsigned workgroups, least;
+    unsigned workgroups, least, setup;
     FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
@@ -35,44 +36,50 @@ __device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readf
 
 struct Sequence {                             // one sequence, checked: whatever the arrays hold, rows and pages stay inside the tensors
     int start, tokens, keys, tiles, ahead;    // ahead: steps of the keys that all its tokens see, rounded up
-    unsigned steps;                           // of one KV head
+    unsigned length;                          // of one KV head: the steps of its units, setup included
 
-    __device__ __forceinline__ unsigned before(int j, int tile_shift, int step_shift) const {   // steps of tiles 0 .. j-1, j < tiles
-        // tile i: ahead + ceil((i + 1) tile / step)
-        if (tile_shift >= step_shift) return (unsigned)j * ahead + (((unsigned)j * (j + 1) / 2) << (tile_shift - step_shift));
-        const int m = step_shift - tile_shift;
-        const unsigned a = (unsigned)j >> m, b = (unsigned)j & ((1u << m) - 1);
-        return (unsigned)j * ahead + ((a * (a + 1) / 2) << m) + b * (a + 1);
+    // the same of tiles 0 .. j - 1, j < tiles
+    __device__ __forceinline__ unsigned before(const PagedArgs& a, int j) const {
+        // tile i: setup + ahead + ceil((i + 1) tile / step)
+        unsigned n = (unsigned)j * (ahead + a.setup);
+        if (a.tile_shift >= a.step_shift) return n + (((unsigned)j * (j + 1) / 2) << (a.tile_shift - a.step_shift));
+        const int m = a.step_shift - a.tile_shift;
+        const unsigned whole = (unsigned)j >> m, rest = (unsigned)j & ((1u << m) - 1);
+        return n + ((whole * (whole + 1) / 2) << m) + rest * (whole + 1);
     }
-    __device__ __forceinline__ unsigned steps_of(int j, int tile_shift, int step_shift) const {
-        if (j == tiles - 1) return max(1u, (unsigned)(keys + (1 << step_shift) - 1) >> step_shift);   // its last token sees all keys
-        return ahead + ((unsigned)(((j + 1) << tile_shift) + (1 << step_shift) - 1) >> step_shift);
+    __device__ __forceinline__ unsigned steps_of(const PagedArgs& a, int j) const {    // without setup
+        if (j == tiles - 1) return max(1u, (unsigned)(keys + (1 << a.step_shift) - 1) >> a.step_shift);   // its last token sees all keys
+        return ahead + ((unsigned)(((j + 1) << a.tile_shift) + (1 << a.step_shift) - 1) >> a.step_shift);
     }
-    // uniform: s is the same in all lanes, and so is what follows
-    __device__ __forceinline__ void load(const PagedArgs& a, int s, bool uniform) {
-        int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
-        if (uniform) { from = first_lane(from); to = first_lane(to); held = first_lane(held); }
+    __device__ __forceinline__ void load(const PagedArgs& a, int s) {
+        const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
         tiles = (tokens + (1 << a.tile_shift) - 1) >> a.tile_shift;
         ahead = (max(keys - tokens, 0) + (1 << a.step_shift) - 1) >> a.step_shift;
-        steps = tiles ? before(tiles - 1, a.tile_shift, a.step_shift) + steps_of(tiles - 1, a.tile_shift, a.step_shift) : 0u;
+        length = tiles ? before(a, tiles - 1) + a.setup + steps_of(a, tiles - 1) : 0u;
+    }
+    __device__ __forceinline__ Sequence of_lane(int l) const {
+        Sequence s;
+        s.start = __builtin_amdgcn_readlane(start, l); s.tokens = __builtin_amdgcn_readlane(tokens, l); s.keys = __builtin_amdgcn_readlane(keys, l);
+        s.tiles = __builtin_amdgcn_readlane(tiles, l); s.ahead = __builtin_amdgcn_readlane(ahead, l); s.length = (unsigned)__builtin_amdgcn_readlane((int)length, l);
+        return s;
     }
 };
 
 // A workgroup's run: where it begins and how long it is.  Every wave works it out by itself.
 struct Run {
     unsigned logical, used, share, left;      // its number among those with work, these, steps of each, steps of this one
-    int seq, head, tile; unsigned step;
+    int seq, head, tile; unsigned at;         // at: inside the unit, setup first
     Sequence now;
 
     __device__ __forceinline__ bool find(const PagedArgs& a, unsigned workgroup, int lane) {
         unsigned total = 0, mine = 0, upto = 0;
         Sequence s;
         for (int base = 0; base < a.n_seqs; base += 64) {
-            mine = 0;
-            if (base + lane < a.n_seqs) { s.load(a, base + lane, false); mine = s.steps * (unsigned)a.hkv; }
+            s.load(a, min(base + lane, a.n_seqs - 1));
+            mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
             upto = mine;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(upto, d); if (lane >= d) upto += o; }
@@ -89,47 +96,149 @@ struct Run {
         unsigned past = 0;
         for (int base = 0; base < a.n_seqs; base += 64) {
             if (a.n_seqs > 64) {
-                mine = 0;
-                if (base + lane < a.n_seqs) { s.load(a, base + lane, false); mine = s.steps * (unsigned)a.hkv; }
+                s.load(a, min(base + lane, a.n_seqs - 1));
+                mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
                 upto = mine;
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(upto, d); if (lane >= d) upto += o; }
             }
             const unsigned long long behind = __builtin_amdgcn_ballot_w64(past + upto > begin);
             if (behind) {
-                const int at = __builtin_ctzll(behind);
-                unsigned rest = begin - past - (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), at);
-                seq = base + at;
-                now.load(a, seq, true);
-                head = first_lane((int)(rest / now.steps));
-                rest -= (unsigned)head * now.steps;
+                const int l = __builtin_ctzll(behind);
+                unsigned rest = begin - past - (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), l);
+                seq = base + l;
+                now = s.of_lane(l);
+                head = first_lane((int)(rest / now.length));
+                rest -= (unsigned)head * now.length;
                 int lo = 0, hi = now.tiles - 1;                    // the last tile that begins at or before it
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
-                    if (now.before(mid, a.tile_shift, a.step_shift) <= rest) lo = mid; else hi = mid - 1;
+                    if (now.before(a, mid) <= rest) lo = mid; else hi = mid - 1;
                 }
                 tile = lo;
-                step = rest - now.before(lo, a.tile_shift, a.step_shift);
+                at = rest - now.before(a, lo);
                 return true;
             }
             past += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
         }
         return false;
     }
-    // the unit behind this one; false past the last
+    // What the run has of its present unit: steps first .. first + count - 1 of `unit`.
+    __device__ __forceinline__ void piece(const PagedArgs& a, unsigned& first, unsigned& count, unsigned& unit) const {
+        unit = now.steps_of(a, tile);
+        first = at > a.setup ? at - a.setup : 0u;
+        count = min(at + left - a.setup, unit) - first;
+    }
+    // Where the run has nothing but setup of its present unit, this is its last, and its steps are the next workgroup's.
+    __device__ __forceinline__ bool has_steps(const PagedArgs& a) const { return at + left > a.setup; }
+    // on to the unit behind this one; false where the run or the work ends
     __device__ __forceinline__ bool next(const PagedArgs& a) {
-        step = 0;
+        const unsigned rest = a.setup + now.steps_of(a, tile) - at;
+        if (left <= rest) return false;
+        left -= rest;
+        at = 0;
         if (++tile < now.tiles) return true;
         tile = 0;
         if (++head < a.hkv) return true;
         head = 0;
         do {
             if (++seq >= a.n_seqs) return false;
-            now.load(a, seq, true);
+            now.load(a, seq);
+            now = now.of_lane(0);
         } while (now.tiles == 0);
         return true;
     }
+    __device__ __forceinline__ bool next_steps(const PagedArgs& a) { return next(a) && has_steps(a); }
 };
+
+// Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x, in order of x.  A row is 32 threads of 4
+// channels; PG groups of them take every PG-th part, so that many parts of few rows are not read one after another (8 units of 64 parts in groups of
+// 16 threads a row, four parts at a time: 31 us).  WIDE: the layout of the kernel of 256-row tiles, where neighbouring threads take neighbouring rows.
+template <typename T, int PG, bool WIDE>
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
+    constexpr int kPer = 8 / PG;                                   // rows of a workgroup at a time
+    __shared__ __attribute__((aligned(16))) float rest[PG > 1 ? 8 * 128 : 4];
+    __shared__ float rest_l[8];
+    const unsigned w = blockIdx.x;
+    if (w >= (unsigned)a.record[0]) return;
+    const int4 rec = *(const int4*)(a.record + 4 + 4 * w);
+    const int parts = rec.w, live = rec.y * a.group;
+    if (parts < 2) return;
+    const int tid = threadIdx.x;
+    const int cg = WIDE ? 8 * (blockIdx.y & 3) + (tid >> 5) : tid & 31, pg = WIDE ? 0 : (tid >> 5) / kPer, local = WIDE ? tid & 31 : (tid >> 5) % kPer;
+    const int first = WIDE ? 32 * (blockIdx.y >> 2) : blockIdx.y * kPer, stride = WIDE ? 32 * (gridDim.y >> 2) : gridDim.y * kPer;
+    const float c = a.scale_log2e;
+    auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
+    for (int r0 = first; r0 < live; r0 += stride) {                // uniform
+        const int r = r0 + local;
+        const bool mine = r < live;
+        const int rr = mine ? r : live - 1;
+        // parts are read ahead of the maximum: each is scaled to the largest of those before it
+        float M = -INFINITY, L = 0.f;
+        float4 sum = {0.f, 0.f, 0.f, 0.f};
+        const int64_t in_row = WIDE ? (rr >> 5) * 4096 + (cg >> 1) * 256 + ((cg & 1) * 32 + (rr & 31)) * 4 : rr * kHeadDim + 4 * cg;
+        constexpr int kAhead = 8;
+        for (int x0 = pg; x0 < parts; x0 += PG * kAhead) {
+            float2 ml[kAhead]; float4 v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int x = min(x0 + i * PG, parts - 1);
+                ml[i] = *(const float2*)(a.stats + 2 * (slot(x) * rows + rr));
+                v[i] = *(const float4*)(a.parts + slot(x) * rows * kHeadDim + in_row);
+            }
+            float top = M;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) top = x0 + i * PG < parts ? fmaxf(top, ml[i].x) : top;
+            const float safe = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f((M - safe) * c);
+            L *= old; sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+            M = top;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const float f = x0 + i * PG < parts ? __builtin_amdgcn_exp2f((ml[i].x - safe) * c) : 0.f;
+                if (x0 + i * PG < parts) {
+                    L = fmaf(f, ml[i].y, L);
+                    sum.x = fmaf(f, v[i].x, sum.x); sum.y = fmaf(f, v[i].y, sum.y); sum.z = fmaf(f, v[i].z, sum.z); sum.w = fmaf(f, v[i].w, sum.w);
+                }
+            }
+        }
+        if (PG > 1) {
+            if (r0 != first) __syncthreads();                      // the row before has been read
+            float* at = rest + (tid >> 5) * 128 + 4 * cg;
+            *(float4*)at = sum;
+            if (cg == 0) { rest_l[tid >> 5] = L; }
+            __shared__ float rest_m[8];
+            if (cg == 0) rest_m[tid >> 5] = M;
+            __syncthreads();
+            if (pg != 0) continue;
+            float top = M;
+#pragma unroll
+            for (int x = 1; x < PG; ++x) top = fmaxf(top, rest_m[local + x * kPer]);
+            const float safe = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f((M - safe) * c);
+            L *= old; sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+#pragma unroll
+            for (int x = 1; x < PG; ++x) {
+                const float f = __builtin_amdgcn_exp2f((rest_m[local + x * kPer] - safe) * c);
+                const float4 v = *(const float4*)(at + x * kPer * 128);
+                L = fmaf(f, rest_l[local + x * kPer], L);
+                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+            }
+            M = top;
+        }
+        if (!mine) continue;
+        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        const int t = (int)a.by_group.div((unsigned)r), h = rec.z * a.group + r - t * a.group;
+        const int64_t row = rec.x + t, to = row * a.os0 + h * a.os1 + 4 * cg;
+        if constexpr (sizeof(T) == 4) {
+            *(float4*)((float*)a.out + to) = float4{sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv};
+        } else {
+            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;
+            bf16x4_t v;
+            v[0] = (__bf16)(sum.x * inv); v[1] = (__bf16)(sum.y * inv); v[2] = (__bf16)(sum.z * inv); v[3] = (__bf16)(sum.w * inv);
+            *(bf16x4_t*)((__bf16*)a.out + to) = v;
+        }
+        if (a.lse && cg == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + __logf(L);
+    }
+}
 
 }  // namespace
 
