@@ -68,7 +68,7 @@ template <> struct Raw<true, false> { f32x4 k[8]; f32x4 v[4][2]; };
 template <> struct Raw<true, true> { u32x4 k[2]; unsigned v[4][2]; unsigned ks; u32x4 vs; };
 
 template <bool F32, bool MX, int NQ>
-__global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
+__global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
     constexpr int kRows = 16 * NQ, kWaveKeys = F32 ? 16 : 32, kGroups = kWaveKeys / 16;
     constexpr int kRowBytes = MX ? kHeadDim : (F32 ? 512 : 256);
     extern __shared__ __attribute__((aligned(16))) float merge[];              // [wave][row][128], then (max, sum) [wave][row]
@@ -134,40 +134,50 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
                 entry[g] = table[max(min(u, high), 0) >> a.page_shift];        // no branch; whether the keys are there is asked in load
             }
         };
-        auto load = [&](Raw<F32, MX>& raw, int (&seen)[kGroups], unsigned step) __attribute__((always_inline)) {
+        Raw<F32, MX> raw;
+        int seen[kGroups], seen_next[kGroups];                                 // keys of a group that exist, of this step and the next
+        int64_t at[kGroups];                                                   // first row of the groups asked for last
+        auto load_k = [&](unsigned step) __attribute__((always_inline)) {
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int u = key_of(step) + 16 * g;
                 const bool there = (unsigned)entry[g] < (unsigned)a.n_pages && u <= high;
-                seen[g] = there ? seq.keys - u : 0;                            // keys of the group that exist
-                const int64_t row = (((int64_t)(there ? entry[g] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
-                const char* kp = (const char*)a.cache.k + row * kRowBytes;
-                const char* vp = (const char*)a.cache.v + row * kRowBytes;
+                seen_next[g] = there ? seq.keys - u : 0;
+                at[g] = (((int64_t)(there ? entry[g] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
+                const char* kp = (const char*)a.cache.k + at[g] * kRowBytes;
                 if constexpr (!F32) {
                     const int per = MX ? 32 : 64;
 #pragma unroll
                     for (int x = 0; x < (MX ? 2 : 4); ++x) raw.k[g][x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * per + 16 * x);
+                    if constexpr (MX) raw.ks[g] = (a.cache.ks + at[g] * 4)[c16 * 4 + kg];
+                } else if constexpr (MX) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) raw.k[x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * 32 + 16 * x);
+                    raw.ks = (a.cache.ks + at[g] * 4)[c16 * 4 + kg];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) raw.k[x] = *(const f32x4*)(kp + c16 * kRowBytes + kg * 128 + 16 * x);
+                }
+            }
+        };
+        auto load_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const char* vp = (const char*)a.cache.v + at[g] * kRowBytes;
+                if constexpr (!F32) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (MX) raw.v[4 * g + i] = *(const u32x2*)(vp + (4 * kg + i) * kRowBytes + 8 * c16);
                         else raw.v[4 * g + i] = *(const u32x4*)(vp + (4 * kg + i) * kRowBytes + 16 * c16);
                     }
-                    if constexpr (MX) {
-                        raw.ks[g] = (a.cache.ks + row * 4)[c16 * 4 + kg];
-                        raw.vs[g] = *(const u32x4*)(a.cache.vs + row * 4 + 16 * kg);   // of four tokens
-                    }
+                    if constexpr (MX) raw.vs[g] = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);   // of four tokens
                 } else if constexpr (MX) {
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) raw.k[x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * 32 + 16 * x);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int x = 0; x < 2; ++x) raw.v[i][x] = *(const unsigned*)(vp + (4 * kg + i) * kRowBytes + 4 * c16 + 64 * x);
-                    raw.ks = (a.cache.ks + row * 4)[c16 * 4 + kg];
-                    raw.vs = *(const u32x4*)(a.cache.vs + row * 4 + 16 * kg);
+                    raw.vs = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);
                 } else {
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) raw.k[x] = *(const f32x4*)(kp + c16 * kRowBytes + kg * 128 + 16 * x);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -175,10 +185,14 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
                 }
             }
         };
-        // ---- one step: the wave's keys u0 .. u0 + kWaveKeys - 1
-        auto multiply = [&](Raw<F32, MX>& raw, const int (&seen)[kGroups], unsigned step) __attribute__((always_inline)) {
-            const int u0 = key_of(step);
-            if (u0 > high) return;                                             // uniform: no row sees any of them
+        // ---- the loop.  K of the next step is asked for when QK has read this one's, V when PV has: each has half a step and the other wave of the SIMD to land in
+        look_up(first); load_k(first); load_v();
+        look_up(first + 1);
+        for (unsigned x = 0; x < count; ++x) {
+            const int u0 = key_of(first + x);
+            const bool more = x + 1 < count;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) seen[g] = seen_next[g];
             f32x4 s[NQ][kGroups];
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq)
@@ -210,6 +224,9 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
                         for (int nq = 0; nq < NQ; ++nq) s[nq][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kw[e], qw[nq][x][e], s[nq][0], 0, 0, 0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) load_k(first + x + 1);
+            __builtin_amdgcn_sched_barrier(0);
             // hidden keys: behind the row's own, or without a page.  Their values may hold anything, NaN included, and a weight of 0 does not stop that:
             // rows of V that no row of the tile sees become 0
             bool whole = u0 + kWaveKeys - 1 <= low;
@@ -295,19 +312,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 ? 2 : 1) void paged_rows_kernel(P
                         for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[n >> 2][n & 3], s[nq][0][i], o[nq][n], 0, 0, 0);
                 }
             }
-        };
-
-        Raw<F32, MX> one, two;
-        int seen_one[kGroups], seen_two[kGroups];
-        look_up(first); load(one, seen_one, first);
-        look_up(first + 1);
-        for (unsigned x = 0; x < count; x += 2) {
-            if (x + 1 < count) { load(two, seen_two, first + x + 1); look_up(first + x + 2); }
-            multiply(one, seen_one, first + x);
-            if (x + 1 < count) {
-                if (x + 2 < count) { load(one, seen_one, first + x + 2); look_up(first + x + 3); }
-                multiply(two, seen_two, first + x + 1);
-            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) { load_v(); look_up(first + x + 2); }
         }
 
         // ---- merge the four waves: sum_w 2^(c (m_w - M)) O_w; 16-byte pieces of a row swizzled by the row
@@ -402,19 +408,24 @@ int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        //
 PagedRoute paged_route(const CacheShape& sh) {
     PagedRoute r;
     const bool f32 = sh.dtype == 0;
-    // More rows a KV head than the smaller tiles hold: tiles of 256 rows, whose keys are read once for all of them
-    r.chunk = !f32 && (long long)sh.max_q * sh.group > 64;
+    // Tiles of 256 rows pay from more than 16 rows on, 8-bit pages from 32.  us, 32/8 heads, waves that split the keys / tiles of 256 rows: 8 x 4 tokens after 1000 17.1 / 19.1,
+    // 1 x 4 after 30000 28.8 / 38.7, 8 x 4 after 16000 103 / 95 (both near the memory's rate), 8 x 8 112 / 95, 1 x 8 after 1000 16.8 / 15.1, 8 x 16 after 2000 66 / 29; 8 bits:
+    // 8 x 4 after 16000 61 / 107, 8 x 8 70 / 107, 8 x 16 114 / 112.
+    const long long want = (long long)sh.max_q * sh.group;
+    r.chunk = !f32 && want > (sh.mxfp8 ? 32 : 16);
     if (r.chunk) {
         r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
         return r;
     }
+    // the smallest tile that holds a sequence's new tokens, the largest there is for longer chunks
+    const int most = f32 ? 2 : sh.mxfp8 ? 2 : 1;
     int nq = 1;
-    while (nq < (f32 ? 2 : 4) && (16 * nq / sh.group < 1 || (1 << log2_of(16 * nq / sh.group)) < sh.max_q)) nq *= 2;
-    while (16 * nq < sh.group) nq *= 2;
+    while (nq < most && (16 * nq < sh.group || (1 << log2_of(16 * nq / sh.group)) < sh.max_q)) nq *= 2;
+    while (16 * nq < sh.group) nq *= 2;                             // fp32: 33 to 64 query heads a KV head
     r.rows = 16 * nq;
     r.tile_shift = log2_of(r.rows / sh.group);
     r.step_shift = f32 ? 6 : 7;
-    r.workgroups = nq == 1 ? 512 : 256;
+    r.workgroups = nq == 1 || !f32 ? 512 : 256;                     // two to a compute unit, where their registers allow it
     r.least = 1;
     r.setup = 1;
     return r;
@@ -431,8 +442,8 @@ hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, cons
         if (sh.mxfp8) return nq == 1 ? launch<true, true, 1>(a, st) : nq == 2 ? launch<true, true, 2>(a, st) : launch<true, true, 4>(a, st);
         return nq == 1 ? launch<true, false, 1>(a, st) : nq == 2 ? launch<true, false, 2>(a, st) : launch<true, false, 4>(a, st);
     }
-    if (sh.mxfp8) return nq == 1 ? launch<false, true, 1>(a, st) : nq == 2 ? launch<false, true, 2>(a, st) : launch<false, true, 4>(a, st);
-    return nq == 1 ? launch<false, false, 1>(a, st) : nq == 2 ? launch<false, false, 2>(a, st) : launch<false, false, 4>(a, st);
+    if (sh.mxfp8) return nq == 1 ? launch<false, true, 1>(a, st) : launch<false, true, 2>(a, st);
+    return launch<false, false, 1>(a, st);
 }
 
 hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
@@ -454,8 +465,8 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     if (e != hipSuccess) return e;
     // a workgroup of the join takes a row at a time; more rows than the grid has, where a chunk is longer than was said, come in turn
     const dim3 grid((unsigned)route.workgroups, (unsigned)std::min<long long>(16, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group));
-    if (sh.dtype == 0) hipLaunchKernelGGL((join_kernel<float, 8, false>), grid, dim3(256), 0, st, a, route.rows);
-    else hipLaunchKernelGGL((join_kernel<__bf16, 8, false>), grid, dim3(256), 0, st, a, route.rows);
+    if (sh.dtype == 0) hipLaunchKernelGGL((join_kernel<float, false>), grid, dim3(256), 0, st, a, route.rows);
+    else hipLaunchKernelGGL((join_kernel<__bf16, false>), grid, dim3(256), 0, st, a, route.rows);
     return hipGetLastError();
 }
 

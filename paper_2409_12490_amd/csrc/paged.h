@@ -151,92 +151,100 @@ struct Run {
     __device__ __forceinline__ bool next_steps(const PagedArgs& a) { return next(a) && has_steps(a); }
 };
 
-// Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x, in order of x.  A row is 32 threads of 4
-// channels; PG groups of them take every PG-th part, so that many parts of few rows are not read one after another (8 units of 64 parts in groups of
-// 16 threads a row, four parts at a time: 31 us).  WIDE: the layout of the kernel of 256-row tiles, where neighbouring threads take neighbouring rows.
-template <typename T, int PG, bool WIDE>
+// Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x.  All that a thread reads of
+// several parts is asked for at once: a part's latency, not its bytes, is what the kernel takes.
+// Few rows: 32 threads of 4 channels take a row, eight groups of them every eighth part, whose sums meet in LDS (8 units of 64 parts by four groups of 16
+// threads: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 16 channels of a row, neighbouring threads neighbouring rows.
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    constexpr int kPer = 8 / PG;                                   // rows of a workgroup at a time
-    __shared__ __attribute__((aligned(16))) float rest[PG > 1 ? 8 * 128 : 4];
-    __shared__ float rest_l[8];
+    constexpr int kGroups = WIDE ? 1 : 8, kPieces = WIDE ? 4 : 1, kAhead = WIDE ? 4 : 8, kRowsAtOnce = WIDE ? 32 : 1;
+    __shared__ __attribute__((aligned(16))) float rest[WIDE ? 4 : 8 * 128];
+    __shared__ float rest_m[8], rest_l[8];
     const unsigned w = blockIdx.x;
     if (w >= (unsigned)a.record[0]) return;
     const int4 rec = *(const int4*)(a.record + 4 + 4 * w);
     const int parts = rec.w, live = rec.y * a.group;
     if (parts < 2) return;
-    const int tid = threadIdx.x;
-    const int cg = WIDE ? 8 * (blockIdx.y & 3) + (tid >> 5) : tid & 31, pg = WIDE ? 0 : (tid >> 5) / kPer, local = WIDE ? tid & 31 : (tid >> 5) % kPer;
-    const int first = WIDE ? 32 * (blockIdx.y >> 2) : blockIdx.y * kPer, stride = WIDE ? 32 * (gridDim.y >> 2) : gridDim.y * kPer;
+    const int tid = threadIdx.x, group = WIDE ? 0 : tid >> 5;
     const float c = a.scale_log2e;
     auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-    for (int r0 = first; r0 < live; r0 += stride) {                // uniform
-        const int r = r0 + local;
-        const bool mine = r < live;
-        const int rr = mine ? r : live - 1;
-        // parts are read ahead of the maximum: each is scaled to the largest of those before it
+    for (int first = blockIdx.y * kRowsAtOnce; first < live; first += gridDim.y * kRowsAtOnce) {     // uniform
+        const int r = min(first + (WIDE ? tid & 31 : 0), live - 1);
+        auto channel = [&](int j) { return 4 * (WIDE ? 8 * j + (tid >> 5) : tid & 31); };
+        auto place = [&](int j) {
+            const int cg = channel(j) >> 2;
+            return WIDE ? (r >> 5) * 4096 + (cg >> 1) * 256 + ((cg & 1) * 32 + (r & 31)) * 4 : r * kHeadDim + 4 * cg;
+        };
         float M = -INFINITY, L = 0.f;
-        float4 sum = {0.f, 0.f, 0.f, 0.f};
-        const int64_t in_row = WIDE ? (rr >> 5) * 4096 + (cg >> 1) * 256 + ((cg & 1) * 32 + (rr & 31)) * 4 : rr * kHeadDim + 4 * cg;
-        constexpr int kAhead = 8;
-        for (int x0 = pg; x0 < parts; x0 += PG * kAhead) {
-            float2 ml[kAhead]; float4 v[kAhead];
+        float4 sum[kPieces];
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) sum[j] = float4{0.f, 0.f, 0.f, 0.f};
+        auto add = [&](float m, float l, const float4 (&v)[kPieces], float safe) {
+            const float f = __builtin_amdgcn_exp2f((m - safe) * c);
+            L = fmaf(f, l, L);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                sum[j].x = fmaf(f, v[j].x, sum[j].x); sum[j].y = fmaf(f, v[j].y, sum[j].y);
+                sum[j].z = fmaf(f, v[j].z, sum[j].z); sum[j].w = fmaf(f, v[j].w, sum[j].w);
+            }
+        };
+        auto move_to = [&](float top) -> float {                   // the reference point; returns what exponents are taken from
+            const float safe = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f((M - safe) * c);
+            L *= f;
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) { sum[j].x *= f; sum[j].y *= f; sum[j].z *= f; sum[j].w *= f; }
+            M = top;
+            return safe;
+        };
+        for (int x0 = group; x0 < parts; x0 += kGroups * kAhead) {
+            float2 ml[kAhead]; float4 v[kAhead][kPieces];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int x = min(x0 + i * PG, parts - 1);
-                ml[i] = *(const float2*)(a.stats + 2 * (slot(x) * rows + rr));
-                v[i] = *(const float4*)(a.parts + slot(x) * rows * kHeadDim + in_row);
+                const int64_t from = slot(min(x0 + i * kGroups, parts - 1)) * rows;
+                ml[i] = *(const float2*)(a.stats + 2 * (from + r));
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) v[i][j] = *(const float4*)(a.parts + from * kHeadDim + place(j));
             }
             float top = M;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) top = x0 + i * PG < parts ? fmaxf(top, ml[i].x) : top;
-            const float safe = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f((M - safe) * c);
-            L *= old; sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
-            M = top;
+            for (int i = 0; i < kAhead; ++i) top = x0 + i * kGroups < parts ? fmaxf(top, ml[i].x) : top;
+            const float safe = move_to(top);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const float f = x0 + i * PG < parts ? __builtin_amdgcn_exp2f((ml[i].x - safe) * c) : 0.f;
-                if (x0 + i * PG < parts) {
-                    L = fmaf(f, ml[i].y, L);
-                    sum.x = fmaf(f, v[i].x, sum.x); sum.y = fmaf(f, v[i].y, sum.y); sum.z = fmaf(f, v[i].z, sum.z); sum.w = fmaf(f, v[i].w, sum.w);
-                }
-            }
+            for (int i = 0; i < kAhead; ++i)
+                if (x0 + i * kGroups < parts) add(ml[i].x, ml[i].y, v[i], safe);
         }
-        if (PG > 1) {
-            if (r0 != first) __syncthreads();                      // the row before has been read
-            float* at = rest + (tid >> 5) * 128 + 4 * cg;
-            *(float4*)at = sum;
-            if (cg == 0) { rest_l[tid >> 5] = L; }
-            __shared__ float rest_m[8];
-            if (cg == 0) rest_m[tid >> 5] = M;
+        if constexpr (!WIDE) {
+            __syncthreads();                                       // the row before has been read
+            *(float4*)(rest + 4 * tid) = sum[0];
+            if ((tid & 31) == 0) { rest_m[group] = M; rest_l[group] = L; }
             __syncthreads();
-            if (pg != 0) continue;
+            if (group != 0) continue;
             float top = M;
 #pragma unroll
-            for (int x = 1; x < PG; ++x) top = fmaxf(top, rest_m[local + x * kPer]);
-            const float safe = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f((M - safe) * c);
-            L *= old; sum.x *= old; sum.y *= old; sum.z *= old; sum.w *= old;
+            for (int x = 1; x < kGroups; ++x) top = fmaxf(top, rest_m[x]);
+            const float safe = move_to(top);
 #pragma unroll
-            for (int x = 1; x < PG; ++x) {
-                const float f = __builtin_amdgcn_exp2f((rest_m[local + x * kPer] - safe) * c);
-                const float4 v = *(const float4*)(at + x * kPer * 128);
-                L = fmaf(f, rest_l[local + x * kPer], L);
-                sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+            for (int x = 1; x < kGroups; ++x) {
+                const float4 v[1] = {*(const float4*)(rest + 4 * (tid + 32 * x))};
+                add(rest_m[x], rest_l[x], v, safe);
             }
-            M = top;
         }
-        if (!mine) continue;
+        if (WIDE && first + (tid & 31) >= live) continue;
         const float inv = L == 0.f ? 0.f : 1.0f / L;
         const int t = (int)a.by_group.div((unsigned)r), h = rec.z * a.group + r - t * a.group;
-        const int64_t row = rec.x + t, to = row * a.os0 + h * a.os1 + 4 * cg;
-        if constexpr (sizeof(T) == 4) {
-            *(float4*)((float*)a.out + to) = float4{sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv};
-        } else {
-            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;
-            bf16x4_t v;
-            v[0] = (__bf16)(sum.x * inv); v[1] = (__bf16)(sum.y * inv); v[2] = (__bf16)(sum.z * inv); v[3] = (__bf16)(sum.w * inv);
-            *(bf16x4_t*)((__bf16*)a.out + to) = v;
+        const int64_t row = rec.x + t;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int64_t to = row * a.os0 + h * a.os1 + channel(j);
+            const float4 y = {sum[j].x * inv, sum[j].y * inv, sum[j].z * inv, sum[j].w * inv};
+            if constexpr (sizeof(T) == 4) {
+                *(float4*)((float*)a.out + to) = y;
+            } else {
+                typedef __attribute__((ext_vector_type(4))) __bf16 four;
+                *(four*)((__bf16*)a.out + to) = four{(__bf16)y.x, (__bf16)y.y, (__bf16)y.z, (__bf16)y.w};
+            }
         }
-        if (a.lse && cg == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + __logf(L);
+        if (a.lse && channel(0) == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + __logf(L);
     }
 }
 
