@@ -154,10 +154,10 @@ struct Run {
 // Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x.  All that a thread reads of
 // several parts is asked for at once: a part's latency, not its bytes, is what the kernel takes.
 // Few rows: 32 threads of 4 channels take a row, eight groups of them every eighth part, whose sums meet in LDS (8 units of 64 parts by four groups of 16
-// threads: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 16 channels of a row, neighbouring threads neighbouring rows.
+// threads: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 8 channels of a row, neighbouring threads neighbouring rows.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    constexpr int kGroups = WIDE ? 1 : 8, kPieces = WIDE ? 4 : 1, kAhead = WIDE ? 4 : 8, kRowsAtOnce = WIDE ? 32 : 1;
+    constexpr int kGroups = WIDE ? 1 : 8, kPieces = WIDE ? 2 : 1, kAhead = WIDE ? 6 : 8, kRowsAtOnce = WIDE ? 32 : 1;
     __shared__ __attribute__((aligned(16))) float rest[WIDE ? 4 : 8 * 128];
     __shared__ float rest_m[8], rest_l[8];
     const unsigned w = blockIdx.x;
@@ -168,9 +168,11 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
     const int tid = threadIdx.x, group = WIDE ? 0 : tid >> 5;
     const float c = a.scale_log2e;
     auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-    for (int first = blockIdx.y * kRowsAtOnce; first < live; first += gridDim.y * kRowsAtOnce) {     // uniform
+    constexpr int kParts = WIDE ? 4 / kPieces : 1;                 // of a row's channels, a workgroup each
+    const int half = blockIdx.y % kParts;
+    for (int first = blockIdx.y / kParts * kRowsAtOnce; first < live; first += gridDim.y / kParts * kRowsAtOnce) {     // uniform
         const int r = min(first + (WIDE ? tid & 31 : 0), live - 1);
-        auto channel = [&](int j) { return 4 * (WIDE ? 8 * j + (tid >> 5) : tid & 31); };
+        auto channel = [&](int j) { return 4 * (WIDE ? 8 * (kPieces * half + j) + (tid >> 5) : tid & 31); };
         auto place = [&](int j) {
             const int cg = channel(j) >> 2;
             return WIDE ? (r >> 5) * 4096 + (cg >> 1) * 256 + ((cg & 1) * 32 + (r & 31)) * 4 : r * kHeadDim + 4 * cg;
