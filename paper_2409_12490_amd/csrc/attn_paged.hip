@@ -126,6 +126,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
 
         // ---- loads.  Pages are looked up a step ahead; one that is not in the pool holds nothing: its keys are hidden, and read from page 0
         int entry[kGroups];
+        bool odd = false;                                                      // see the loop
         auto key_of = [&](unsigned step) { return (int)(step << a.step_shift) + wave * kWaveKeys; };
         auto look_up = [&](unsigned step) __attribute__((always_inline)) {
 #pragma unroll
@@ -227,8 +228,9 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
             __builtin_amdgcn_sched_barrier(0);
             if (more) load_k(first + x + 1);
             __builtin_amdgcn_sched_barrier(0);
-            // hidden keys: behind the row's own, or without a page.  Their values may hold anything, NaN included, and a weight of 0 does not stop that:
-            // rows of V that no row of the tile sees become 0
+            // Hidden keys: behind the row's own, or without a page.  Their values may hold anything, and a weight of 0 does not keep an infinity or NaN out of a
+            // sum: rows of V that no row sees become 0, and so does what is not finite in those that some rows do not see (only with more than one token); `odd`
+            // says that there was any, and the unit's end adds it for the rows that see it.
             bool whole = u0 + kWaveKeys - 1 <= low;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) whole = whole && seen[g] > 0;
@@ -241,13 +243,43 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
 #pragma unroll
                         for (int i = 0; i < 4; ++i) s[nq][g][i] = i > lim ? -INFINITY : s[nq][g][i];
                     }
-                    const int lim = seen[g] > 0 ? high - u0 - 16 * g - 4 * kg : -1;
+                    const int lim = seen[g] > 0 ? high - u0 - 16 * g - 4 * kg : -1, sure = low - u0 - 16 * g - 4 * kg;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if constexpr (!F32 && MX) { if (i > lim) { raw.v[4 * g + i] = u32x2{0, 0}; raw.vs[g][i] = 0x7f7f7f7fu; } }
-                        else if constexpr (!F32) { if (i > lim) raw.v[4 * g + i] = u32x4{0, 0, 0, 0}; }
-                        else if constexpr (MX) { if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; raw.vs[i] = 0x7f7f7f7fu; } }
-                        else { if (i > lim) raw.v[i][0] = raw.v[i][1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+                        bool any = false;
+                        auto clean32 = [&](float x) { const bool bad = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; any = any || bad; return bad ? 0.f : x; };
+                        auto clean8 = [&](unsigned x) {                        // e4m3: 0x7f of either sign
+                            unsigned keep = 0;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) keep |= ((x >> (8 * e)) & 0x7f) == 0x7f ? 0u : 0xffu << (8 * e);
+                            any = any || ~keep;
+                            return x & keep;
+                        };
+                        if constexpr (!F32 && MX) {
+                            if (i > lim) { raw.v[4 * g + i] = u32x2{0, 0}; raw.vs[g][i] = 0x7f7f7f7fu; }
+                            else if (i > sure) { raw.v[4 * g + i][0] = clean8(raw.v[4 * g + i][0]); raw.v[4 * g + i][1] = clean8(raw.v[4 * g + i][1]); }
+                        } else if constexpr (!F32) {
+                            if (i > lim) raw.v[4 * g + i] = u32x4{0, 0, 0, 0};
+                            else if (i > sure) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const unsigned x = raw.v[4 * g + i][e];
+                                    const unsigned keep = ((x & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu);
+                                    any = any || ~keep;
+                                    raw.v[4 * g + i][e] = x & keep;
+                                }
+                            }
+                        } else if constexpr (MX) {
+                            if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; raw.vs[i] = 0x7f7f7f7fu; }
+                            else if (i > sure) { raw.v[i][0] = clean8(raw.v[i][0]); raw.v[i][1] = clean8(raw.v[i][1]); }
+                        } else {
+                            if (i > lim) raw.v[i][0] = raw.v[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                            else if (i > sure) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) raw.v[i][e >> 2][e & 3] = clean32(raw.v[i][e >> 2][e & 3]);
+                            }
+                        }
+                        if (any) odd = true;
                     }
                 }
             }
@@ -314,6 +346,33 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
             }
             __builtin_amdgcn_sched_barrier(0);
             if (more) { load_v(); look_up(first + x + 2); }
+        }
+
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+            for (unsigned x = 0; x < count; ++x)
+                for (int i = 0; i < kWaveKeys; ++i) {                          // once in a blue moon: a key after another, from memory
+                    const int u = key_of(first + x) + i;
+                    if (u <= low || u > high) continue;
+                    const int page = table[u >> a.page_shift];
+                    if ((unsigned)page >= (unsigned)a.n_pages) continue;
+                    const int64_t row = (((int64_t)page * a.hkv + head) << a.page_shift) + (u & page_mask);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {                          // o[][n][e] is this channel's
+                            const int ch = F32 ? 64 * (n >> 2) + 4 * (4 * kg + e) + (n & 3) : 8 * (4 * kg + e) + n;
+                            float v;
+                            if constexpr (MX) {
+                                const unsigned b = ((const uint8_t*)a.cache.v)[row * kRowBytes + ch];
+                                v = (b & 0x7f) == 0x7f ? NAN : 0.f;
+                            } else if constexpr (F32) v = ((const float*)((const char*)a.cache.v + row * kRowBytes))[ch];
+                            else v = __uint_as_float((unsigned)((const uint16_t*)((const char*)a.cache.v + row * kRowBytes))[ch] << 16);
+                            const bool bad = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+                            for (int nq = 0; nq < NQ; ++nq)
+                                if (bad && u <= last[nq]) o[nq][n][e] += v;
+                        }
+                }
         }
 
         // ---- merge the four waves: sum_w 2^(c (m_w - M)) O_w; 16-byte pieces of a row swizzled by the row

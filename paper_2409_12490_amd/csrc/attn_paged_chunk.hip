@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kChunkRows = 256, WQ = 32, TK = 64, NBUF = 4;
 constexpr int kTileBytes = TK * 256;
-constexpr int kVOff = 0, kKOff = NBUF * kTileBytes, kSmem = 2 * NBUF * kTileBytes;
+constexpr int kVOff = 0, kKOff = NBUF * kTileBytes, kOddOff = 2 * NBUF * kTileBytes, kSmem = kOddOff + 16;
 constexpr int kOutPitch = 272;                        // epilogue staging: one output row + 16 B, in bytes
 static_assert(8 * WQ * kOutPitch <= kSmem, "epilogue staging reuses the tile rings");
 
@@ -37,6 +37,8 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
 template <bool MX, bool WHOLE, bool ROTATED>
 __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home, unsigned lds0) {
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
+    if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
+    __syncthreads();
     while (true) {
         // What follows from the thread's number is worked out for each unit: kept from one to the next it would be spilled, 60 registers of it.
         int tid = thread_id();
@@ -119,7 +121,22 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
         int high_v = high;
         asm("" : "+v"(high_v));                                      // like wq_lo
         auto in_vector = [](int x) { asm("" : "+v"(x)); return x; };
-        auto bare = [&](int x, int bits) { return base(x) + TK - 1 > high_v || in_vector(bits) != 15; };   // it has rows that no row sees
+        // Tiles with keys that some rows do not see, or none: a weight of 0 does not keep an infinity or NaN of theirs out of a sum.  As V of such a tile comes in, rows that
+        // no row sees become 0, and so does what is not finite in the others; where there was any, `odd` in LDS is set and the unit's end adds it for the rows that see it.
+        int low_v = min(past + t0, seq.keys - 1);                    // the last key that the first row sees
+        asm("" : "+v"(low_v));
+        auto partly = [&](int x, int bits) { return base(x) + TK - 1 > low_v || in_vector(bits) != 15; };
+        auto clean = [&](u32x4 v, bool there) __attribute__((always_inline)) -> u32x4 {
+            unsigned any = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned keep = ((v[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((v[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu);
+                any |= ~keep;
+                v[e] = there ? v[e] & keep : 0u;
+            }
+            if (there && any) *LDS_PTR(unsigned, lds0 + kOddOff) = 1;
+            return v;
+        };
         auto issue_k = [&](int slot) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -130,12 +147,12 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
             for (int i = 0; i < 2; ++i)
                 dma16(uniform_ptr((const char*)a.cache.v + (now ? at[i] : v_at[i]) * 256), lane_v, lds0 + kVOff + slot * kTileBytes + (32 * i + 4 * wave) * 256);
         };
-        auto zero_v = [&](int x, int bits, int slot) {               // the lane's pieces of rows that no row sees
+        auto clean_v = [&](int x, int bits, int slot) {              // the lane's own pieces
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int row = 32 * i + 4 * wave + r4;
-                if (base(x) + row > high_v || !((bits >> (row >> 4)) & 1))
-                    *LDS_PTR(u32x4, lds0 + kVOff + slot * kTileBytes + (32 * i + 4 * wave) * 256 + lane * 16) = u32x4{0, 0, 0, 0};
+                const unsigned at = lds0 + kVOff + slot * kTileBytes + (32 * i + 4 * wave) * 256 + lane * 16;
+                *LDS_PTR(u32x4, at) = clean(*LDS_PTR(const u32x4, at), base(x) + row <= high_v && ((bits >> (row >> 4)) & 1));
             }
         };
         // 8-bit: the tile in flight
@@ -149,16 +166,18 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
         };
         auto store_raw = [&](int x, int bits, int slot) __attribute__((always_inline)) {
             const float sk = __uint_as_float(scale_k << 23), sv = __uint_as_float(scale_v << 23);
-            u32x4 k2[2] = {widen8(raw_k[0], raw_k[1], sk), widen8(raw_k[2], raw_k[3], sk)};
+            const unsigned row = lds0 + slot * kTileBytes + xrow * 256;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *LDS_PTR(u32x4, row + kKOff + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = widen8(raw_k[2 * h], raw_k[2 * h + 1], sk);
+            __builtin_amdgcn_sched_barrier(0);                       // registers of one at a time
             u32x4 v2[2] = {widen8(raw_v[0], raw_v[1], sv), widen8(raw_v[2], raw_v[3], sv)};
-            if (bare(x, bits)) {
-                if (base(x) + xrow > high_v || !((bits >> (xrow >> 4)) & 1)) v2[0] = v2[1] = u32x4{0, 0, 0, 0};
+            if (partly(x, bits)) {
+                const bool there = base(x) + xrow <= high_v && ((bits >> (xrow >> 4)) & 1);
+                v2[0] = clean(v2[0], there); v2[1] = clean(v2[1], there);
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                *LDS_PTR(u32x4, lds0 + kKOff + slot * kTileBytes + xrow * 256 + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = k2[h];
-                *LDS_PTR(u32x4, lds0 + kVOff + slot * kTileBytes + xrow * 256 + (((2 * xpiece + h) ^ (4 * (xrow & 3))) << 4)) = v2[h];
-            }
+            for (int h = 0; h < 2; ++h) *LDS_PTR(u32x4, row + kVOff + (((2 * xpiece + h) ^ (4 * (xrow & 3))) << 4)) = v2[h];
         };
 
         bf16x8 qf[8];
@@ -297,7 +316,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
                 if (issued == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
                 else if (issued == 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                if (t + 1 < ntiles && bare(t + 1, bits)) zero_v(t + 1, bits, (t + 1) & 3);
+                if (t + 1 < ntiles && partly(t + 1, bits)) clean_v(t + 1, bits, (t + 1) & 3);
             }
             __syncthreads();
         };
@@ -349,7 +368,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
             issue_k(1); issue_v(1, true);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (!MX && bare(0, bits0)) zero_v(0, bits0, 0);
+        if (!MX && partly(0, bits0)) clean_v(0, bits0, 0);
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) qf[ks] = as_bf16x8(*LDS_PTR(const u32x4, q_lds + l32 * 256 + (((2 * ks + hh) ^ (l32 & 15)) << 4)));
 #pragma unroll
@@ -418,6 +437,34 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home
         const float l_tot = half_sum(l_run);
         const bool began = first == 0, ended = first + count == unit;
         __syncthreads();                                             // every wave is past its last tile reads
+        if (__builtin_amdgcn_readfirstlane(*LDS_PTR(const int, lds0 + kOddOff))) {
+            const int from = max(base0, __builtin_amdgcn_readfirstlane(low_v) + 1), to = min(high, base0 + ntiles * TK - 1);
+            for (int u = from; u <= to; ++u) {                       // once in a blue moon: a key after another, from memory
+                const int page = table[u >> a.page_shift];
+                if ((unsigned)page >= (unsigned)a.n_pages) continue;
+                const int64_t row = (((int64_t)page * a.hkv + head) << a.page_shift) + (u & mask);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {                       // channels 8 j + 4 hh ..
+                    unsigned w[2];
+                    if (MX) {
+                        const unsigned b = *(const unsigned*)((const char*)a.cache.v + row * 128 + 8 * j + 4 * hh);
+                        const float scale = __uint_as_float((unsigned)a.cache.vs[row * 4 + (j >> 2)] << 23);
+                        w[0] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
+                        w[1] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true));
+                    } else {
+                        const uint2 b = *(const uint2*)((const char*)a.cache.v + row * 256 + 16 * j + 8 * hh);
+                        w[0] = b.x; w[1] = b.y;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned b = e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16;
+                        if (u <= qpos && (b & 0x7f800000u) == 0x7f800000u) o[j >> 2][4 * (j & 3) + e] += __uint_as_float(b);
+                    }
+                }
+            }
+            __syncthreads();                                         // all have seen the flag
+            if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
+        }
         if (began && ended) {                                        // O^T / l through LDS, so that stores are whole rows
             const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
             const unsigned stage = lds0 + wave * (WQ * kOutPitch);

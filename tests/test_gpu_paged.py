@@ -4,8 +4,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import cache_oracle as O
 from paper_2409_12490_amd import binding as B
-from tests.cache_helpers import DEV, DTYPES, Pool, attend, check_attention, randn
+from tests.cache_helpers import DEV, Pool, attend, check_attention, f64, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -163,3 +164,30 @@ def test_the_same_twice_and_beside_other_work(dtype, mxfp8, new):
         again = attend(pool, q, start, total, max_q_len=new)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("dtype,hq,hkv,page,seqs", [("bf16", 4, 1, 16, [(4, 40), (2, 9)]), ("bf16", 8, 2, 64, [(100, 230), (5, 5)]), ("bf16", 8, 2, 16, [(70, 70), (1, 40)]),
+                                                     ("fp32", 4, 2, 16, [(6, 50), (40, 40)]), ("fp32", 1, 1, 64, [(16, 16)]), ("bf16", 4, 1, 64, [(300, 5000)])])
+def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, hq, hkv, page, seqs, mxfp8):
+    """K and V of some new tokens hold infinities and NaN: the rows before them must not notice, those that see them get what the formula gives."""
+    pool, q, start, total = _case(dtype, mxfp8, hq, hkv, page, seqs)
+    for i, (n, t) in enumerate(seqs):
+        if n < 2:
+            continue
+        for u, what, ch in ((t - 1, "k", 3), (t - n // 2, "v", 77), (t - n // 3 - 1, "v", 5), (t - n + 1, "inf", 120)):
+            slot = int(pool.slots[i][u])
+            at = (slot // page, i % hkv, slot % page, ch)
+            value = float("-inf") if what == "inf" and not mxfp8 else float("nan")
+            which = 0 if what == "k" else 1
+            pool.cache[which][at] = 0x7f if mxfp8 else value
+            (pool.held_k, pool.held_v)[which][at] = value
+    hint = max(n for n, _ in seqs)
+    out, lse = attend(pool, q, start, total, max_q_len=hint)
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, _ = O.paged_attention(f64(q), pool.held_k, pool.held_v, page, pool.table.numpy(), start, total, 128 ** -0.5)
+    got, got_lse = f64(out), f64(lse)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want)) and np.array_equal(np.isnan(got_lse), np.isnan(want_lse))
+    fine = np.isfinite(want)
+    assert fine.any() and not fine.all() and (got[np.isinf(want)] < 0).all()
+    assert np.abs(got[fine] - want[fine]).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-5) * np.abs(want[fine]).max()
