@@ -522,10 +522,17 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     if (route.chunk) return launch_paged_chunk(sh, a, st);
     hipError_t e = launch_paged_rows(sh, route, a, st);
     if (e != hipSuccess) return e;
-    // a workgroup of the join takes a row at a time; more rows than the grid has, where a chunk is longer than was said, come in turn
-    const dim3 grid((unsigned)route.workgroups, (unsigned)std::min<long long>(16, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group));
-    if (sh.dtype == 0) hipLaunchKernelGGL((join_kernel<float, false>), grid, dim3(256), 0, st, a, route.rows);
-    else hipLaunchKernelGGL((join_kernel<__bf16, false>), grid, dim3(256), 0, st, a, route.rows);
+    // A workgroup of the join takes a row with eight groups of threads, or two with four; more rows than its grid has, where a chunk is longer than was said, come in
+    // turn.  Eight and four: 1 x 4 tokens after 5000 (16 rows, 64 parts) 16.1 and 17.2 us; 8 x 8 after 16000 over 8-bit pages (32 rows) 70 and 67, fp32 4/2 heads 3 x 200 40.6 and 38.7.
+    const int rows = (int)std::min<long long>(route.rows, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group);
+    const dim3 grid((unsigned)route.workgroups, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
+    if (sh.dtype == 0) {
+        if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows);
+        else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows);
+    } else {
+        if (rows <= 16) hipLaunchKernelGGL((join_kernel<__bf16, false, 8>), grid, dim3(256), 0, st, a, route.rows);
+        else hipLaunchKernelGGL((join_kernel<__bf16, false, 4>), grid, dim3(256), 0, st, a, route.rows);
+    }
     return hipGetLastError();
 }
 

@@ -153,25 +153,25 @@ struct Run {
 
 // Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x.  All that a thread reads of
 // several parts is asked for at once: a part's latency, not its bytes, is what the kernel takes.
-// Few rows: 32 threads of 4 channels take a row, eight groups of them every eighth part, whose sums meet in LDS (8 units of 64 parts by four groups of 16
-// threads: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 8 channels of a row, neighbouring threads neighbouring rows.
-template <typename T, bool WIDE>
+// Few rows: 32 threads of 4 channels take a row, and GROUPS of them every GROUPS-th part, whose sums meet in LDS (8 units of 64 parts by four groups of 16
+// threads, four parts at a time: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 8 channels of a row, neighbouring threads neighbouring rows.
+template <typename T, bool WIDE, int GROUPS>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    constexpr int kGroups = WIDE ? 1 : 8, kPieces = WIDE ? 2 : 1, kAhead = WIDE ? 6 : 8, kRowsAtOnce = WIDE ? 32 : 1;
-    __shared__ __attribute__((aligned(16))) float rest[WIDE ? 4 : 8 * 128];
+    constexpr int kGroups = WIDE ? 1 : GROUPS, kPieces = WIDE ? 2 : 1, kAhead = WIDE ? 6 : 8, kRowsAtOnce = WIDE ? 32 : 8 / GROUPS;
+    __shared__ __attribute__((aligned(16))) float rest[kGroups > 1 ? 8 * 128 : 4];
     __shared__ float rest_m[8], rest_l[8];
     const unsigned w = blockIdx.x;
     if (w >= (unsigned)a.record[0]) return;
     const int4 rec = *(const int4*)(a.record + 4 + 4 * w);
     const int parts = rec.w, live = rec.y * a.group;
     if (parts < 2) return;
-    const int tid = threadIdx.x, group = WIDE ? 0 : tid >> 5;
+    const int tid = threadIdx.x, local = WIDE ? tid & 31 : (tid >> 5) % kRowsAtOnce, group = WIDE ? 0 : (tid >> 5) / kRowsAtOnce;
     const float c = a.scale_log2e;
     auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
     constexpr int kParts = WIDE ? 4 / kPieces : 1;                 // of a row's channels, a workgroup each
     const int half = blockIdx.y % kParts;
     for (int first = blockIdx.y / kParts * kRowsAtOnce; first < live; first += gridDim.y / kParts * kRowsAtOnce) {     // uniform
-        const int r = min(first + (WIDE ? tid & 31 : 0), live - 1);
+        const int r = min(first + local, live - 1);
         auto channel = [&](int j) { return 4 * (WIDE ? 8 * (kPieces * half + j) + (tid >> 5) : tid & 31); };
         auto place = [&](int j) {
             const int cg = channel(j) >> 2;
@@ -215,23 +215,23 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
             for (int i = 0; i < kAhead; ++i)
                 if (x0 + i * kGroups < parts) add(ml[i].x, ml[i].y, v[i], safe);
         }
-        if constexpr (!WIDE) {
+        if constexpr (kGroups > 1) {
             __syncthreads();                                       // the row before has been read
             *(float4*)(rest + 4 * tid) = sum[0];
-            if ((tid & 31) == 0) { rest_m[group] = M; rest_l[group] = L; }
+            if ((tid & 31) == 0) { rest_m[tid >> 5] = M; rest_l[tid >> 5] = L; }
             __syncthreads();
             if (group != 0) continue;
             float top = M;
 #pragma unroll
-            for (int x = 1; x < kGroups; ++x) top = fmaxf(top, rest_m[x]);
+            for (int x = 1; x < kGroups; ++x) top = fmaxf(top, rest_m[local + x * kRowsAtOnce]);
             const float safe = move_to(top);
 #pragma unroll
             for (int x = 1; x < kGroups; ++x) {
-                const float4 v[1] = {*(const float4*)(rest + 4 * (tid + 32 * x))};
-                add(rest_m[x], rest_l[x], v, safe);
+                const float4 v[1] = {*(const float4*)(rest + 4 * (tid + 32 * kRowsAtOnce * x))};
+                add(rest_m[local + x * kRowsAtOnce], rest_l[local + x * kRowsAtOnce], v, safe);
             }
         }
-        if (WIDE && first + (tid & 31) >= live) continue;
+        if (first + local >= live) continue;
         const float inv = L == 0.f ? 0.f : 1.0f / L;
         const int t = (int)a.by_group.div((unsigned)r), h = rec.z * a.group + r - t * a.group;
         const int64_t row = rec.x + t;
