@@ -85,22 +85,27 @@ def paged_attention(q, held_k, held_v, page_size, table, q_start, kv_len, scale)
         u = np.arange(total)
         page = np.asarray(table[i])[u // page_size] if total else np.zeros(0, dtype=np.int64)
         there = (page >= 0) & (page < pages)
+        rows = slice(int(q_start[i]), int(q_start[i]) + n)
+        see = there[None] & (u[None] <= (total - n + np.arange(n))[:, None])              # [n, total]
+        some = see.any(1)
         for h in range(hkv):
             k = np.asarray(held_k[np.where(there, page, 0), h, u % page_size], dtype=np.float64)
             v = np.asarray(held_v[np.where(there, page, 0), h, u % page_size], dtype=np.float64)
-            for t in range(n):
-                row = int(q_start[i]) + t
-                see = np.nonzero(there & (u <= total - n + t))[0]
-                if not len(see):
-                    continue
-                for g in range(G):
-                    x = q[row, h * G + g]
-                    z = k[see] @ x * scale
-                    m = z.max()
-                    p = np.exp(z - m)
-                    l = p.sum()
-                    out[row, h * G + g] = (p / l) @ v[see]
-                    size[row, h * G + g] = (p / l) @ np.abs(v[see])
-                    lse[row, h * G + g] = m + np.log(l)
-                    logit[row, h * G + g] = (np.abs(k[see]) @ np.abs(x)).max() * scale
+            odd = np.nonzero((~np.isfinite(v)).any(1))[0]
+            whole = np.where(np.isfinite(v), v, 0.0)
+            for g in range(G if some.any() else 0):
+                x = q[rows, h * G + g]
+                z = np.where(see, x @ k.T * scale, -np.inf)
+                m = np.where(some, z.max(1), 0.0)[:, None]
+                p = np.exp(z - m)
+                l = p.sum(1)
+                p = p / np.where(some, l, 1.0)[:, None]
+                y = p @ whole
+                for key in odd:                                                           # only the rows that see it have part in it
+                    for ch in np.nonzero(~np.isfinite(v[key]))[0]:
+                        y[see[:, key], ch] += p[see[:, key], key] * v[key, ch]
+                out[rows, h * G + g] = y
+                size[rows, h * G + g] = p @ np.abs(whole)
+                lse[rows, h * G + g] = np.where(some, m[:, 0] + np.log(np.where(some, l, 1.0)), -np.inf)
+                logit[rows, h * G + g] = np.where(see, np.abs(x) @ np.abs(k).T * scale, 0.0).max(1)
     return out, lse, size, logit

@@ -76,13 +76,12 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
 
     const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, kg = lane >> 4;
     const int wave = first_lane(tid >> 6);
-    Run run;
+    Run<false> run;
     const bool any = run.find(a, blockIdx.x, lane);
-    if (blockIdx.x == 0 && tid == 0) a.record[0] = any ? (int)run.used : 0;    // workgroup 0 is the first run's, if there is one
+    if (blockIdx.x == 0 && tid == 0) a.record[0] = (int)run.used;
+    if (run.logical < run.used && tid == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;
-    if (tid == 0) a.record[4 + 4 * home + 3] = 0;
-    if (!run.has_steps(a)) return;
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
     const int page_mask = (1 << a.page_shift) - 1;
 

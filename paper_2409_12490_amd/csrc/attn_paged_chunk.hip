@@ -35,7 +35,7 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
 // around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
 // WHOLE: pages of 64 keys and more, a tile lies in one: 80 scalar instructions a step less than four runs of 16 keys, 8192 new tokens of 32768 (32/8 heads) 3571 -> 3310 us.
 template <bool MX, bool WHOLE, bool ROTATED>
-__device__ __forceinline__ void work(const PagedArgs& a, Run& run, unsigned home, unsigned lds0) {
+__device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
     if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
     __syncthreads();
@@ -520,13 +520,12 @@ template <bool MX, bool WHOLE>
 __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    Run run;
+    Run<true> run;
     const bool any = run.find(a, workgroup_id(), thread_id() & 63);
-    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = any ? (int)run.used : 0;
+    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = (int)run.used;
+    if (run.logical < run.used && thread_id() == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;
-    if (thread_id() == 0) a.record[4 + 4 * home + 3] = 0;
-    if (!run.has_steps(a)) return;
     if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<MX, WHOLE, false>(a, run, home, lds0);
     else work<MX, WHOLE, true>(a, run, home, lds0);
 }

@@ -43,6 +43,8 @@ CASES = [
     # everything in one batch, sequences without new tokens and without any, new tokens that nothing is held for
     ("bf16", 8, 2, 64, [(1, 500), (200, 260), (0, 77), (1, 0), (0, 0), (5, 3), (1, 1), (64, 2000), (3, 0)]),
     ("fp32", 4, 2, 16, [(0, 0), (2, 1), (40, 100), (1, 300), (0, 10), (4, 0)]),
+    # sequences that are alike, units for two and more rounds of workgroups: none left over, some left over, an odd number of rounds
+    ("bf16", 32, 4, 16, [(512, 600)] * 8), ("bf16", 16, 2, 64, [(600, 600)] * 17), ("bf16", 64, 1, 64, [(3100, 3111)]),
 ]
 
 
