@@ -172,7 +172,8 @@ typedef struct critiprefill_cache_params {
     int32_t cache_format;                     /* CP_CACHE_* */
     int32_t page_size, n_pages;               /* page_size: a power of two, 16 or more; n_pages * page_size < 2^31 */
     int32_t n_seqs, max_pages;                /* paged_attn: sequences, and the pitch of the page table */
-    int32_t max_q_len;                        /* paged_attn: new tokens that a sequence has at most, 0: not known.  Chooses the kernel; more are right too */
+    int32_t max_q_len, max_kv_len;            /* paged_attn: new tokens, and tokens in all, that a sequence has at most, 0: not known (tokens, and
+                                                 max_pages * page_size).  They choose the kernel and the way the work is cut; more are right too */
     int32_t rotary_dim, rotary_interleaved;   /* norm_rope: channels that turn (0 .. 128, a multiple of 16), and how they pair */
     float norm_eps, attn_scale;               /* attn_scale: 0 -> 1/sqrt(head_dim) */
     int64_t q_stride[2], k_stride[2], v_stride[2]; /* token, head.  cache_read: k_stride, v_stride are the outputs' */
@@ -200,7 +201,7 @@ int critiprefill_cache_write(const critiprefill_cache_params *p, const void *k, 
 int critiprefill_cache_read(const critiprefill_cache_params *p, const int32_t *slots, const void *k_cache, const void *v_cache, const uint8_t *k_scale,
                             const uint8_t *v_scale, void *k, void *v, void *hip_stream);
 
-/* Bytes of scratch critiprefill_paged_attn needs: parts of results that several workgroups work on.  It depends on the sizes of heads, dtype and max_q_len
+/* Bytes of scratch critiprefill_paged_attn needs: parts of results that several workgroups work on.  It depends on heads, dtype, cache_format and max_q_len
  * (tokens where that is 0) alone, not on lengths.  Contents do not matter before a call; calls that may overlap need one each. */
 size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
 

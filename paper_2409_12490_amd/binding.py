@@ -34,7 +34,7 @@ class Params(ctypes.Structure):
 
 class CacheParams(ctypes.Structure):
     _fields_ = ([(x, ctypes.c_int32) for x in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "tokens", "cache_format", "page_size", "n_pages",
-                                               "n_seqs", "max_pages", "max_q_len", "rotary_dim", "rotary_interleaved")]
+                                               "n_seqs", "max_pages", "max_q_len", "max_kv_len", "rotary_dim", "rotary_interleaved")]
                 + [("norm_eps", ctypes.c_float), ("attn_scale", ctypes.c_float)]
                 + [(x, ctypes.c_int64 * 2) for x in ("q_stride", "k_stride", "v_stride", "o_stride", "ko_stride")])
 
@@ -189,7 +189,7 @@ def _dtype_code(dtype: torch.dtype) -> int:
 
 
 def make_cache_params(n_q_heads: int, n_kv_heads: int, dtype: torch.dtype, *, q=None, k=None, v=None, out=None, k_out=None, k_cache=None,
-                      mxfp8: bool = False, page_table=None, max_q_len: int = 0, rotary_dim: int = 0, interleaved: bool = False,
+                      mxfp8: bool = False, page_table=None, max_q_len: int = 0, max_kv_len: int = 0, rotary_dim: int = 0, interleaved: bool = False,
                       norm_eps: float = 0.0, attn_scale: float = 0.0) -> CacheParams:
     """Fill the parameter block from the tensors of a call: q, k, v, out (q_out or the attention's) and k_out are [tokens, heads, 128], each with
     strides of its own; k_cache [n_pages, n_kv_heads, page_size, 128] says the pool's size, page_table [n_seqs, max_pages] the sequences."""
@@ -222,7 +222,8 @@ def make_cache_params(n_q_heads: int, n_kv_heads: int, dtype: torch.dtype, *, q=
         if page_table.dim() != 2 or not page_table.is_contiguous():
             raise ValueError("page_table: expected a contiguous [n_seqs, max_pages]")
         p.n_seqs, p.max_pages = page_table.shape
-    p.max_q_len, p.rotary_dim, p.rotary_interleaved, p.norm_eps, p.attn_scale = max_q_len, rotary_dim, int(interleaved), norm_eps, attn_scale
+    p.max_q_len, p.max_kv_len, p.rotary_dim, p.rotary_interleaved = max_q_len, max_kv_len, rotary_dim, int(interleaved)
+    p.norm_eps, p.attn_scale = norm_eps, attn_scale
     return p
 
 

@@ -535,7 +535,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t st) {
     const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX, WHOLE>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((paged_chunk_kernel<MX, WHOLE>), dim3(a.workgroups), dim3(512), kSmem, st, a);
-    hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.workgroups, kChunkRows / 32 * 2), dim3(256), 0, st, a, kChunkRows);
+    if (!a.whole) hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.workgroups, kChunkRows / 32 * 2), dim3(256), 0, st, a, kChunkRows);
     return hipGetLastError();
 }
 

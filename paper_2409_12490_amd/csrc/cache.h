@@ -11,6 +11,7 @@ struct CacheShape {
     int mxfp8;                                // the cache holds e4m3 elements and a scale per 32 channels, else elements of dtype
     int page, page_shift, n_pages;            // tokens of a page, a power of two of at least 16
     int tokens, n_seqs, max_pages, max_q;
+    long long max_kv;
     int rotary, interleaved;
     float eps, scale;                         // of the norm, of the logits
     int64_t qs[2], ks[2], vs[2], os[2], kos[2];   // element strides: token, head
@@ -36,6 +37,7 @@ struct PagedRoute {
     int workgroups;
     int least;                                // steps that a workgroup takes at least
     int setup;                                // what a unit takes beside its steps, in steps
+    int whole;                                // units are not cut: sequences are known to be short, and there is nothing to join
 };
 PagedRoute paged_route(const CacheShape& sh);
 size_t paged_workspace(const CacheShape& sh);

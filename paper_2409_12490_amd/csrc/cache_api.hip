@@ -36,12 +36,13 @@ int make_cache_shape(const critiprefill_cache_params* p, int uses, cp::CacheShap
         sh->rotary = p->rotary_dim; sh->interleaved = p->rotary_interleaved != 0; sh->eps = p->norm_eps;
     }
     if (uses & USES_SEQS) {
-        if (p->n_seqs < 0 || p->max_pages < 0 || p->max_q_len < 0 || !(p->attn_scale >= 0.f)) return CP_ERR_SHAPE;
+        if (p->n_seqs < 0 || p->max_pages < 0 || p->max_q_len < 0 || p->max_kv_len < 0 || !(p->attn_scale >= 0.f)) return CP_ERR_SHAPE;
         if (sh->group > 64) return CP_ERR_UNSUPPORTED;
         sh->n_seqs = p->n_seqs; sh->max_pages = p->max_pages; sh->max_q = p->max_q_len > 0 ? p->max_q_len : p->tokens;
         sh->scale = p->attn_scale > 0.f ? p->attn_scale : 1.0f / std::sqrt((float)p->head_dim);
         const long long keys = (long long)p->max_pages * p->page_size;
         if (keys >= (1ll << 30)) return CP_ERR_UNSUPPORTED;
+        sh->max_kv = p->max_kv_len > 0 ? p->max_kv_len : keys;
         // key steps are counted in 32 bits
         const cp::PagedRoute r = cp::paged_route(*sh);
         const double tiles = (double)(sh->tokens >> r.tile_shift) + sh->n_seqs, steps = (double)(keys >> r.step_shift) + 2 + r.setup;

@@ -25,6 +25,7 @@ struct PagedArgs {
     int tokens, n_seqs, max_pages, n_pages, hq, hkv, group;
     int page_shift, tile_shift, step_shift;
     unsigned workgroups, least, setup;
+    int whole;                                // units are not cut: a unit counts as one, whatever its steps
     FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
@@ -44,6 +45,7 @@ struct Sequence {                             // one sequence, checked: whatever
 
     // the same of tiles 0 .. j - 1, j < tiles
     __device__ __forceinline__ unsigned before(const PagedArgs& a, int j) const {
+        if (a.whole) return (unsigned)j;
         // tile i: setup + ahead + ceil((i + 1) tile / step)
         unsigned n = (unsigned)j * (ahead + a.setup);
         if (a.tile_shift >= a.step_shift) return n + (((unsigned)j * (j + 1) / 2) << (a.tile_shift - a.step_shift));
@@ -62,7 +64,7 @@ struct Sequence {                             // one sequence, checked: whatever
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
         tiles = (tokens + (1 << a.tile_shift) - 1) >> a.tile_shift;
         ahead = (max(keys - tokens, 0) + (1 << a.step_shift) - 1) >> a.step_shift;
-        length = tiles ? before(a, tiles - 1) + a.setup + steps_of(a, tiles - 1) : 0u;
+        length = tiles ? before(a, tiles - 1) + (a.whole ? 1u : a.setup + steps_of(a, tiles - 1)) : 0u;
     }
     __device__ __forceinline__ Sequence of_lane(int l) const {
         Sequence s;
@@ -95,7 +97,7 @@ struct Run {
         used = 0; logical = 0; left = 0; round = rounds = 0;
         if (total == 0) return false;
         unsigned skip = 0;                                         // what the rounds take
-        if (ROUNDS && a.n_seqs <= 64) {
+        if (ROUNDS && !a.whole && a.n_seqs <= 64) {
             const Sequence one = s.of_lane(0);
             const unsigned units = (unsigned)a.n_seqs * (unsigned)a.hkv * (unsigned)one.tiles;
             if (__builtin_amdgcn_ballot_w64(s.tokens != one.tokens || s.keys != one.keys) == 0 && units >= a.workgroups) {
@@ -111,7 +113,7 @@ struct Run {
             }
         }
         total -= skip;
-        share = max(a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
+        share = max(a.whole ? 1u : a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
         used = (unsigned)first_lane((int)((total + share - 1) / share));
         // neighbouring runs share keys (tiles of one head) and go to one XCD (workgroup id mod 8)
         logical = (workgroup & 7) * ((used + 7) / 8) + (workgroup >> 3);
@@ -170,14 +172,15 @@ struct Run {
     // What there is of the present unit: steps first .. first + count - 1 of `unit`.
     __device__ __forceinline__ void piece(const PagedArgs& a, unsigned& first, unsigned& count, unsigned& unit) const {
         unit = now.steps_of(a, tile);
+        if (a.whole) { first = 0; count = unit; return; }
         first = at > a.setup ? at - a.setup : 0u;
         count = min(at + left - a.setup, unit) - first;
     }
     // Where the run has nothing but setup of its present unit, this is its last, and its steps are the next workgroup's.
-    __device__ __forceinline__ bool has_steps(const PagedArgs& a) const { return at + left > a.setup; }
+    __device__ __forceinline__ bool has_steps(const PagedArgs& a) const { return a.whole || at + left > a.setup; }
     // on to the unit behind this one; false where the run or the work ends
     __device__ __forceinline__ bool next(const PagedArgs& a) {
-        const unsigned rest = a.setup + now.steps_of(a, tile) - at;
+        const unsigned rest = a.whole ? 1u : a.setup + now.steps_of(a, tile) - at;
         if (left <= rest) return false;
         left -= rest;
         at = 0;

@@ -58,12 +58,12 @@ class Pool:
             self.cache = [k.to(DEV), v.to(DEV), None, None]
 
 
-def attend(pool, q, q_start, kv_len, table=None, max_q_len=0, out=None, scale=0.0, workspace=None):
+def attend(pool, q, q_start, kv_len, table=None, max_q_len=0, out=None, scale=0.0, workspace=None, max_kv_len=0):
     table = (pool.table if table is None else table).to(DEV)
     out = torch.full((q.shape[0], q.shape[1], 128), float("nan"), dtype=q.dtype, device=DEV) if out is None else out
     lse = torch.full(q.shape[:2], float("nan"), device=DEV)
     p = B.make_cache_params(q.shape[1], pool.hkv, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp8=pool.mxfp8, page_table=table, max_q_len=max_q_len,
-                            attn_scale=scale)
+                            max_kv_len=max_kv_len, attn_scale=scale)
     ws = B.alloc_paged_workspace(p) if workspace is None else workspace
     ws.fill_(0xff)                                                   # whatever it holds
     start, lens = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (q_start, kv_len))

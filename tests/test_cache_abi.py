@@ -63,7 +63,7 @@ EVERY = [rope, rope_write, write, read, attn]
     (dict(n_pages=1 << 25), -3, [rope_write, write, read, attn]), (dict(cache_format=2), -3, [rope_write, write, read, attn]),
     (dict(rotary_dim=-16), -2, [rope, rope_write]), (dict(rotary_dim=144), -2, [rope, rope_write]), (dict(rotary_dim=24), -3, [rope, rope_write]),
     (dict(norm_eps=-1.0), -2, [rope, rope_write]), (dict(norm_eps=float("nan")), -2, [rope, rope_write]),
-    (dict(n_seqs=-1), -2, [attn]), (dict(max_pages=-1), -2, [attn]), (dict(max_q_len=-1), -2, [attn]), (dict(attn_scale=-1.0), -2, [attn]),
+    (dict(n_seqs=-1), -2, [attn]), (dict(max_pages=-1), -2, [attn]), (dict(max_q_len=-1), -2, [attn]), (dict(max_kv_len=-1), -2, [attn]), (dict(attn_scale=-1.0), -2, [attn]),
     (dict(attn_scale=float("nan")), -2, [attn]), (dict(n_q_heads=130), -3, [attn]), (dict(max_pages=1 << 24), -3, [attn]),
     (dict(tokens=1 << 30, max_pages=1 << 20), -3, [attn]),
 ])

@@ -57,10 +57,21 @@ def test_against_fp64(case, mxfp8):
     check_attention(pool, q, start, total, out, lse)
 
 
+@pytest.mark.parametrize("keys", [0, 1, 100000])
 @pytest.mark.parametrize("hint", [0, 1, 7, 40, 2000])
-def test_any_hint_of_the_longest_chunk_is_right(hint):
-    pool, q, start, total = _case("bf16", hint % 2 == 1, 8, 2, 32, [(1, 90), (33, 150), (300, 420)])
-    out, lse = attend(pool, q, start, total, max_q_len=hint)
+def test_any_hint_of_the_longest_chunk_and_sequence_is_right(hint, keys):
+    pool, q, start, total = _case("bf16", hint % 2 == 1, 8, 2, 32, [(1, 90), (33, 150), (300, 420), (1, 1700)])
+    out, lse = attend(pool, q, start, total, max_q_len=hint, max_kv_len=keys)
+    check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("dtype,hint", [("bf16", 1), ("bf16", 0), ("fp32", 1), ("fp32", 0)])
+def test_units_that_are_not_cut(dtype, hint, mxfp8):
+    """Sequences said to be short, whatever they are: more units than workgroups, empty ones among them."""
+    seqs = [(1, 1 + 5 * i % 111) if i % 7 else (0, 0) for i in range(100)] + [(40, 900), (1, 0), (3, 2)]
+    pool, q, start, total = _case(dtype, mxfp8, 12, 6, 16, seqs)
+    out, lse = attend(pool, q, start, total, max_q_len=hint, max_kv_len=100)
     check_attention(pool, q, start, total, out, lse)
 
 
