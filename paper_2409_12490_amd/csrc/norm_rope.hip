@@ -53,50 +53,72 @@ __device__ __forceinline__ float max4(float x) {                   // over a lan
     return fmaxf(x, dpp<0x4E>(x));
 }
 
+// STREAM: what goes past the caches.  Calls that move more than kStreamBytes find nothing of theirs in a cache and leave nothing that is still there when it is read
+// (Infinity Cache: 256 MiB, shared with what runs before and after); smaller ones do.  us, ordinary / past the caches, 32/8 heads in bf16: 16384 tokens as tensors (336 MB) 73.6 / 63.8,
+// 8192 (168 MB) 40.4 / 33.2, 16384 into 8-bit pages 82.7 / 75.3, 65536 tokens' K and V into plain pages 114 / 100 and back 99 / 87; 9000 tokens' back in fp32 (147 MB) 33 / 43, 3000
+// tokens as tensors (61 MB) 15.1 / 17.0.
+constexpr long long kStreamBytes = 150ll << 20;
+template <bool STREAM, typename V>
+__device__ __forceinline__ V get(const void* p) { return STREAM ? __builtin_nontemporal_load((const V*)p) : *(const V*)p; }
+template <bool STREAM, typename V>
+__device__ __forceinline__ void put(void* p, V v) { if (STREAM) __builtin_nontemporal_store(v, (V*)p); else *(V*)p = v; }
+
+template <bool STREAM>
 __device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
-    const bf16x8 v = *(const bf16x8*)p;
+    const bf16x8 v = get<STREAM, bf16x8>(p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
 }
+template <bool STREAM>
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+    const f32x4 a = get<STREAM, f32x4>(p), b = get<STREAM, f32x4>(p + 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
 }
+template <bool STREAM>
 __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
     bf16x8 v;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
-    *(bf16x8*)p = v;
+    put<STREAM>(p, v);
 }
+template <bool STREAM>
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
     f32x4 a, b;
 #pragma unroll
     for (int e = 0; e < 4; ++e) { a[e] = x[e]; b[e] = x[4 + e]; }
-    *(f32x4*)p = a; *(f32x4*)(p + 4) = b;
+    put<STREAM>(p, a); put<STREAM>(p + 4, b);
 }
 
 // 8 channels of a row in e4m3, and in the first lane of four the biased exponent of their 32 channels.  Values that are not finite take no part in the
 // maximum and are stored as e4m3's NaN; exponents stay in 1 .. 254, where 2^(e - 127) is a normal number.
-__device__ __forceinline__ u32x2 quantise8(const float (&x)[8], int& exponent) {
-    float most = 0.f;
+__device__ __forceinline__ u32x2 quantise8(float (&x)[8], int& exponent) {
+    float most = fabsf(x[0]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
-    const unsigned bits = __float_as_uint(max4(most));
+    for (int e = 1; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));   // a NaN takes no part by itself
+    most = max4(most);
+    if (!(most < INFINITY)) {                                      // an infinity, or nothing but NaN: rare, and not worth three instructions an element
+        most = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (!(fabsf(x[e]) < INFINITY)) x[e] = NAN;
+            else most = fmaxf(most, fabsf(x[e]));
+        }
+        most = max4(most);
+    }
+    const unsigned bits = __float_as_uint(most);
     exponent = min(max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 1), 254);   // 448 = 1.75 * 2^8
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fabsf(x[e]) < INFINITY ? ldexpf(x[e], 127 - exponent) : NAN;
+    const float scale = __uint_as_float(exponent == 254 ? 0x400000u : (unsigned)(254 - exponent) << 23);     // 2^(127 - exponent), exact also where it is subnormal
     u32x2 w;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        int d = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * e], y[4 * e + 1], 0, false);
-        w[e] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * e + 2], y[4 * e + 3], d, true);
+        const int d = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e] * scale, x[4 * e + 1] * scale, 0, false);
+        w[e] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e + 2] * scale, x[4 * e + 3] * scale, d, true);
     }
     return w;
 }
 
-template <typename T, int TURN, int TO>
+template <typename T, int TURN, int TO, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     __shared__ f32x2 turns[4][64];                                 // (cos, sin) of the wave's token
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15;
@@ -130,8 +152,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     const bool turned = 8 * c16 < 2 * a.half;
     float qw[8], kw[8];
     if (TURN != TURN_NONE || TO == TO_TENSOR) {
-        if (a.qw) load8((const T*)a.qw + 8 * c16, qw);
-        if (a.kw) load8((const T*)a.kw + 8 * c16, kw);
+        if (a.qw) load8<false>((const T*)a.qw + 8 * c16, qw);
+        if (a.kw) load8<false>((const T*)a.kw + 8 * c16, kw);
     }
     for (int head = 4 * part + (lane >> 4); head < a.heads; head += 4 * a.waves) {
         const int kind = head < a.hq ? 0 : (head < a.hq + a.hkv ? 1 : 2);
@@ -139,7 +161,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
         const T* from = kind == 0 ? (const T*)a.q + token * a.qs0 + h * a.qs1
                                   : (kind == 1 ? (const T*)a.k + token * a.ks0 + h * a.ks1 : (const T*)a.v + token * a.vs0 + h * a.vs1);
         float x[8];
-        load8(from + 8 * c16, x);
+        load8<STREAM>(from + 8 * c16, x);
         if (TURN != TURN_NONE || TO == TO_TENSOR) {
             if (kind < 2 && (kind ? a.kw : a.qw)) {
                 float sq = 0.f;
@@ -175,18 +197,18 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
             }
         }
         if (kind == 0) {
-            store8((T*)a.q_out + token * a.os0 + h * a.os1 + 8 * c16, x);
+            store8<STREAM>((T*)a.q_out + token * a.os0 + h * a.os1 + 8 * c16, x);
         } else if (TO == TO_TENSOR) {
-            store8((T*)a.k_out + token * a.kos0 + h * a.kos1 + 8 * c16, x);
+            store8<STREAM>((T*)a.k_out + token * a.kos0 + h * a.kos1 + 8 * c16, x);
         } else {
             const int64_t row = (((int64_t)(slot >> a.page_shift) * a.hkv + h) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
             if (TO == TO_PLAIN) {
-                if (kept) store8((T*)(kind == 1 ? a.cache.k : a.cache.v) + row * kHeadDim + 8 * c16, x);
+                if (kept) store8<STREAM>((T*)(kind == 1 ? a.cache.k : a.cache.v) + row * kHeadDim + 8 * c16, x);
             } else {
                 int e;
                 const u32x2 w = quantise8(x, e);
                 if (kept) {
-                    *(u32x2*)((uint8_t*)(kind == 1 ? a.cache.k : a.cache.v) + row * kHeadDim + 8 * c16) = w;
+                    put<STREAM>((uint8_t*)(kind == 1 ? a.cache.k : a.cache.v) + row * kHeadDim + 8 * c16, w);
                     if ((c16 & 3) == 0) (kind == 1 ? a.cache.ks : a.cache.vs)[row * 4 + (c16 >> 2)] = (uint8_t)e;
                 }
             }
@@ -194,7 +216,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     }
 }
 
-template <typename T, bool MX>
+template <typename T, bool MX, bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15;
     const unsigned index = blockIdx.x * 4u + wave;
@@ -212,7 +234,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
         for (int e = 0; e < 8; ++e) x[e] = 0.f;                    // a token without a place in the cache
         if (held) {
             if (MX) {
-                const u32x2 w = *(const u32x2*)((const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16);
+                const u32x2 w = get<STREAM, u32x2>((const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16);
                 const float scale = __uint_as_float((unsigned)(is_v ? a.cache.vs : a.cache.ks)[row * 4 + (c16 >> 2)] << 23);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -220,10 +242,10 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
                     x[4 * e] = lo[0]; x[4 * e + 1] = lo[1]; x[4 * e + 2] = hi[0]; x[4 * e + 3] = hi[1];
                 }
             } else {
-                load8((const T*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16, x);
+                load8<STREAM>((const T*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16, x);
             }
         }
-        store8((T*)(is_v ? a.q_out : a.k_out) + token * (is_v ? a.vs0 : a.ks0) + h * (is_v ? a.vs1 : a.ks1) + 8 * c16, x);
+        store8<STREAM>((T*)(is_v ? a.q_out : a.k_out) + token * (is_v ? a.vs0 : a.ks0) + h * (is_v ? a.vs1 : a.ks1) + 8 * c16, x);
     }
 }
 
@@ -243,12 +265,26 @@ RopeArgs common(const CacheShape& sh, int heads, const CachePtr* cache) {
 
 unsigned grid_of(const RopeArgs& a) { return (unsigned)(((long long)a.tokens * a.waves + 3) / 4); }
 
+// bytes read and written: `rows` of each token as elements of dtype, `held` of each in the cache
+bool past_caches(const CacheShape& sh, int rows, int held) {
+    const long long e = sh.dtype == 1 ? 2 : 4;
+    return (long long)sh.tokens * kHeadDim * (rows * e + held * (sh.mxfp8 ? 1 : e)) > kStreamBytes;
+}
+
+template <typename T, int TURN, int TO>
+hipError_t launch(const RopeArgs& a, bool stream, hipStream_t st) {
+    if (stream) hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
 template <typename T, int TO>
-hipError_t launch(const RopeArgs& a, int turn, hipStream_t st) {
-    const dim3 grid(grid_of(a)), block(256);
-    if (turn == TURN_WHOLE) hipLaunchKernelGGL((norm_rope_kernel<T, TURN_WHOLE, TO>), grid, block, 0, st, a);
-    else if (turn == TURN_HALVES) hipLaunchKernelGGL((norm_rope_kernel<T, TURN_HALVES, TO>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((norm_rope_kernel<T, TURN_PAIRS, TO>), grid, block, 0, st, a);
+hipError_t launch_turn(const RopeArgs& a, int turn, bool stream, hipStream_t st) {
+    return turn == TURN_WHOLE ? launch<T, TURN_WHOLE, TO>(a, stream, st) : turn == TURN_HALVES ? launch<T, TURN_HALVES, TO>(a, stream, st) : launch<T, TURN_PAIRS, TO>(a, stream, st);
+}
+template <typename T, bool MX>
+hipError_t launch_read(const RopeArgs& a, bool stream, hipStream_t st) {
+    if (stream) hipLaunchKernelGGL((cache_read_kernel<T, MX, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_read_kernel<T, MX, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -260,37 +296,28 @@ hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, 
     a.q = q; a.k = k; a.v = v; a.qw = q_weight; a.kw = k_weight; a.freq = inv_freq; a.pos = positions; a.slots = slots; a.q_out = q_out; a.k_out = k_out;
     a.half = sh.rotary / 2;
     const int turn = sh.interleaved ? TURN_PAIRS : (sh.rotary == kHeadDim ? TURN_WHOLE : TURN_HALVES);
+    const bool stream = past_caches(sh, 2 * sh.hq + 2 * sh.hkv, cache ? 2 * sh.hkv : 0);
     if (sh.dtype == 1)
-        return !cache ? launch<__bf16, TO_TENSOR>(a, turn, st) : sh.mxfp8 ? launch<__bf16, TO_MXFP8>(a, turn, st) : launch<__bf16, TO_PLAIN>(a, turn, st);
-    return !cache ? launch<float, TO_TENSOR>(a, turn, st) : sh.mxfp8 ? launch<float, TO_MXFP8>(a, turn, st) : launch<float, TO_PLAIN>(a, turn, st);
+        return !cache ? launch_turn<__bf16, TO_TENSOR>(a, turn, stream, st)
+                      : sh.mxfp8 ? launch_turn<__bf16, TO_MXFP8>(a, turn, stream, st) : launch_turn<__bf16, TO_PLAIN>(a, turn, stream, st);
+    return !cache ? launch_turn<float, TO_TENSOR>(a, turn, stream, st)
+                  : sh.mxfp8 ? launch_turn<float, TO_MXFP8>(a, turn, stream, st) : launch_turn<float, TO_PLAIN>(a, turn, stream, st);
 }
 
 hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v, const int32_t* slots, const CachePtr& cache, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.hq = 0; a.k = k; a.v = v; a.slots = slots;
-    const dim3 grid(grid_of(a)), block(256);
-    if (sh.dtype == 1) {
-        if (sh.mxfp8) hipLaunchKernelGGL((norm_rope_kernel<__bf16, TURN_NONE, TO_MXFP8>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((norm_rope_kernel<__bf16, TURN_NONE, TO_PLAIN>), grid, block, 0, st, a);
-    } else {
-        if (sh.mxfp8) hipLaunchKernelGGL((norm_rope_kernel<float, TURN_NONE, TO_MXFP8>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((norm_rope_kernel<float, TURN_NONE, TO_PLAIN>), grid, block, 0, st, a);
-    }
-    return hipGetLastError();
+    const bool stream = past_caches(sh, 2 * sh.hkv, 2 * sh.hkv);
+    if (sh.dtype == 1) return sh.mxfp8 ? launch<__bf16, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<__bf16, TURN_NONE, TO_PLAIN>(a, stream, st);
+    return sh.mxfp8 ? launch<float, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<float, TURN_NONE, TO_PLAIN>(a, stream, st);
 }
 
 hipError_t launch_cache_read(const CacheShape& sh, const int32_t* slots, const CachePtr& cache, void* k, void* v, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.slots = slots; a.k_out = k; a.q_out = v;
-    const dim3 grid(grid_of(a)), block(256);
-    if (sh.dtype == 1) {
-        if (sh.mxfp8) hipLaunchKernelGGL((cache_read_kernel<__bf16, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((cache_read_kernel<__bf16, false>), grid, block, 0, st, a);
-    } else {
-        if (sh.mxfp8) hipLaunchKernelGGL((cache_read_kernel<float, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((cache_read_kernel<float, false>), grid, block, 0, st, a);
-    }
-    return hipGetLastError();
+    const bool stream = past_caches(sh, 2 * sh.hkv, 2 * sh.hkv);
+    if (sh.dtype == 1) return sh.mxfp8 ? launch_read<__bf16, true>(a, stream, st) : launch_read<__bf16, false>(a, stream, st);
+    return sh.mxfp8 ? launch_read<float, true>(a, stream, st) : launch_read<float, false>(a, stream, st);
 }
 
 }  // namespace cp
