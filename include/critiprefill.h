@@ -161,7 +161,7 @@ int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, 
  *
  * Tensors are [tokens, heads, 128]: `tokens` rows, those of all sequences one after another, with strides of token and head in the
  * parameter block (elements, multiples of 8; channels lie together), so that the parts of a joint projection are read where they are.
- * Written tensors: strides of at least 128.  tokens == 0 (and n_seqs == 0) is no error: nothing is launched or looked at.
+ * Written tensors: strides of at least 128 that leave every row its own place.  tokens == 0 (and n_seqs == 0) is no error: nothing is launched or looked at.
  */
 enum { CP_CACHE_PLAIN = 0, CP_CACHE_MXFP8 = 1 };
 
@@ -211,8 +211,9 @@ size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
  * page_table[i, u / page_size] (int32[n_seqs, max_pages]) at u % page_size.  The t-th of its n new tokens sees the tokens u <= kv_len[i] - n + t.
  * out[tokens, n_q_heads, 128] has dtype and o_stride; lse (nullable, fp32 [tokens, n_q_heads]) receives log(sum exp(scaled logits)).  A
  * row that sees nothing gets output 0 and lse -inf.  All four arrays are read on the device and the lengths never by the host: a captured call follows them.
- * Whatever they hold, nothing outside the tensors is touched: rows and lengths are cut to the tensors' sizes, and tokens of a page outside the pool are seen
- * by no row.  Rows of no sequence are not written.  At most 64 query heads for a KV head.
+ * Whatever they hold, nothing outside the tensors is touched: rows and lengths are cut to the tensors' sizes, tokens of a page outside the pool are seen
+ * by no row, and with a q_start that does not ascend nothing is done.  Rows of no sequence are not written.  out must not overlap q or the cache.  At most 64
+ * query heads for a KV head.
  */
 int critiprefill_paged_attn(const critiprefill_cache_params *p, const void *q, const void *k_cache, const void *v_cache, const uint8_t *k_scale,
                             const uint8_t *v_scale, const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len, void *out, float *lse,

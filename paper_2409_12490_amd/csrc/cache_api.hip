@@ -62,11 +62,13 @@ int check_tensor(const void* p, const int64_t* stride) {
     return CP_OK;
 }
 
-// written tensors: rows must not share elements
-int check_output(const void* p, const int64_t* stride) {
+// written tensors: rows must not share elements, so all heads of a token lie before the next token, or all tokens of a head before the next head
+int check_output(const void* p, const int64_t* stride, int tokens, int heads) {
     const int e = check_tensor(p, stride);
     if (e != CP_OK) return e;
-    return stride[0] < cp::kHeadDim || stride[1] < cp::kHeadDim ? CP_ERR_SHAPE : CP_OK;
+    if (stride[0] < cp::kHeadDim || stride[1] < cp::kHeadDim) return CP_ERR_SHAPE;
+    const bool apart = tokens == 1 || heads == 1 || (stride[0] - cp::kHeadDim) / stride[1] >= heads - 1 || (stride[1] - cp::kHeadDim) / stride[0] >= tokens - 1;
+    return apart ? CP_OK : CP_ERR_SHAPE;
 }
 
 int check_cache(const cp::CacheShape& sh, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs) {
@@ -98,7 +100,7 @@ int critiprefill_norm_rope(const critiprefill_cache_params* p, const void* q, co
     CP_TRY(make_cache_shape(p, USES_Q | USES_TURN, &sh));
     if (sh.tokens == 0) return CP_OK;
     CP_TRY(check_tensor(q, sh.qs)); CP_TRY(check_tensor(k, sh.ks));
-    CP_TRY(check_output(q_out, sh.os)); CP_TRY(check_output(k_out, sh.kos));
+    CP_TRY(check_output(q_out, sh.os, sh.tokens, sh.hq)); CP_TRY(check_output(k_out, sh.kos, sh.tokens, sh.hkv));
     CP_TRY(check_turn(sh, q_weight, k_weight, inv_freq, positions));
     return done(cp::launch_norm_rope(sh, q, k, nullptr, q_weight, k_weight, inv_freq, positions, nullptr, q_out, k_out, nullptr, (hipStream_t)hip_stream));
 }
@@ -110,7 +112,7 @@ int critiprefill_norm_rope_write(const critiprefill_cache_params* p, const void*
     CP_TRY(make_cache_shape(p, USES_Q | USES_PAGES | USES_TURN, &sh));
     if (sh.tokens == 0) return CP_OK;
     CP_TRY(check_tensor(q, sh.qs)); CP_TRY(check_tensor(k, sh.ks)); CP_TRY(check_tensor(v, sh.vs));
-    CP_TRY(check_output(q_out, sh.os));
+    CP_TRY(check_output(q_out, sh.os, sh.tokens, sh.hq));
     CP_TRY(check_turn(sh, q_weight, k_weight, inv_freq, positions));
     CP_TRY(check_ints(slots));
     CP_TRY(check_cache(sh, k_cache, v_cache, k_scale, v_scale));
@@ -135,7 +137,7 @@ int critiprefill_cache_read(const critiprefill_cache_params* p, const int32_t* s
     cp::CacheShape sh;
     CP_TRY(make_cache_shape(p, USES_PAGES, &sh));
     if (sh.tokens == 0) return CP_OK;
-    CP_TRY(check_output(k, sh.ks)); CP_TRY(check_output(v, sh.vs));
+    CP_TRY(check_output(k, sh.ks, sh.tokens, sh.hkv)); CP_TRY(check_output(v, sh.vs, sh.tokens, sh.hkv));
     CP_TRY(check_ints(slots));
     CP_TRY(check_cache(sh, k_cache, v_cache, k_scale, v_scale));
     const cp::CachePtr cache = {const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<uint8_t*>(k_scale), const_cast<uint8_t*>(v_scale)};
@@ -155,7 +157,7 @@ int critiprefill_paged_attn(const critiprefill_cache_params* p, const void* q, c
     CP_TRY(make_cache_shape(p, USES_Q | USES_PAGES | USES_SEQS, &sh));
     if (sh.tokens == 0 || sh.n_seqs == 0) return CP_OK;
     CP_TRY(check_tensor(q, sh.qs));
-    CP_TRY(check_output(out, sh.os));
+    CP_TRY(check_output(out, sh.os, sh.tokens, sh.hq));
     CP_TRY(check_ints(q_start)); CP_TRY(check_ints(kv_len));
     if (sh.max_pages) CP_TRY(check_ints(page_table));
     if (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) return CP_ERR_ALIGN;

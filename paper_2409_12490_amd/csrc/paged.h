@@ -57,7 +57,7 @@ struct Sequence {                             // one sequence, checked: whatever
         if (j == tiles - 1) return max(1u, (unsigned)(keys + (1 << a.step_shift) - 1) >> a.step_shift);   // its last token sees all keys
         return ahead + ((unsigned)(((j + 1) << a.tile_shift) + (1 << a.step_shift) - 1) >> a.step_shift);
     }
-    __device__ __forceinline__ void load(const PagedArgs& a, int s) {
+    __device__ __forceinline__ bool load(const PagedArgs& a, int s) {       // whether its rows ascend
         const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
@@ -65,6 +65,7 @@ struct Sequence {                             // one sequence, checked: whatever
         tiles = (tokens + (1 << a.tile_shift) - 1) >> a.tile_shift;
         ahead = (max(keys - tokens, 0) + (1 << a.step_shift) - 1) >> a.step_shift;
         length = tiles ? before(a, tiles - 1) + (a.whole ? 1u : a.setup + steps_of(a, tiles - 1)) : 0u;
+        return from <= to;
     }
     __device__ __forceinline__ Sequence of_lane(int l) const {
         Sequence s;
@@ -86,8 +87,9 @@ struct Run {
     __device__ __forceinline__ bool find(const PagedArgs& a, unsigned workgroup, int lane) {
         unsigned total = 0, mine = 0, upto = 0;
         Sequence s;
+        unsigned long long wrong = 0;
         for (int base = 0; base < a.n_seqs; base += 64) {
-            s.load(a, min(base + lane, a.n_seqs - 1));
+            wrong |= __builtin_amdgcn_ballot_w64(!s.load(a, min(base + lane, a.n_seqs - 1)));
             mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
             upto = mine;
 #pragma unroll
@@ -95,7 +97,8 @@ struct Run {
             total += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
         }
         used = 0; logical = 0; left = 0; round = rounds = 0;
-        if (total == 0) return false;
+        // Rows that do not ascend are nobody's: sequences could share rows, and be more work than the host has bounded.  Nobody does anything then.
+        if (wrong || total == 0) return false;
         unsigned skip = 0;                                         // what the rounds take
         if (ROUNDS && !a.whole && a.n_seqs <= 64) {
             const Sequence one = s.of_lane(0);

@@ -93,6 +93,10 @@ def test_strides():
             assert f(_strided(t, 1028, 128)) == -4 and f(_strided(t, 1024, 132)) == -4 and f(_strided(t, -1024, 128)) == -4
             if t in ("o", "ko") or f is read:
                 assert f(_strided(t, 0, 128)) == -2 and f(_strided(t, 1024, 64)) == -2
+                heads = 8 if t == "o" else 2
+                assert f(_strided(t, heads * 128 - 8, 128)) == -2 and f(_strided(t, 128, 10 * 128 - 8)) == -2      # rows that share elements
+                past = {rope: dict(q=ODD), rope_write: dict(slots=None), read: dict(slots=None), attn: dict(ws_bytes=16)}[f]
+                assert f(_strided(t, 128, 10 * 128), **past) != -2 and f(_strided(t, heads * 128 + 8, 128), **past) != -2
 
 
 def test_plain_pages_need_no_scales_and_no_rotation_needs_no_angles():

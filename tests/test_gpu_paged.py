@@ -97,9 +97,14 @@ def test_arrays_that_say_nonsense_stay_inside_the_tensors():
     pool, q, start, total = _case("bf16", False, 8, 2, 16, [(3, 60), (2, 30), (4, 100)])
     guard = torch.full((q.shape[0] + 8, 8, 128), 5.0, dtype=q.dtype, device=DEV)
     out = guard[4:-4]
-    for start_, total_ in (([-5, 3, 1, 2 ** 31 - 1], total), ([0, 2 ** 30, -2 ** 31, 9], [2 ** 31 - 1, -1, 2 ** 31 - 1]), ([9, 9, 9, 9], total), ([0, 0, 0, 0], [0, 0, 0])):
-        attend(pool, q, start_, total_, max_q_len=4, out=out)
-        attend(pool, q, start_, total_, max_q_len=0, out=out)
+    for hint in (4, 0):
+        for start_, total_ in (([-5, 3, 4, 2 ** 31 - 1], total), ([-2 ** 31, -7, 0, 9], [2 ** 31 - 1, -1, 2 ** 31 - 1]), ([0, 0, 2 ** 30, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1, 5])):
+            attend(pool, q, start_, total_, max_q_len=hint, out=out)
+        out.fill_(5.0)
+        for start_ in ([0, 9, 3, 9], [9, 9, 9, 0], [0, 3, 2, 9], [9, 9, 9, 9], [0, 0, 0, 0]):      # not ascending: nothing is done; or nothing to do
+            attend(pool, q, start_, total, max_q_len=hint, out=out)
+        assert (guard == 5).all()
+        out.fill_(7.0)
     assert (guard[:4] == 5).all() and (guard[-4:] == 5).all()
 
 
