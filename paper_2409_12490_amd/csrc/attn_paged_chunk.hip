@@ -33,8 +33,9 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
 
 // All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
 // around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
-// WHOLE: pages of 64 keys and more, a tile lies in one: 80 scalar instructions a step less than four runs of 16 keys, 8192 new tokens of 32768 (32/8 heads) 3571 -> 3310 us.
-template <bool MX, bool WHOLE, bool ROTATED>
+// RUNS: pages that a tile of 64 keys lies in: 1 (pages of 64 and more), 2 or 4 (of 16).  Four look-ups and what follows from them are 80 scalar instructions a step more than one:
+// 8192 new tokens of 32768 (32/8 heads), pages of 64, 3571 us with four and 3310 with one.
+template <bool MX, int RUNS, bool ROTATED>
 __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
     const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
     if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
@@ -82,13 +83,13 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             dma16_far((const char*)row + (((unsigned)(pch ^ r4) << 4) ^ (64 * (i & 3))), q_lds + i * 1024);
         }
 
-        // ---- pages: of tile x the entries of its runs of 16 keys (WHOLE: the tile's one), and what follows from them
-        constexpr int kRuns = WHOLE ? 1 : 4, kRunKeys = TK / kRuns;
+        // ---- pages: of tile x the entries of its runs of keys, and what follows from them
+        constexpr int kRunKeys = TK / RUNS, kRunBits = (1 << (4 / RUNS)) - 1;
         const int mask = (1 << a.page_shift) - 1;
-        int entry[kRuns];
+        int entry[RUNS];
         auto look_up = [&](int x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int g = 0; g < kRuns; ++g)
+            for (int g = 0; g < RUNS; ++g)
                 entry[g] = table[max(min(base0 + x * TK + kRunKeys * g, high), 0) >> a.page_shift];     // no branch; whether the key is there is asked in describe
         };
         int ok[4] = {0, 0, 0, 0};                                    // of tiles t .. t + 3: which runs of 16 keys are there, a bit each
@@ -96,23 +97,26 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
         auto describe = [&](int x) __attribute__((always_inline)) {  // from `entry`
             v_at[0] = at[0]; v_at[1] = at[1];
             ok[0] = ok[1]; ok[1] = ok[2]; ok[2] = ok[3]; ok[3] = 0;
-            int page[kRuns];
+            int page[RUNS];
 #pragma unroll
-            for (int g = 0; g < kRuns; ++g) {
+            for (int g = 0; g < RUNS; ++g) {
                 const bool there = (unsigned)entry[g] < (unsigned)a.n_pages && base0 + x * TK + kRunKeys * g <= high;
-                ok[3] |= there ? (WHOLE ? 15 : 1 << g) : 0;
+                ok[3] |= there ? kRunBits << (g * (4 / RUNS)) : 0;
                 page[g] = there ? entry[g] : 0;                      // keys that are not there are read from page 0 and hidden
             }
-            if (WHOLE) {
-                at[0] = (((int64_t)page[0] * a.hkv + head) << a.page_shift) + ((base0 + x * TK) & mask) + (MX ? 8 : 4) * wave;
-                at[1] = at[0] + 32;
-            } else if (MX) {
-                const int own = wave >> 1, p = own == 0 ? page[0] : own == 1 ? page[1 % kRuns] : own == 2 ? page[2 % kRuns] : page[3 % kRuns];
+            // the wave's rows: 4 * wave .. + 3 and 32 + 4 * wave .. + 3, or 8 * wave .. + 7
+            if (MX) {
+                int p = page[0];
+#pragma unroll
+                for (int g = 1; g < RUNS; ++g) p = wave / (8 / RUNS) == g ? page[g] : p;
                 at[0] = (((int64_t)p * a.hkv + head) << a.page_shift) + ((base0 + x * TK + 8 * wave) & mask);
+            } else if (RUNS == 1) {
+                at[0] = (((int64_t)page[0] * a.hkv + head) << a.page_shift) + ((base0 + x * TK) & mask) + 4 * wave;
+                at[1] = at[0] + 32;
             } else {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int p = wave < 4 ? page[2 * i % kRuns] : page[(2 * i + 1) % kRuns];
+                    const int p = RUNS == 2 ? page[i % RUNS] : wave < 4 ? page[2 * i % RUNS] : page[(2 * i + 1) % RUNS];
                     at[i] = (((int64_t)p * a.hkv + head) << a.page_shift) + ((base0 + x * TK + 32 * i + 4 * wave) & mask);
                 }
             }
@@ -336,16 +340,16 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
         // ---- prologue: the pages of tiles 0 to 3 are looked up at once; K and V of tiles 0 and 1 are asked for, then, when Q has left its place, K of tile 2
         // (8-bit: 0 and 1 are stored, 2 asked for)
         at[0] = at[1] = 0;
-        int ahead[4][kRuns];
+        int ahead[4][RUNS];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             look_up(x);
 #pragma unroll
-            for (int g = 0; g < kRuns; ++g) ahead[x][g] = entry[g];
+            for (int g = 0; g < RUNS; ++g) ahead[x][g] = entry[g];
         }
         auto describe_first = [&](int x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int g = 0; g < kRuns; ++g) entry[g] = ahead[x][g];
+            for (int g = 0; g < RUNS; ++g) entry[g] = ahead[x][g];
             describe(x);
         };
         describe_first(0);
@@ -516,7 +520,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
     }
 }
 
-template <bool MX, bool WHOLE>
+template <bool MX, int RUNS>
 __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
@@ -526,15 +530,15 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     if (run.logical < run.used && thread_id() == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;
-    if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<MX, WHOLE, false>(a, run, home, lds0);
-    else work<MX, WHOLE, true>(a, run, home, lds0);
+    if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<MX, RUNS, false>(a, run, home, lds0);
+    else work<MX, RUNS, true>(a, run, home, lds0);
 }
 
-template <bool MX, bool WHOLE>
+template <bool MX, int RUNS>
 hipError_t launch(const PagedArgs& a, hipStream_t st) {
-    const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX, WHOLE>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX, RUNS>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_chunk_kernel<MX, WHOLE>), dim3(a.workgroups), dim3(512), kSmem, st, a);
+    hipLaunchKernelGGL((paged_chunk_kernel<MX, RUNS>), dim3(a.workgroups), dim3(512), kSmem, st, a);
     if (!a.whole) hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.workgroups, kChunkRows / 32 * 2), dim3(256), 0, st, a, kChunkRows);
     return hipGetLastError();
 }
@@ -542,8 +546,9 @@ hipError_t launch(const PagedArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_paged_chunk(const CacheShape& sh, const PagedArgs& a, hipStream_t st) {
-    if (sh.page_shift >= 6) return sh.mxfp8 ? launch<true, true>(a, st) : launch<false, true>(a, st);
-    return sh.mxfp8 ? launch<true, false>(a, st) : launch<false, false>(a, st);
+    if (sh.page_shift >= 6) return sh.mxfp8 ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
+    if (sh.page_shift == 5) return sh.mxfp8 ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+    return sh.mxfp8 ? launch<true, 4>(a, st) : launch<false, 4>(a, st);
 }
 
 }  // namespace cp
