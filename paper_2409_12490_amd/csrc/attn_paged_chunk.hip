@@ -6,9 +6,15 @@
 // a SIMD half a period apart, K and V in rings of four tiles of 64 keys in LDS, 16-byte pieces swizzled by the row.  What differs: a tile's rows come from up to
 // four pages, looked up by scalar loads a step ahead (pages are whole multiples of 16 tokens, so the rows of one load lie together); rows past the sequence's end lie in
 // its last page and may hold anything, so rows of V that no row sees are zeroed in LDS; the row sum adds P before it is rounded, since the log-sum-exp is an
-// output in its own right here.
+// output in its own right here (32 additions a step for 16 dot products).
 // 8-bit pages: a thread takes 16 channels of a row of K and of V into registers, a step ahead, and writes them to LDS as bf16 (exact: the scales are powers of two).
 // Every wave converts an eighth of a tile, where conversion at the reads from LDS would have each wave convert all of it.
+//
+// What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
+// library reaches 1.24; the MFMA pipe is busy for 55 % of the launch, the vector units for 43 %, 96 % of the reads come from L2.  Over 8-bit pages 3.38 ms: 14 % more vector
+// instructions.  512 after 16384: 141 us, 0.99 PFLOP/s, with four parts to a unit and 14 us to join them.
+// Not kept: 8-bit bytes by way of LDS, three tiles in flight (no faster at 109 us for 8 x 4 tokens after 16000, 4 % slower in mixed batches); conversion that writes to LDS without bank
+// conflicts at the price of selections (257 conflict cycles a step less, 3 % slower); the places of the key loops within 32 bytes (1 % between the best and the worst).
 #include "attn_bf16.h"
 #include "paged.h"
 
