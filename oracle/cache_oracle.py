@@ -1,4 +1,4 @@
-"""fp64 checker of the operators around the paged cache: head norms with the position rotation, the 8-bit format, attention of new tokens.
+"""fp64 oracle of the operators around the paged cache: head norms with the position rotation, the 8-bit format, attention of new tokens.
 
 Written from the formulas, in numpy, without the library's code.  Functions return the result and, where it helps a test to derive how far an
 fp32 evaluation may be off, the sizes of the terms it is made of.

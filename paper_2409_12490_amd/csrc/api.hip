@@ -238,6 +238,6 @@ const char* critiprefill_strerror(int status) {
     }
 }
 
-int critiprefill_version(void) { return 200; }
+int critiprefill_version(void) { return 300; }
 
 }  // extern "C"

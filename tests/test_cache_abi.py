@@ -1,4 +1,4 @@
-"""CPU-side checks of the cache operators: the checker's own format, the refusals of the library before any launch, and of the binding."""
+"""CPU-side checks of the cache operators: the oracle's own format, the refusals of the library before any launch, and of the binding."""
 import ctypes
 
 import numpy as np
@@ -143,7 +143,7 @@ def test_binding_refuses_what_the_parameter_block_does_not_fit():
         B.critiprefill_norm_rope(p, q, k, None, None, torch.zeros(32, dtype=torch.float64), torch.zeros(4, dtype=torch.int32), q, k)
 
 
-def test_checkers_format_against_torch():
+def test_the_oracles_format_against_torch():
     rng = np.random.default_rng(0)
     x = rng.standard_normal((50, 128)) * 2.0 ** rng.integers(-20, 20, (50, 1))
     x[0] = 0.0
