@@ -131,16 +131,18 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
         int high_v = high;
         asm("" : "+v"(high_v));                                      // like wq_lo
         auto in_vector = [](int x) { asm("" : "+v"(x)); return x; };
-        // Tiles with keys that some rows do not see, or none: a weight of 0 does not keep an infinity or NaN of theirs out of a sum.  As V of such a tile comes in, rows that
-        // no row sees become 0, and so does what is not finite in the others; where there was any, `odd` in LDS is set and the unit's end adds it for the rows that see it.
+        // Tiles with keys that some rows do not see, or none: a weight of 0 does not keep an infinity or NaN of theirs out of a sum.  As V of such a tile comes in, keys that
+        // no row sees become 0, and so does what is not finite in those that some rows do not see; where there was any, `odd` in LDS is set and the unit's end adds it for the rows that see it.
         int low_v = min(past + t0, seq.keys - 1);                    // the last key that the first row sees
         asm("" : "+v"(low_v));
         auto partly = [&](int x, int bits) { return base(x) + TK - 1 > low_v || in_vector(bits) != 15; };
-        auto clean = [&](u32x4 v, bool there) __attribute__((always_inline)) -> u32x4 {
+        auto clean = [&](u32x4 v, int key, bool there) __attribute__((always_inline)) -> u32x4 {
+            there = there && key <= high_v;
+            const unsigned all_see = key <= low_v ? ~0u : 0u;
             unsigned any = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const unsigned keep = ((v[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((v[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu);
+                const unsigned keep = ((v[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u) | ((v[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | all_see;
                 any |= ~keep;
                 v[e] = there ? v[e] & keep : 0u;
             }
@@ -162,7 +164,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             for (int i = 0; i < 2; ++i) {
                 const int row = 32 * i + 4 * wave + r4;
                 const unsigned at = lds0 + kVOff + slot * kTileBytes + (32 * i + 4 * wave) * 256 + lane * 16;
-                *LDS_PTR(u32x4, at) = clean(*LDS_PTR(const u32x4, at), base(x) + row <= high_v && ((bits >> (row >> 4)) & 1));
+                *LDS_PTR(u32x4, at) = clean(*LDS_PTR(const u32x4, at), base(x) + row, (bits >> (row >> 4)) & 1);
             }
         };
         // 8-bit: the tile in flight
@@ -183,8 +185,8 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             __builtin_amdgcn_sched_barrier(0);                       // registers of one at a time
             u32x4 v2[2] = {widen8(raw_v[0], raw_v[1], sv), widen8(raw_v[2], raw_v[3], sv)};
             if (partly(x, bits)) {
-                const bool there = base(x) + xrow <= high_v && ((bits >> (xrow >> 4)) & 1);
-                v2[0] = clean(v2[0], there); v2[1] = clean(v2[1], there);
+                const bool there = (bits >> (xrow >> 4)) & 1;
+                v2[0] = clean(v2[0], base(x) + xrow, there); v2[1] = clean(v2[1], base(x) + xrow, there);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) *LDS_PTR(u32x4, row + kVOff + (((2 * xpiece + h) ^ (4 * (xrow & 3))) << 4)) = v2[h];

@@ -209,3 +209,30 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, hq, hkv, page
     fine = np.isfinite(want)
     assert fine.any() and not fine.all() and (got[np.isinf(want)] < 0).all()
     assert np.abs(got[fine] - want[fine]).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-5) * np.abs(want[fine]).max()
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("dtype,hq,hkv,page,seqs", [("bf16", 8, 2, 64, [(100, 230), (70, 5000)]), ("bf16", 16, 1, 16, [(40, 200), (33, 33)]), ("bf16", 1, 1, 32, [(700, 1000)]),
+                                                     ("bf16", 4, 1, 16, [(4, 600)]), ("fp32", 4, 1, 16, [(40, 300)])])
+@pytest.mark.parametrize("spread", [1, 5])
+def test_what_is_not_finite_at_any_key(dtype, hq, hkv, page, seqs, mxfp8, spread):
+    """Every ``spread``-th key from a little before the new tokens on holds a NaN or an infinity in a channel of its own: a row has one where a key that it sees has it."""
+    pool, q, start, total = _case(dtype, mxfp8, hq, hkv, page, seqs)
+    for i, (n, t) in enumerate(seqs):
+        for u in range(max(0, t - n - 70), t, spread):
+            if u % 128 >= 120:                                       # channels that stay finite
+                continue
+            slot = int(pool.slots[i][u])
+            for h in range(hkv):
+                at = (slot // page, h, slot % page, u % 128)
+                value = float("-inf") if u % 3 == 0 and not mxfp8 else float("nan")
+                pool.cache[1][at] = 0x7f if mxfp8 else value
+                pool.held_v[at] = value
+    out, lse = attend(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, _ = O.paged_attention(f64(q), pool.held_k, pool.held_v, page, pool.table.numpy(), start, total, 128 ** -0.5)
+    got, got_lse = f64(out), f64(lse)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want)) and np.isfinite(got_lse).all()
+    fine = np.isfinite(want)
+    assert fine.any() and not fine.all()
+    assert np.abs(got[fine] - want[fine]).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-5) * np.abs(want[fine]).max()
