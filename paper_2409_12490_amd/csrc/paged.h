@@ -13,6 +13,7 @@
 // a unit: 34 % of the reads come from L2 for 8192 new tokens of 32768, 32/8 heads, 3346 us; now 3145).
 #pragma once
 #include "cache.h"
+#include "paged_steps.h"
 
 namespace cp {
 
@@ -41,37 +42,29 @@ namespace {
 __device__ __forceinline__ int first_lane(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 struct Sequence {                             // one sequence, checked: whatever the arrays hold, rows and pages stay inside the tensors
-    int start, tokens, keys, tiles, ahead;    // ahead: steps of the keys that all its tokens see, rounded up
+    int start, tokens, keys, tiles;
     unsigned length;                          // of one KV head: the steps of its units, setup included
 
-    // the same of tiles 0 .. j - 1, j < tiles
+    // the same of tiles 0 .. j - 1
     __device__ __forceinline__ unsigned before(const PagedArgs& a, int j) const {
-        if (a.whole) return (unsigned)j;
-        // tile i: setup + ahead + ceil((i + 1) tile / step)
-        unsigned n = (unsigned)j * (ahead + a.setup);
-        if (a.tile_shift >= a.step_shift) return n + (((unsigned)j * (j + 1) / 2) << (a.tile_shift - a.step_shift));
-        const int m = a.step_shift - a.tile_shift;
-        const unsigned whole = (unsigned)j >> m, rest = (unsigned)j & ((1u << m) - 1);
-        return n + ((whole * (whole + 1) / 2) << m) + rest * (whole + 1);
+        return a.whole ? (unsigned)j : (unsigned)j * a.setup + TileSteps(tokens, keys, a.step_shift).before((unsigned)j, a.tile_shift, a.step_shift);
     }
     __device__ __forceinline__ unsigned steps_of(const PagedArgs& a, int j) const {    // without setup
-        if (j == tiles - 1) return max(1u, (unsigned)(keys + (1 << a.step_shift) - 1) >> a.step_shift);   // its last token sees all keys
-        return ahead + ((unsigned)(((j + 1) << a.tile_shift) + (1 << a.step_shift) - 1) >> a.step_shift);
+        return TileSteps(tokens, keys, a.step_shift).of((unsigned)j, a.tile_shift, a.step_shift);
     }
     __device__ __forceinline__ bool load(const PagedArgs& a, int s) {       // whether its rows ascend
         const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
-        tiles = (tokens + (1 << a.tile_shift) - 1) >> a.tile_shift;
-        ahead = (max(keys - tokens, 0) + (1 << a.step_shift) - 1) >> a.step_shift;
-        length = tiles ? before(a, tiles - 1) + (a.whole ? 1u : a.setup + steps_of(a, tiles - 1)) : 0u;
+        tiles = (int)(((unsigned)tokens + (1u << a.tile_shift) - 1) >> a.tile_shift);
+        length = before(a, tiles);
         return from <= to;
     }
     __device__ __forceinline__ Sequence of_lane(int l) const {
         Sequence s;
         s.start = __builtin_amdgcn_readlane(start, l); s.tokens = __builtin_amdgcn_readlane(tokens, l); s.keys = __builtin_amdgcn_readlane(keys, l);
-        s.tiles = __builtin_amdgcn_readlane(tiles, l); s.ahead = __builtin_amdgcn_readlane(ahead, l); s.length = (unsigned)__builtin_amdgcn_readlane((int)length, l);
+        s.tiles = __builtin_amdgcn_readlane(tiles, l); s.length = (unsigned)__builtin_amdgcn_readlane((int)length, l);
         return s;
     }
 };
