@@ -22,6 +22,7 @@
 #include "paged.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace cp {
 namespace {
@@ -476,14 +477,17 @@ PagedRoute paged_route(const CacheShape& sh) {
     // 1 x 4 after 30000 28.8 / 38.7, 8 x 4 after 16000 103 / 95 (both near the memory's rate), 8 x 8 112 / 95, 1 x 8 after 1000 16.8 / 15.1, 8 x 16 after 2000 66 / 29; 8 bits:
     // 8 x 4 after 16000 61 / 107, 8 x 8 70 / 107, 8 x 16 114 / 112.
     const long long want = (long long)sh.max_q * sh.group;
-    // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 11.3 / 7.5, after 511 10.7 / 9.6, after 1023 11.3 / 14.4,
-    // 32 x 1 of up to 512 14.7 / 10.6; 256 tokens at once 22.4 / 15.6, 64 after 448 19.9 / 21.1, 16 x up to 300 28.3 / 19.6, 64 after 960 about 21 / 35; fp32 (steps of half as many
-    // keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.
-    const bool brief = sh.max_kv <= (f32 ? 128 : 512);
     r.chunk = !f32 && want > (sh.mxfp8 ? 32 : 16);
+    // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.0 / 7.7, after 499 10.0 / 10.0, after 999 10.1 / 14.7,
+    // 32 x 1 of up to 512 14.7 / 10.6; 256 tokens at once 22.4 / 15.6, 64 after 448 19.9 / 21.1, 16 x up to 300 28.3 / 19.6, 64 after 960 about 21 / 35; fp32 (steps of half as many
+    // keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760 12.9 / 12.9, of 1000 15.9 / 15.8,
+    // 32 x 1 of 760 25.2 / 19.2, 8 bits 8 x 1 of 760 12.4 / 10.7, of 1000 14.0 / 12.2, of 1500 14.2 / 16.4, 32 x 1 of 1000 21.4 / 15.6 (a single long one among short ones: 15 % lost).
+    // (Eight waves to a workgroup, half as many steps: no faster; a unit's 56 GB/s are what one compute unit reads.)
+    const bool many = (long long)sh.n_seqs * sh.hkv >= 64;
+    const int brief = f32 ? 128 : r.chunk || !many ? 512 : sh.mxfp8 ? 1024 : 768;
     if (r.chunk) {
         r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
-        r.whole = brief;
+        r.whole = sh.max_kv <= brief;
         return r;
     }
     // the smallest tile that holds a sequence's new tokens, the largest there is for longer chunks
@@ -497,8 +501,16 @@ PagedRoute paged_route(const CacheShape& sh) {
     r.workgroups = nq == 1 || !f32 ? 512 : 256;                     // two to a compute unit, where their registers allow it
     r.least = 1;
     r.setup = 1;
-    r.whole = brief;
+    r.whole = sh.max_kv <= brief;
     return r;
+}
+
+// No more workgroups than there can be runs, from what the host knows of the lengths: any number is right, and those without a run take time to begin and end, in the
+// join above all.  A multiple of 8, see Run.
+static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r) {
+    const double units = (double)sh.hkv * ((sh.tokens >> r.tile_shift) + (double)sh.n_seqs), steps = (double)(sh.max_kv >> r.step_shift) + 2 + r.setup;
+    const double runs = r.whole ? units : units * steps / r.least;
+    return (unsigned)std::min<double>(r.workgroups, 8.0 * std::ceil(runs / 8));
 }
 
 size_t paged_workspace(const CacheShape& sh) {
@@ -526,7 +538,7 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
     a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
     a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
-    a.workgroups = route.workgroups; a.least = route.least; a.setup = route.setup; a.whole = route.whole;
+    a.workgroups = useful_workgroups(sh, route); a.least = route.least; a.setup = route.setup; a.whole = route.whole; a.mxfp8 = sh.mxfp8;
     a.by_group = FastDiv(sh.group);
     a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
     a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
@@ -537,7 +549,7 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     // A workgroup of the join takes a row with eight groups of threads, or two with four; more rows than its grid has, where a chunk is longer than was said, come in
     // turn.  Eight and four: 1 x 4 tokens after 5000 (16 rows, 64 parts) 16.1 and 17.2 us; 8 x 8 after 16000 over 8-bit pages (32 rows) 70 and 67, fp32 4/2 heads 3 x 200 40.6 and 38.7.
     const int rows = (int)std::min<long long>(route.rows, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group);
-    const dim3 grid((unsigned)route.workgroups, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
+    const dim3 grid(a.workgroups, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
     if (sh.dtype == 0) {
         if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows);
         else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows);

@@ -534,7 +534,7 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     Run<true> run;
     const bool any = run.find(a, workgroup_id(), thread_id() & 63);
-    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = (int)run.used;
+    if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = run.whole ? 0 : (int)run.used;   // whole: nothing to join
     if (run.logical < run.used && thread_id() == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;

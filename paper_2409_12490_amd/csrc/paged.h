@@ -10,7 +10,8 @@
 //
 // Where all sequences are alike and there are units for every workgroup, workgroups first take whole units, round by round to and fro, and share what
 // the rounds leave over as above: the 32 workgroups of an XCD then read the keys of one head at the same time, from its L2 (runs of equal length begin anywhere in
-// a unit: 34 % of the reads come from L2 for 8192 new tokens of 32768, 32/8 heads, 3346 us; now 3145).
+// a unit: 34 % of the reads come from L2 for 8192 new tokens of 32768, 32/8 heads, 3346 us; now 3145).  In the kernel of 256-row tiles units are not cut at all, or not those
+// that the rounds leave over, where that takes no longer: see find.
 #pragma once
 #include "cache.h"
 #include "paged_steps.h"
@@ -28,6 +29,7 @@ struct PagedArgs {
     int page_shift, tile_shift, step_shift;
     unsigned workgroups, least, setup;
     int whole;                                // units are not cut: a unit counts as one, whatever its steps
+    int mxfp8;
     FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
@@ -46,19 +48,19 @@ struct Sequence {                             // one sequence, checked: whatever
     unsigned length;                          // of one KV head: the steps of its units, setup included
 
     // the same of tiles 0 .. j - 1
-    __device__ __forceinline__ unsigned before(const PagedArgs& a, int j) const {
-        return a.whole ? (unsigned)j : (unsigned)j * a.setup + TileSteps(tokens, keys, a.step_shift).before((unsigned)j, a.tile_shift, a.step_shift);
+    __device__ __forceinline__ unsigned before(const PagedArgs& a, int j, int whole) const {
+        return whole ? (unsigned)j : (unsigned)j * a.setup + TileSteps(tokens, keys, a.step_shift).before((unsigned)j, a.tile_shift, a.step_shift);
     }
     __device__ __forceinline__ unsigned steps_of(const PagedArgs& a, int j) const {    // without setup
         return TileSteps(tokens, keys, a.step_shift).of((unsigned)j, a.tile_shift, a.step_shift);
     }
-    __device__ __forceinline__ bool load(const PagedArgs& a, int s) {       // whether its rows ascend
+    __device__ __forceinline__ bool load(const PagedArgs& a, int s, int whole) {       // whether its rows ascend
         const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
         tiles = (int)(((unsigned)tokens + (1u << a.tile_shift) - 1) >> a.tile_shift);
-        length = before(a, tiles);
+        length = before(a, tiles, whole);
         return from <= to;
     }
     __device__ __forceinline__ Sequence of_lane(int l) const {
@@ -75,28 +77,42 @@ struct Run {
     unsigned logical, used, share, left;      // its number among those that share, these, steps of each, steps left to it
     int seq, head, tile; unsigned at;         // at: inside the unit, setup first
     Sequence now;
+    int whole;                                // units are not cut
     unsigned place; int round, rounds;        // rounds: its number among all; the present round, and how many there are
     unsigned run_left, run_at; int run_seq, run_head, run_tile;     // where the run begins, kept for after the rounds
 
     __device__ __forceinline__ bool find(const PagedArgs& a, unsigned workgroup, int lane) {
-        unsigned total = 0, mine = 0, upto = 0;
+        unsigned total = 0, mine = 0, upto = 0, units = 0, longest = 0;        // units, and the longest with its setup: for ROUNDS
+        bool again = a.n_seqs > 64;
+        whole = a.whole;
         Sequence s;
         unsigned long long wrong = 0;
         for (int base = 0; base < a.n_seqs; base += 64) {
-            wrong |= __builtin_amdgcn_ballot_w64(!s.load(a, min(base + lane, a.n_seqs - 1)));
+            wrong |= __builtin_amdgcn_ballot_w64(!s.load(a, min(base + lane, a.n_seqs - 1), whole));
             mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
             upto = mine;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(upto, d); if (lane >= d) upto += o; }
             total += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+            if (ROUNDS) {
+                const bool there = base + lane < a.n_seqs && s.tiles;
+                units += there ? (unsigned)s.tiles : 0u;
+                longest = max(longest, there ? a.setup + s.steps_of(a, s.tiles - 1) : 0u);
+            }
         }
         used = 0; logical = 0; left = 0; round = rounds = 0;
+        seq = head = tile = 0; at = 0; place = 0; now = Sequence{};
         // Rows that do not ascend are nobody's: sequences could share rows, and be more work than the host has bounded.  Nobody does anything then.
         if (wrong || total == 0) return false;
         unsigned skip = 0;                                         // what the rounds take
-        if (ROUNDS && !a.whole && a.n_seqs <= 64) {
+        if (ROUNDS && !whole) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) { units += __shfl_xor(units, d); longest = max(longest, (unsigned)__shfl_xor(longest, d)); }
+            units = (unsigned)first_lane((int)units) * (unsigned)a.hkv;
+            longest = (unsigned)first_lane((int)longest);
+        }
+        if (ROUNDS && !whole && a.n_seqs <= 64) {
             const Sequence one = s.of_lane(0);
-            const unsigned units = (unsigned)a.n_seqs * (unsigned)a.hkv * (unsigned)one.tiles;
             if (__builtin_amdgcn_ballot_w64(s.tokens != one.tokens || s.keys != one.keys) == 0 && units >= a.workgroups) {
                 const unsigned last = one.steps_of(a, one.tiles - 1);
                 rounds = first_lane((int)(units / a.workgroups));
@@ -105,22 +121,40 @@ struct Run {
             if (rounds) {
                 const unsigned cut = (unsigned)rounds * a.workgroups, heads = (unsigned)first_lane((int)(cut / (unsigned)one.tiles));
                 const unsigned rest = cut - heads * (unsigned)one.tiles;
-                skip = heads * one.length + one.before(a, (int)rest);
+                skip = heads * one.length + one.before(a, (int)rest, whole);
                 place = (workgroup & 7) * (a.workgroups / 8) + (workgroup >> 3);
             }
         }
         total -= skip;
-        share = max(a.whole ? 1u : a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
-        used = (unsigned)first_lane((int)((total + share - 1) / share));
+        auto deal = [&]() {
+            share = max(whole ? 1u : a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
+            used = (unsigned)first_lane((int)((total + share - 1) / share));
+        };
+        deal();
+        if (ROUNDS && !whole && total) {
+            // Cutting evens the work out but is not free: what is left for the join is written and read again, 9 steps' worth where every workgroup leaves some and 4 in
+            // any case, and in plain pages a step of a run takes a quarter longer than one of a whole unit.  Where whole units take no longer they are not cut.
+            // us, cut / whole (32/8 heads): 4 x 300 new tokens of 600 40.5 / 29.6, of 1000 47.8 / 38.9, of 4000 102 / 106; 16 x 64 of 600 43.2 / 30.9, of 2000 59.9 / 63.2;
+            // 1 x 2000 of 2400 78.3 / 74.6; 16 x 300 of 600 (two rounds and a half) 78.1 / 72.3; 8 bits 4 x 300 of 1000 50.7 / 42.7, of 2000 67.7 / 68.6.
+            const unsigned rest = units - (unsigned)rounds * a.workgroups, turns = (unsigned)first_lane((int)((rest + a.workgroups - 1) / a.workgroups));
+            const unsigned cut = 4 + 9 * used / 256 + share + (turns == 1 && !a.mxfp8 ? share / 4 : 0);
+            if (first_lane(turns * longest <= cut)) {
+                if (rounds) { rounds += (int)turns; total = used = 0; }        // the last round not full
+                else {
+                    whole = 1; again = true; total = units;
+                    deal();
+                }
+            }
+        }
         // neighbouring runs share keys (tiles of one head) and go to one XCD (workgroup id mod 8)
         logical = (workgroup & 7) * ((used + 7) / 8) + (workgroup >> 3);
-        if ((workgroup >> 3) < (used + 7) / 8 && logical < used) {
+        if ((workgroup >> 3) < (used + 7) / 8 && logical < used) {              // not where used is 0
             left = min(share, total - logical * share);
             const unsigned begin = skip + logical * share;
             unsigned past = 0;
             for (int base = 0; base < a.n_seqs; base += 64) {
-                if (a.n_seqs > 64) {
-                    s.load(a, min(base + lane, a.n_seqs - 1));
+                if (again) {
+                    s.load(a, min(base + lane, a.n_seqs - 1), whole);
                     mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
                     upto = mine;
 #pragma unroll
@@ -137,47 +171,54 @@ struct Run {
                     int lo = 0, hi = now.tiles - 1;                // the last tile that begins at or before it
                     while (lo < hi) {
                         const int mid = (lo + hi + 1) >> 1;
-                        if (now.before(a, mid) <= rest) lo = mid; else hi = mid - 1;
+                        if (now.before(a, mid, whole) <= rest) lo = mid; else hi = mid - 1;
                     }
                     tile = lo;
-                    at = rest - now.before(a, lo);
+                    at = rest - now.before(a, lo, whole);
                     break;
                 }
                 past += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
             }
         }
         else logical = ~0u;
+        if (ROUNDS) {                                              // all of it is the same for the wave: back into scalar registers
+            auto fix = [](auto& x) { x = first_lane((int)x); };
+            fix(logical); fix(used); fix(share); fix(left); fix(at); fix(seq); fix(head); fix(tile); fix(rounds); fix(whole); fix(place);
+            fix(now.start); fix(now.tokens); fix(now.keys); fix(now.tiles); fix(now.length);
+        }
         if (ROUNDS && rounds) {
             run_left = left; run_at = at; run_seq = seq; run_head = head; run_tile = tile;
-            whole_unit(a);
-            return true;
+            return whole_unit(a);
         }
         return left > 0 && has_steps(a);
     }
-    __device__ __forceinline__ void whole_unit(const PagedArgs& a) {
+    // the unit of the present round; false where a round that is not full has none for this workgroup
+    __device__ __forceinline__ bool whole_unit(const PagedArgs& a) {
         const unsigned unit = (unsigned)round * a.workgroups + (round & 1 ? a.workgroups - 1 - place : place);
-        now.load(a, 0);                                            // all are alike but for their start
+        now.load(a, 0, whole);                                            // all are alike but for their start
         const unsigned tiles = (unsigned)first_lane(now.tiles), heads = (unsigned)first_lane((int)(unit / tiles));
         tile = (int)(unit - heads * tiles);
         seq = first_lane((int)(heads / (unsigned)a.hkv));
+        if (seq >= a.n_seqs) return false;
         head = (int)(heads - (unsigned)seq * (unsigned)a.hkv);
-        now.load(a, seq);
+        now.load(a, seq, whole);
         now = now.of_lane(0);
         at = 0;
         left = a.setup + now.steps_of(a, tile);
+        return true;
     }
     // What there is of the present unit: steps first .. first + count - 1 of `unit`.
     __device__ __forceinline__ void piece(const PagedArgs& a, unsigned& first, unsigned& count, unsigned& unit) const {
         unit = now.steps_of(a, tile);
-        if (a.whole) { first = 0; count = unit; return; }
+        if (whole) { first = 0; count = unit; return; }
         first = at > a.setup ? at - a.setup : 0u;
         count = min(at + left - a.setup, unit) - first;
     }
     // Where the run has nothing but setup of its present unit, this is its last, and its steps are the next workgroup's.
-    __device__ __forceinline__ bool has_steps(const PagedArgs& a) const { return a.whole || at + left > a.setup; }
+    __device__ __forceinline__ bool has_steps(const PagedArgs& a) const { return whole || at + left > a.setup; }
     // on to the unit behind this one; false where the run or the work ends
     __device__ __forceinline__ bool next(const PagedArgs& a) {
-        const unsigned rest = a.whole ? 1u : a.setup + now.steps_of(a, tile) - at;
+        const unsigned rest = whole ? 1u : a.setup + now.steps_of(a, tile) - at;
         if (left <= rest) return false;
         left -= rest;
         at = 0;
@@ -187,17 +228,18 @@ struct Run {
         head = 0;
         do {
             if (++seq >= a.n_seqs) return false;
-            now.load(a, seq);
+            now.load(a, seq, whole);
             now = now.of_lane(0);
         } while (now.tiles == 0);
         return true;
     }
     __device__ __forceinline__ bool next_steps(const PagedArgs& a) {
         if (ROUNDS && round < rounds) {
-            if (++round < rounds) { whole_unit(a); return true; }
+            if (++round < rounds && whole_unit(a)) return true;
+            round = rounds;
             left = run_left; at = run_at; seq = run_seq; head = run_head; tile = run_tile;
             if (left == 0) return false;
-            now.load(a, seq);
+            now.load(a, seq, whole);
             now = now.of_lane(0);
             return has_steps(a);
         }

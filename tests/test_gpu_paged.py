@@ -75,6 +75,22 @@ def test_units_that_are_not_cut(dtype, hint, mxfp8):
     check_attention(pool, q, start, total, out, lse)
 
 
+# The kernel of 256-row tiles leaves units whole where that takes no longer: all of them (alike, ragged, more sequences than a wave has lanes), those that rounds leave
+# over, in a round of its own or two; and cuts them where it does.
+DEALT = [("bf16", 32, 8, 32, [(300, 600)] * 4), ("bf16", 32, 8, 64, [(200 + 37 * i, 520 + 50 * i) for i in range(5)]), ("bf16", 8, 2, 16, [(5 + i % 40, 300 + 7 * i) for i in range(70)]),
+         ("bf16", 32, 8, 64, [(130, 560)] * 12), ("bf16", 16, 4, 16, [(460, 700)] * 10), ("bf16", 32, 8, 64, [(70, 4000), (300, 600), (0, 0), (1, 700)]), ("bf16", 32, 1, 32, [(257, 9000)]),
+         ("bf16", 4, 2, 64, [(128, 520)] * 129)]
+
+
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+@pytest.mark.parametrize("case", DEALT, ids=lambda c: f"{c[1]}x{c[2]}x{c[3]}x{len(c[4])}x{c[4][0][0]}x{c[4][0][1]}")
+def test_units_whole_and_cut(case, mxfp8):
+    dtype, hq, hkv, page, seqs = case
+    pool, q, start, total = _case(dtype, mxfp8, hq, hkv, page, seqs)
+    out, lse = attend(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    check_attention(pool, q, start, total, out, lse)
+
+
 @pytest.mark.parametrize("hint", [1, 0])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_far_logits_and_a_scale(dtype, hint):
