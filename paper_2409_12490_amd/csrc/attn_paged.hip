@@ -490,8 +490,16 @@ PagedRoute paged_route(const CacheShape& sh) {
         r.whole = sh.max_kv <= brief;
         return r;
     }
-    // the smallest tile that holds a sequence's new tokens, the largest there is for longer chunks
-    const int most = f32 ? 2 : sh.mxfp8 ? 2 : 1;
+    // The smallest tile that holds a sequence's new tokens, up to 16 rows, in bf16 over 8-bit pages (K and V converted once) and fp32 over plain ones (K and V read once) 32.  Of fp32
+    // with 32 rows one workgroup has room on a compute unit, and few steps are better shared by twice as many of 16: us, 32 / 16 rows (4/2 heads): 1 x 9 tokens after 3000
+    // 16.2 / 13.0, 1 x 16 after 8000 26.4 / 21.1, 1 x 50 after 600 15.5 / 13.2, after 3000 20.4 / 21.6, 8 x 16 after 3000 28.7 / 36.2, 1 x 500 after 8000 99 / 117; 8-bit pages 1 x 50 after
+    // 600 15.3 / 12.8, 3 x 200 after 3000 56 / 52, 20 x 200 after 8000 720 / 645.
+    int most = sh.mxfp8 ? 2 : 1;
+    if (f32) {
+        const int shift = log2_of(std::max(1, 32 / sh.group));
+        const double steps = (double)sh.n_seqs * sh.hkv * (((long long)sh.max_q + (1 << shift) - 1) >> shift) * ((double)(sh.max_kv >> 6) + 1);
+        most = !sh.mxfp8 && steps > 256 ? 2 : 1;
+    }
     int nq = 1;
     while (nq < most && (16 * nq < sh.group || (1 << log2_of(16 * nq / sh.group)) < sh.max_q)) nq *= 2;
     while (16 * nq < sh.group) nq *= 2;                             // fp32: 33 to 64 query heads a KV head
@@ -514,8 +522,8 @@ static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r) {
 }
 
 size_t paged_workspace(const CacheShape& sh) {
-    const PagedRoute r = paged_route(sh);
-    return (size_t)r.workgroups * 2 * r.rows * (kHeadDim + 2) * 4 + (4 + 4 * (size_t)r.workgroups) * 4;
+    const PagedRoute r = paged_route(sh);                           // fp32: 512 workgroups of 16 rows or 256 of 32, the same bytes but for the records
+    return (size_t)r.workgroups * 2 * r.rows * (kHeadDim + 2) * 4 + (4 + 4 * (size_t)512) * 4;
 }
 
 hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st) {
