@@ -16,10 +16,12 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # bf16 attention: MFMA results stay in architectural VGPRs (S^T feeds the softmax VALU code directly; the
 # operands that only MFMA touches live in AGPRs), and fmaxf needs no NaN-quieting pre-pass (the kernel
-# never produces NaN: masked logits are -inf and the running max is guarded).
+# never produces NaN: masked logits are -inf and the running max is guarded).  attn_paged.hip takes the former
+# alone: 32 fp32 rows lose 64 copies a step (20 x 200 tokens after 8000, 4/2 heads, 724 -> 684 us), 64 rows their
+# spills (1 x 16 tokens after 3000, 64/1 heads, 55 -> 45 us).
 _BF16_ATTN = ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-fno-honor-nans", "-mno-amdgpu-ieee"]
 EXTRA = {"attn_bf16.hip": _BF16_ATTN, "attn_bf16_rows.hip": _BF16_ATTN, "attn_bf16_half.hip": _BF16_ATTN,
-         "attn_paged_chunk.hip": _BF16_ATTN}
+         "attn_paged_chunk.hip": _BF16_ATTN, "attn_paged.hip": _BF16_ATTN[:2]}
 
 
 def _compile(src: str, objdir: str) -> str:
