@@ -157,7 +157,7 @@ int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, 
  * n_kv_heads, page_size, 4], stand for 2^(e - 127); 2^e is the smallest with max |x| <= 448 * 2^e, e in 1 .. 254.  Values that are not
  * finite have no part in the maximum and are held as NaN.  With CP_CACHE_PLAIN the scales are not read and may be NULL.
  * A token's place is its slot, page * page_size + offset; a token whose slot is not in 0 .. n_pages * page_size - 1 has no place: it is
- * not written, and read as zeros.  Two tokens of one call with the same slot leave one of the two, which one is not said.
+ * not written, and read as zeros.  Two tokens of one written call must not have the same slot: what it then holds is made of both.
  *
  * Tensors are [tokens, heads, 128]: `tokens` rows, those of all sequences one after another, with strides of token and head in the
  * parameter block (elements, multiples of 8; channels lie together), so that the parts of a joint projection are read where they are.

@@ -120,11 +120,12 @@ def _ptr(t):
 # The current stream's handle straight from torch: torch.cuda.current_stream() builds a Stream object first (2.8 of the 7.3 us
 # that a call of this module took on the host; the lookup below takes 0.1).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream(stream):
     if stream is None and _raw_stream is not None and torch.cuda.is_initialized():
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
 
 

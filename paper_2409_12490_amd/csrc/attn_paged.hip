@@ -17,8 +17,9 @@
 //
 // What bounds it, 32/8 heads: the memory, with all of K and V read once: one token after 131071 in bf16 95 us and 5.6 TB/s (a copy moves 4.9, half of it written), 48 single tokens
 // of up to 32769 each over 8-bit pages 75 us and 5.2 TB/s; MFMA and vector units are busy for a twentieth of that.  After 1999 tokens it is latency: 7 us, of which an empty launch
-// takes 3, then lengths, page table, keys and the join's launch one after another (5 more).  fp32, 4/2 heads, 3 x up to 200 tokens after 3000: 34 us, 15 of them matrix work (16x16x4
-// fp32 MFMAs, 154 TFLOP/s in a large product), the rest the beginnings and ends of runs of eight steps.
+// takes 3, then lengths, page table, keys and the join's launch one after another (4 more).  fp32, 4/2 heads: the matrix units (16x16x4 fp32 MFMAs, 154 TFLOP/s in a large product)
+// for two thirds of 20 x 200 tokens after 8000 (684 us); of 3 x up to 200 after 3000 (32 us) for 15, the rest are the beginnings and ends of runs of eight steps.  Two workgroups of
+// 32 fp32 rows to a compute unit, within 256 registers: no faster for 20 x 200 after 8000, up to 40 % slower for less.
 #include "paged.h"
 
 #include <algorithm>
