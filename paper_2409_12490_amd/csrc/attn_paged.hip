@@ -516,8 +516,9 @@ PagedRoute paged_route(const CacheShape& sh) {
 
 // No more workgroups than there can be runs, from what the host knows of the lengths: any number is right, and those without a run take time to begin and end, in the
 // join above all.  A multiple of 8, see Run.
+static double most_units(const CacheShape& sh, const PagedRoute& r) { return (double)sh.hkv * ((sh.tokens >> r.tile_shift) + (double)sh.n_seqs); }
 static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r) {
-    const double units = (double)sh.hkv * ((sh.tokens >> r.tile_shift) + (double)sh.n_seqs), steps = (double)(sh.max_kv >> r.step_shift) + 2 + r.setup;
+    const double units = most_units(sh, r), steps = (double)(sh.max_kv >> r.step_shift) + 2 + r.setup;
     const double runs = r.whole ? units : units * steps / r.least;
     return (unsigned)std::min<double>(r.workgroups, 8.0 * std::ceil(runs / 8));
 }
@@ -547,7 +548,7 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
     a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
     a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
-    a.workgroups = useful_workgroups(sh, route); a.least = route.least; a.setup = route.setup; a.whole = route.whole; a.mxfp8 = sh.mxfp8;
+    a.workgroups = useful_workgroups(sh, route); a.cut_units = (unsigned)std::min<double>(a.workgroups, most_units(sh, route)); a.least = route.least; a.setup = route.setup; a.whole = route.whole; a.mxfp8 = sh.mxfp8;
     a.by_group = FastDiv(sh.group);
     a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
     a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
@@ -558,7 +559,7 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     // A workgroup of the join takes a row with eight groups of threads, or two with four; more rows than its grid has, where a chunk is longer than was said, come in
     // turn.  Eight and four: 1 x 4 tokens after 5000 (16 rows, 64 parts) 16.1 and 17.2 us; 8 x 8 after 16000 over 8-bit pages (32 rows) 70 and 67, fp32 4/2 heads 3 x 200 40.6 and 38.7.
     const int rows = (int)std::min<long long>(route.rows, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group);
-    const dim3 grid(a.workgroups, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
+    const dim3 grid(a.cut_units, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
     if (sh.dtype == 0) {
         if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows);
         else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows);

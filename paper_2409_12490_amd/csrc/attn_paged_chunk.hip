@@ -18,6 +18,8 @@
 #include "attn_bf16.h"
 #include "paged.h"
 
+#include <algorithm>
+
 namespace cp {
 namespace {
 
@@ -543,20 +545,26 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
 }
 
 template <bool MX, int RUNS>
-hipError_t launch(const PagedArgs& a, hipStream_t st) {
+hipError_t launch(const PagedArgs& a, int rows, hipStream_t st) {
     const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX, RUNS>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((paged_chunk_kernel<MX, RUNS>), dim3(a.workgroups), dim3(512), kSmem, st, a);
-    if (!a.whole) hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.workgroups, kChunkRows / 32 * 2), dim3(256), 0, st, a, kChunkRows);
+    if (a.whole) return hipGetLastError();
+    // A workgroup of the join takes half of the channels of 32 rows, or where these are few a sixteenth, its waves every fourth part; more rows than were said come in turn.
+    // us, half / sixteenth: 1 x 20 tokens after 100000 (48 workgroups of the first kind) 11.1 / 5.7, 1 x 64 after 4000 (128) 7.5 / 9.9, after 16000 10.2 / 11.6, 1 x 256 9.6 / 18.
+    const unsigned pieces = ((unsigned)rows + 31) / 32;
+    if (2 * pieces * a.cut_units < 64) hipLaunchKernelGGL((join_kernel<__bf16, true, 4>), dim3(a.cut_units, 16 * pieces), dim3(256), 0, st, a, kChunkRows);
+    else hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.cut_units, 2 * pieces), dim3(256), 0, st, a, kChunkRows);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_paged_chunk(const CacheShape& sh, const PagedArgs& a, hipStream_t st) {
-    if (sh.page_shift >= 6) return sh.mxfp8 ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
-    if (sh.page_shift == 5) return sh.mxfp8 ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
-    return sh.mxfp8 ? launch<true, 4>(a, st) : launch<false, 4>(a, st);
+    const int rows = std::min(sh.max_q, 1 << a.tile_shift) * sh.group;       // of a tile, as far as is known
+    if (sh.page_shift >= 6) return sh.mxfp8 ? launch<true, 1>(a, rows, st) : launch<false, 1>(a, rows, st);
+    if (sh.page_shift == 5) return sh.mxfp8 ? launch<true, 2>(a, rows, st) : launch<false, 2>(a, rows, st);
+    return sh.mxfp8 ? launch<true, 4>(a, rows, st) : launch<false, 4>(a, rows, st);
 }
 
 }  // namespace cp

@@ -28,6 +28,7 @@ struct PagedArgs {
     int tokens, n_seqs, max_pages, n_pages, hq, hkv, group;
     int page_shift, tile_shift, step_shift;
     unsigned workgroups, least, setup;
+    unsigned cut_units;                       // that there can be: a workgroup leaves one at most
     int whole;                                // units are not cut: a unit counts as one, whatever its steps
     int mxfp8;
     FastDiv by_group;
@@ -250,26 +251,49 @@ struct Run {
 // Adds up the parts of a unit that more than one workgroup worked on: sum_x 2^(c (m_x - M)) O_x / sum_x 2^(c (m_x - M)) l_x.  All that a thread reads of
 // several parts is asked for at once: a part's latency, not its bytes, is what the kernel takes.
 // Few rows: 32 threads of 4 channels take a row, and GROUPS of them every GROUPS-th part, whose sums meet in LDS (8 units of 64 parts by four groups of 16
-// threads, four parts at a time: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 8 channels of a row, neighbouring threads neighbouring rows,
-// and asks for no part that is not there (six at once, the last again where there are fewer, 12 follow-ups of 1 to 300 tokens over 8-bit pages: 13.4 us, now 11.3).
+// threads, four parts at a time: 31 us, now 5).  WIDE, the layout of the kernel of 256-row tiles: a thread takes 8 channels of a row (4 with GROUPS), neighbouring threads
+// neighbouring rows, and asks for no part that is not there (six at once, the last again where there are fewer, 12 follow-ups of 1 to 300 tokens over 8-bit pages: 13.4 us, now 11).
+// The grid has a place for each unit that can be cut, and a workgroup finds the record of its own among all: with a place for each workgroup of the first kernel the
+// units of 32 parts, all their pieces, were all on one XCD (1 x 64 tokens after 16000, 32/8 heads: 42 us, now 10; 1 x 256 17 and 9.6, 1 x 512 12.3 and 9.6).
 template <typename T, bool WIDE, int GROUPS>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    constexpr int kGroups = WIDE ? 1 : GROUPS, kPieces = WIDE ? 2 : 1, kAhead = WIDE ? 4 : 8, kRowsAtOnce = WIDE ? 32 : 8 / GROUPS;
-    __shared__ __attribute__((aligned(16))) float rest[kGroups > 1 ? 8 * 128 : 4];
-    __shared__ float rest_m[8], rest_l[8];
-    const unsigned w = blockIdx.x;
-    if (w >= (unsigned)a.record[0]) return;
-    const int4 rec = *(const int4*)(a.record + 4 + 4 * w);
+    // at once: rows, fours of channels, and of each thread
+    constexpr int kRowsAtOnce = WIDE ? 32 : 8 / GROUPS, kAcross = WIDE ? 8 / GROUPS : 32, kPieces = WIDE && GROUPS == 1 ? 2 : 1, kAhead = kPieces == 2 ? 4 : 8;
+    constexpr int kParts = 32 / (kAcross * kPieces);               // of a row's channels, a workgroup each
+    __shared__ __attribute__((aligned(16))) float rest[GROUPS > 1 ? 8 * 128 : 4];
+    __shared__ float rest_m[GROUPS * kRowsAtOnce], rest_l[GROUPS * kRowsAtOnce];
+    const int tid = threadIdx.x, lane = tid & 63;
+    // the blockIdx.x-th unit that was cut: there are no more of them than units, where workgroups are up to 512
+    constexpr int kRecords = WIDE ? 4 : 8;                         // of a lane
+    const unsigned used = (unsigned)a.record[0];
+    int4 all[kRecords];
+#pragma unroll
+    for (int i = 0; i < kRecords; ++i) all[i] = *(const int4*)(a.record + 4 + 4 * min(64u * i + lane, a.workgroups - 1));
+    unsigned rank = blockIdx.x, w = ~0u;
+    int4 rec{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kRecords; ++i) {
+        const bool cut = 64u * i + lane < used && all[i].w >= 2;
+        const unsigned long long which = __builtin_amdgcn_ballot_w64(cut);
+        const unsigned n = (unsigned)__builtin_popcountll(which);
+        if (w == ~0u && rank < n) {
+            const unsigned before = __builtin_amdgcn_mbcnt_hi((unsigned)(which >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)which, 0u));
+            const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(cut && before == rank));
+            w = 64u * i + (unsigned)l;
+            rec.x = __builtin_amdgcn_readlane(all[i].x, l); rec.y = __builtin_amdgcn_readlane(all[i].y, l);
+            rec.z = __builtin_amdgcn_readlane(all[i].z, l); rec.w = __builtin_amdgcn_readlane(all[i].w, l);
+        }
+        rank -= n;                                                 // of no meaning behind the unit
+    }
+    if (w == ~0u) return;
     const int parts = rec.w, live = rec.y * a.group;
-    if (parts < 2) return;
-    const int tid = threadIdx.x, local = WIDE ? tid & 31 : (tid >> 5) % kRowsAtOnce, group = WIDE ? 0 : (tid >> 5) / kRowsAtOnce;
+    const int local = WIDE ? tid & 31 : (tid >> 5) % kRowsAtOnce, group = tid / (256 / GROUPS), across = WIDE ? (tid >> 5) % kAcross : tid & 31;
     const float c = a.scale_log2e;
     auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-    constexpr int kParts = WIDE ? 4 / kPieces : 1;                 // of a row's channels, a workgroup each
     const int half = blockIdx.y % kParts;
     for (int first = blockIdx.y / kParts * kRowsAtOnce; first < live; first += gridDim.y / kParts * kRowsAtOnce) {     // uniform
         const int r = min(first + local, live - 1);
-        auto channel = [&](int j) { return 4 * (WIDE ? 8 * (kPieces * half + j) + (tid >> 5) : tid & 31); };
+        auto channel = [&](int j) { return 4 * (kAcross * (kPieces * half + j) + across); };
         auto place = [&](int j) {
             const int cg = channel(j) >> 2;
             return WIDE ? (r >> 5) * 4096 + (cg >> 1) * 256 + ((cg & 1) * 32 + (r & 31)) * 4 : r * kHeadDim + 4 * cg;
@@ -295,37 +319,37 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
             M = top;
             return safe;
         };
-        for (int x0 = group; x0 < parts; x0 += kGroups * kAhead) {
+        for (int x0 = group; x0 < parts; x0 += GROUPS * kAhead) {
             float2 ml[kAhead]; float4 v[kAhead][kPieces];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (WIDE && x0 + i >= parts) continue;             // uniform
-                const int64_t from = slot(min(x0 + i * kGroups, parts - 1)) * rows;
+                if (WIDE && x0 + i * GROUPS >= parts) continue;    // the same for a wave
+                const int64_t from = slot(min(x0 + i * GROUPS, parts - 1)) * rows;
                 ml[i] = *(const float2*)(a.stats + 2 * (from + r));
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) v[i][j] = *(const float4*)(a.parts + from * kHeadDim + place(j));
             }
             float top = M;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) top = x0 + i * kGroups < parts ? fmaxf(top, ml[i].x) : top;
+            for (int i = 0; i < kAhead; ++i) top = x0 + i * GROUPS < parts ? fmaxf(top, ml[i].x) : top;
             const float safe = move_to(top);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (x0 + i * kGroups < parts) add(ml[i].x, ml[i].y, v[i], safe);
+                if (x0 + i * GROUPS < parts) add(ml[i].x, ml[i].y, v[i], safe);
         }
-        if constexpr (kGroups > 1) {
+        if constexpr (GROUPS > 1) {
             __syncthreads();                                       // the row before has been read
             *(float4*)(rest + 4 * tid) = sum[0];
-            if ((tid & 31) == 0) { rest_m[tid >> 5] = M; rest_l[tid >> 5] = L; }
+            if (across == 0) { rest_m[group * kRowsAtOnce + local] = M; rest_l[group * kRowsAtOnce + local] = L; }
             __syncthreads();
             if (group != 0) continue;
             float top = M;
 #pragma unroll
-            for (int x = 1; x < kGroups; ++x) top = fmaxf(top, rest_m[local + x * kRowsAtOnce]);
+            for (int x = 1; x < GROUPS; ++x) top = fmaxf(top, rest_m[local + x * kRowsAtOnce]);
             const float safe = move_to(top);
 #pragma unroll
-            for (int x = 1; x < kGroups; ++x) {
-                const float4 v[1] = {*(const float4*)(rest + 4 * (tid + 32 * kRowsAtOnce * x))};
+            for (int x = 1; x < GROUPS; ++x) {
+                const float4 v[1] = {*(const float4*)(rest + 4 * (tid + 256 / GROUPS * x))};
                 add(rest_m[local + x * kRowsAtOnce], rest_l[local + x * kRowsAtOnce], v, safe);
             }
         }
