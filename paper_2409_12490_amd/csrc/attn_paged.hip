@@ -479,16 +479,18 @@ PagedRoute paged_route(const CacheShape& sh) {
     // 8 x 4 after 16000 61 / 107, 8 x 8 70 / 107, 8 x 16 114 / 112.
     const long long want = (long long)sh.max_q * sh.group;
     r.chunk = !f32 && want > (sh.mxfp8 ? 32 : 16);
-    // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.0 / 7.7, after 499 10.0 / 10.0, after 999 10.1 / 14.7,
-    // 32 x 1 of up to 512 14.7 / 10.6; 256 tokens at once 22.4 / 15.6, 64 after 448 19.9 / 21.1, 16 x up to 300 28.3 / 19.6, 64 after 960 about 21 / 35; fp32 (steps of half as many
-    // keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760 12.9 / 12.9, of 1000 15.9 / 15.8,
-    // 32 x 1 of 760 25.2 / 19.2, 8 bits 8 x 1 of 760 12.4 / 10.7, of 1000 14.0 / 12.2, of 1500 14.2 / 16.4, 32 x 1 of 1000 21.4 / 15.6 (a single long one among short ones: 15 % lost).
+    // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.1 / 7.8, after 509 10.2 / 10.1, after 999 10.2 / 14.7;
+    // fp32 (steps of half as many keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760
+    // 13.0 / 12.5, of 1000 15.6 / 15.9, 32 x 1 of 760 26.0 / 19.5, 8 bits 8 x 1 of 760 12.6 / 10.7, of 1000 14.0 / 12.3, of 1500 14.2 / 16.4, 32 x 1 of 1000 22.2 / 15.8 (a single long
+    // one among short ones: 20 % lost).  Tiles of 256 rows: 8 units (1 x 64) of 250 keys 16.4 / 15.9, of 510 17.0 / 21.6; 16 (2 x 64) of 510 22.2 / 21.7, of 760 24.6 / 27.5; 80 (2 x 300)
+    // of 510 25.9 / 22.3, of 760 31.7 / 28.0, of 1000 34.2 / 33.0.
     // (Eight waves to a workgroup, half as many steps: no faster; a unit's 56 GB/s are what one compute unit reads.)
-    const bool many = (long long)sh.n_seqs * sh.hkv >= 64;
-    const int brief = f32 ? 128 : r.chunk || !many ? 512 : sh.mxfp8 ? 1024 : 768;
+    const double heads = (double)sh.n_seqs * sh.hkv;
+    const int brief = f32 ? 128 : heads < 64 ? 512 : sh.mxfp8 ? 1024 : 768;
     if (r.chunk) {
         r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
-        r.whole = sh.max_kv <= brief;
+        const double units = heads * (((long long)sh.max_q + (1 << r.tile_shift) - 1) >> r.tile_shift);
+        r.whole = sh.max_kv <= (units < 16 ? 256 : units < 64 ? 512 : 768);
         return r;
     }
     // The smallest tile that holds a sequence's new tokens, up to 16 rows, in bf16 over 8-bit pages (K and V converted once) and fp32 over plain ones (K and V read once) 32.  Of fp32

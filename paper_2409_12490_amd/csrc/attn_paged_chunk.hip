@@ -12,7 +12,7 @@
 //
 // What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
 // library reaches 1.24; the MFMA pipe is busy for 55 % of the launch, the vector units for 43 %, 96 % of the reads come from L2.  Over 8-bit pages 3.38 ms: 14 % more vector
-// instructions.  512 after 16384: 141 us, 0.99 PFLOP/s, with four parts to a unit and 12 us to join them.
+// instructions.  512 after 16384: 139 us, 1.01 PFLOP/s, with four parts to a unit and 10 us to join them.
 // Not kept: 8-bit bytes by way of LDS, three tiles in flight (no faster at 109 us for 8 x 4 tokens after 16000, 4 % slower in mixed batches); conversion that writes to LDS without bank
 // conflicts at the price of selections (257 conflict cycles a step less, 3 % slower); the places of the key loops within 32 bytes (1 % between the best and the worst).
 #include "attn_bf16.h"
