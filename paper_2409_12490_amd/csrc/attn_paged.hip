@@ -474,18 +474,18 @@ int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        //
 PagedRoute paged_route(const CacheShape& sh) {
     PagedRoute r;
     const bool f32 = sh.dtype == 0;
-    // Tiles of 256 rows pay from more than 16 rows on, 8-bit pages from 32.  us, 32/8 heads, waves that split the keys / tiles of 256 rows: 8 x 4 tokens after 1000 17.1 / 19.1,
-    // 1 x 4 after 30000 28.8 / 38.7, 8 x 4 after 16000 103 / 95 (both near the memory's rate), 8 x 8 112 / 95, 1 x 8 after 1000 16.8 / 15.1, 8 x 16 after 2000 66 / 29; 8 bits:
-    // 8 x 4 after 16000 61 / 107, 8 x 8 70 / 107, 8 x 16 114 / 112.
+    // Tiles of 256 rows pay from more than 16 rows on, 8-bit pages from 32; up to 32 rows not for few units and keys (and not where a token alone has more than 16).  us, 32/8 heads, waves that split the keys / tiles of 256 rows:
+    // 1 x 4 tokens of 2000 10.8 / 16.1, of 60000 44 / 56, 8 x 4 of 2000 23.6 / 26.3, of 16000 102 / 105; 1 x 8 of 2000 14.1 / 16.3, of 16000 24.6 / 29.1, of 60000 78 / 57, 8 x 8 of 2000
+    // 32.5 / 26.3, of 16000 127 / 104; 8 bits: 1 x 8 of 16000 19.9 / 28.9, 8 x 8 55 / 106, 8 x 16 114 / 112.
     const long long want = (long long)sh.max_q * sh.group;
-    r.chunk = !f32 && want > (sh.mxfp8 ? 32 : 16);
+    const double heads = (double)sh.n_seqs * sh.hkv;
+    r.chunk = !f32 && want > (sh.mxfp8 ? 32 : 16) && !(sh.group <= 16 && want <= 32 && heads <= 8 && sh.max_kv <= 24576);
     // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.1 / 7.8, after 509 10.2 / 10.1, after 999 10.2 / 14.7;
     // fp32 (steps of half as many keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760
     // 13.0 / 12.5, of 1000 15.6 / 15.9, 32 x 1 of 760 26.0 / 19.5, 8 bits 8 x 1 of 760 12.6 / 10.7, of 1000 14.0 / 12.3, of 1500 14.2 / 16.4, 32 x 1 of 1000 22.2 / 15.8 (a single long
     // one among short ones: 20 % lost).  Tiles of 256 rows: 8 units (1 x 64) of 250 keys 16.4 / 15.9, of 510 17.0 / 21.6; 16 (2 x 64) of 510 22.2 / 21.7, of 760 24.6 / 27.5; 80 (2 x 300)
     // of 510 25.9 / 22.3, of 760 31.7 / 28.0, of 1000 34.2 / 33.0.
     // (Eight waves to a workgroup, half as many steps: no faster; a unit's 56 GB/s are what one compute unit reads.)
-    const double heads = (double)sh.n_seqs * sh.hkv;
     const int brief = f32 ? 128 : heads < 64 ? 512 : sh.mxfp8 ? 1024 : 768;
     if (r.chunk) {
         r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
@@ -526,7 +526,9 @@ static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r) {
 }
 
 size_t paged_workspace(const CacheShape& sh) {
-    const PagedRoute r = paged_route(sh);                           // fp32: 512 workgroups of 16 rows or 256 of 32, the same bytes but for the records
+    CacheShape many = sh;                                          // the larger of what the number of sequences decides between
+    many.n_seqs = 1 << 20;
+    const PagedRoute r = paged_route(many);                         // fp32: 512 workgroups of 16 rows or 256 of 32, the same bytes but for the records
     return (size_t)r.workgroups * 2 * r.rows * (kHeadDim + 2) * 4 + (4 + 4 * (size_t)512) * 4;
 }
 

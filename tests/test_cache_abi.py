@@ -118,10 +118,10 @@ def test_workspace():
     assert need > 0 and attn(p, ws_bytes=need - 1) == -5
     # sizes of the lengths do not move it
     assert B.critiprefill_paged_workspace_bytes(_params(n_seqs=100, max_pages=1000)) == need
-    for fmt in (B.CP_CACHE_PLAIN, B.CP_CACHE_MXFP8):
+    for dtype, fmt in ((d, f) for d in (B.CP_DTYPE_FP32, B.CP_DTYPE_BF16) for f in (B.CP_CACHE_PLAIN, B.CP_CACHE_MXFP8)):
         for heads in (2, 8, 40, 128):
             for longest in (1, 7, 300):
-                sizes = {B.critiprefill_paged_workspace_bytes(_params(dtype=B.CP_DTYPE_FP32, cache_format=fmt, n_q_heads=heads, max_q_len=longest, n_seqs=n, max_pages=m, max_kv_len=v))
+                sizes = {B.critiprefill_paged_workspace_bytes(_params(dtype=dtype, cache_format=fmt, n_q_heads=heads, max_q_len=longest, n_seqs=n, max_pages=m, max_kv_len=v))
                          for n in (1, 9, 500) for m in (1, 30, 1000) for v in (0, 50, 3000)}
                 assert len(sizes) == 1 and min(sizes) > 0
 

@@ -80,6 +80,8 @@ def test_units_that_are_not_cut(dtype, hint, mxfp8):
 DEALT = [("bf16", 32, 8, 32, [(300, 600)] * 4), ("bf16", 32, 8, 64, [(200 + 37 * i, 520 + 50 * i) for i in range(5)]), ("bf16", 8, 2, 16, [(5 + i % 40, 300 + 7 * i) for i in range(70)]),
          ("bf16", 32, 8, 64, [(130, 560)] * 12), ("bf16", 16, 4, 16, [(460, 700)] * 10), ("bf16", 32, 8, 64, [(70, 4000), (300, 600), (0, 0), (1, 700)]), ("bf16", 32, 1, 32, [(257, 9000)]),
          ("bf16", 4, 2, 64, [(128, 520)] * 129),
+         # 17 to 32 rows: of one sequence, of a long one, of several
+         ("bf16", 32, 8, 64, [(8, 3000)]), ("bf16", 28, 4, 16, [(3, 700), (4, 90)]), ("bf16", 8, 1, 32, [(4, 26000)]), ("bf16", 32, 8, 64, [(7, 900), (5, 400)]),
          # fp32, tiles of 16 and of 32 rows
          ("fp32", 4, 2, 16, [(60, 1500), (200, 700), (1, 2000)]), ("fp32", 4, 2, 64, [(9, 700)]), ("fp32", 20, 1, 16, [(5, 200), (1, 900)]), ("fp32", 3, 1, 32, [(40, 3000), (33, 33)])]
 
