@@ -18,7 +18,8 @@ int make_cache_shape(const critiprefill_cache_params* p, int uses, cp::CacheShap
     if (p->head_dim != cp::kHeadDim) return CP_ERR_UNSUPPORTED;
     if (p->dtype != CP_DTYPE_FP32 && p->dtype != CP_DTYPE_BF16) return CP_ERR_UNSUPPORTED;
     *sh = cp::CacheShape{};
-    sh->hq = p->n_q_heads; sh->hkv = p->n_kv_heads; sh->group = (uses & USES_Q) ? sh->hq / sh->hkv : 1;
+    sh->hkv = p->n_kv_heads;
+    sh->hq = (uses & USES_Q) ? p->n_q_heads : p->n_kv_heads; sh->group = sh->hq / sh->hkv;     // without USES_Q the field may hold anything
     sh->dtype = p->dtype; sh->tokens = p->tokens;
     if (sh->hq > 65535 || sh->hkv > 65535) return CP_ERR_UNSUPPORTED;
     if (uses & USES_PAGES) {

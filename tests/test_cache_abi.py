@@ -74,6 +74,12 @@ def test_bad_sizes_are_refused_before_launch(kw, code, of):
         assert B.critiprefill_paged_workspace_bytes(_params(**kw)) == 0
 
 
+@pytest.mark.parametrize("heads", [70000, 2 ** 31 - 1, -1, 0, 7])
+def test_write_and_read_do_not_look_at_the_query_heads(heads):
+    for f in (write, read):
+        assert f(_params(n_q_heads=heads), slots=None) == -1                             # past the checks of sizes: the next refusal is another one
+
+
 @pytest.mark.parametrize("f", EVERY, ids=lambda f: f.__name__)
 def test_null_and_misaligned_arguments(f):
     assert f(None) == -1
