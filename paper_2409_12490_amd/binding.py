@@ -232,12 +232,43 @@ def _refuse(t, dtype, least):
     raise ValueError(f"expected a contiguous tensor of {dtype} with {least} elements or more, got {t.dtype} {tuple(t.shape)}")
 
 
-# Of these the library sees only an address.  The wrappers below are written out, with no calls for each argument: a single token's operators take 4 us on the
-# GPU, and a loop over arguments took 3 us of the 9 that a call took on the host.
+# Of all but q, k, v and the outputs, whose strides stand in the parameter block, the library sees only an address: type, size and contiguity are looked at here, at every
+# call.  Of the others, that there are as many elements as the block says.  Written out, with no loop over arguments: a single token's operators take 4 us on the GPU.
+_TYPES = {CP_DTYPE_FP32: torch.float32, CP_DTYPE_BF16: torch.bfloat16}
+
+
 def _ints(t, least):
     if t.dtype is not torch.int32 or t.numel() < least or not t.is_contiguous():
         _refuse(t, torch.int32, least)
     return t.data_ptr()
+
+
+def _weight(t, dtype):
+    if t.dtype is not dtype or t.numel() != 128 or not t.is_contiguous():
+        raise ValueError(f"weight: expected 128 contiguous elements of {dtype}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _few(tokens, *tensors):
+    raise ValueError(f"the parameter block says {tokens} tokens, got {' '.join(str(tuple(t.shape)) for t in tensors)}")
+
+
+def _pool(p, k_cache, v_cache, k_scale, v_scale):
+    """The addresses of the pool's four tensors, which the library takes to be as large as n_pages says."""
+    rows = p.n_pages * p.n_kv_heads * p.page_size
+    size, mxfp8 = rows * 128, p.cache_format == CP_CACHE_MXFP8
+    dtype = torch.uint8 if mxfp8 else _TYPES.get(p.dtype)
+    if k_cache.dtype is not dtype or k_cache.numel() < size or not k_cache.is_contiguous():
+        _refuse(k_cache, dtype, size)
+    if v_cache.dtype is not dtype or v_cache.numel() < size or not v_cache.is_contiguous():
+        _refuse(v_cache, dtype, size)
+    if not mxfp8 or k_scale is None or v_scale is None:                  # not read, or refused by the library
+        return k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale)
+    if k_scale.dtype is not torch.uint8 or k_scale.numel() < 4 * rows or not k_scale.is_contiguous():
+        _refuse(k_scale, torch.uint8, 4 * rows)
+    if v_scale.dtype is not torch.uint8 or v_scale.numel() < 4 * rows or not v_scale.is_contiguous():
+        _refuse(v_scale, torch.uint8, 4 * rows)
+    return k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
 
 
 def _angles(p, inv_freq, positions):
@@ -253,30 +284,43 @@ def _angles(p, inv_freq, positions):
 
 def critiprefill_norm_rope(p, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream=None):
     freq, pos = _angles(p, inv_freq, positions)
+    dtype, channels = _TYPES.get(p.dtype), p.tokens * 128
+    least_q, least_k = channels * p.n_q_heads, channels * p.n_kv_heads
+    if q.numel() < least_q or k.numel() < least_k or q_out.numel() < least_q or k_out.numel() < least_k:
+        _few(p.tokens, q, k, q_out, k_out)
     _check((_lib or load()).critiprefill_norm_rope(
-        p, q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), freq, pos,
+        p, q.data_ptr(), k.data_ptr(), None if q_weight is None else _weight(q_weight, dtype), None if k_weight is None else _weight(k_weight, dtype), freq, pos,
         q_out.data_ptr(), k_out.data_ptr(), _stream(stream)), "critiprefill_norm_rope")
 
 
 def critiprefill_norm_rope_write(p, q, k, v, q_weight, k_weight, inv_freq, positions, slots, q_out, k_cache, v_cache, k_scale=None, v_scale=None,
                                  stream=None):
     freq, pos = _angles(p, inv_freq, positions)
+    dtype, tokens = _TYPES.get(p.dtype), p.tokens
+    least_q, least_k = tokens * 128 * p.n_q_heads, tokens * 128 * p.n_kv_heads
+    if q.numel() < least_q or k.numel() < least_k or v.numel() < least_k or q_out.numel() < least_q:
+        _few(tokens, q, k, v, q_out)
     _check((_lib or load()).critiprefill_norm_rope_write(
-        p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-        freq, pos, _ints(slots, p.tokens), q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-        None if v_scale is None else v_scale.data_ptr(), _stream(stream)), "critiprefill_norm_rope_write")
+        p, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if q_weight is None else _weight(q_weight, dtype), None if k_weight is None else _weight(k_weight, dtype),
+        freq, pos, _ints(slots, tokens), q_out.data_ptr(), *_pool(p, k_cache, v_cache, k_scale, v_scale), _stream(stream)), "critiprefill_norm_rope_write")
 
 
 def critiprefill_cache_write(p, k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None):
+    tokens = p.tokens
+    least = tokens * 128 * p.n_kv_heads
+    if k.numel() < least or v.numel() < least:
+        _few(tokens, k, v)
     _check((_lib or load()).critiprefill_cache_write(
-        p, k.data_ptr(), v.data_ptr(), _ints(slots, p.tokens), k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-        None if v_scale is None else v_scale.data_ptr(), _stream(stream)), "critiprefill_cache_write")
+        p, k.data_ptr(), v.data_ptr(), _ints(slots, tokens), *_pool(p, k_cache, v_cache, k_scale, v_scale), _stream(stream)), "critiprefill_cache_write")
 
 
 def critiprefill_cache_read(p, slots, k_cache, v_cache, k_scale, v_scale, k, v, stream=None):
+    tokens = p.tokens
+    least = tokens * 128 * p.n_kv_heads
+    if k.numel() < least or v.numel() < least:
+        _few(tokens, k, v)
     _check((_lib or load()).critiprefill_cache_read(
-        p, _ints(slots, p.tokens), k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-        None if v_scale is None else v_scale.data_ptr(), k.data_ptr(), v.data_ptr(), _stream(stream)), "critiprefill_cache_read")
+        p, _ints(slots, tokens), *_pool(p, k_cache, v_cache, k_scale, v_scale), k.data_ptr(), v.data_ptr(), _stream(stream)), "critiprefill_cache_read")
 
 
 def critiprefill_paged_workspace_bytes(p: CacheParams) -> int:
@@ -285,11 +329,13 @@ def critiprefill_paged_workspace_bytes(p: CacheParams) -> int:
 
 def critiprefill_paged_attn(p, q, k_cache, v_cache, k_scale, v_scale, page_table, q_start, kv_len, out, lse, workspace, stream=None):
     seqs = p.n_seqs
-    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() < p.tokens * p.n_q_heads or not lse.is_contiguous()):
-        _refuse(lse, torch.float32, p.tokens * p.n_q_heads)
+    rows = p.tokens * p.n_q_heads
+    if q.numel() < rows * 128 or out.numel() < rows * 128:
+        _few(p.tokens, q, out)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() < rows or not lse.is_contiguous()):
+        _refuse(lse, torch.float32, rows)
     _check((_lib or load()).critiprefill_paged_attn(
-        p, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
-        None if v_scale is None else v_scale.data_ptr(), _ints(page_table, seqs * p.max_pages), _ints(q_start, seqs + 1), _ints(kv_len, seqs),
+        p, q.data_ptr(), *_pool(p, k_cache, v_cache, k_scale, v_scale), _ints(page_table, seqs * p.max_pages), _ints(q_start, seqs + 1), _ints(kv_len, seqs),
         out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
         _stream(stream)), "critiprefill_paged_attn")
 

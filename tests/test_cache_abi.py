@@ -155,6 +155,39 @@ def test_binding_refuses_what_the_parameter_block_does_not_fit():
         B.critiprefill_norm_rope(p, q, k, None, None, torch.zeros(32, dtype=torch.float64), torch.zeros(4, dtype=torch.int32), q, k)
 
 
+@pytest.mark.parametrize("mxfp8", [False, True], ids=["plain", "mxfp8"])
+def test_binding_refuses_tensors_of_which_the_library_sees_an_address(mxfp8):
+    """Pages, scales and weights of another type, too small or not contiguous, and q, k, v and outputs of fewer rows than the block says.  The library must not be reached:
+    nothing here is on a GPU."""
+    bf16, n = torch.bfloat16, 5
+    q, k, ints = torch.zeros(n, 8, 128, dtype=bf16), torch.zeros(n, 2, 128, dtype=bf16), torch.zeros(n + 1, dtype=torch.int32)
+    table, ws, w, freq = torch.zeros(n, 3, dtype=torch.int32), torch.zeros(1 << 20, dtype=torch.uint8), torch.ones(128, dtype=bf16), B.rotary_frequencies(64, device="cpu")
+    cache = B.alloc_cache(3, 2, 16, mxfp8=mxfp8, device="cpu")
+    p = B.make_cache_params(8, 2, bf16, q=q, k=k, v=k, out=q, k_out=k, k_cache=cache[0], mxfp8=mxfp8, page_table=table, rotary_dim=64)
+    names = dict(q=q, k=k, v=k, qw=w, kw=w, q_out=q, k_out=k, kc=cache[0], vc=cache[1], ks=cache[2], vs=cache[3])
+
+    def calls(t):
+        pool = (t["kc"], t["vc"], t["ks"], t["vs"])
+        return {"rope": lambda: B.critiprefill_norm_rope(p, t["q"], t["k"], t["qw"], t["kw"], freq, ints, t["q_out"], t["k_out"]),
+                "rope_write": lambda: B.critiprefill_norm_rope_write(p, t["q"], t["k"], t["v"], t["qw"], t["kw"], freq, ints, ints, t["q_out"], *pool),
+                "write": lambda: B.critiprefill_cache_write(p, t["k"], t["v"], ints, *pool),
+                "read": lambda: B.critiprefill_cache_read(p, ints, *pool, t["k"], t["v"]),
+                "attn": lambda: B.critiprefill_paged_attn(p, t["q"], *pool, table, ints, ints, t["q_out"], None, ws)}
+
+    takes = {"rope": "q k qw kw q_out k_out", "rope_write": "q k v qw kw q_out kc vc ks vs", "write": "k v kc vc ks vs", "read": "k v kc vc ks vs", "attn": "q q_out kc vc ks vs"}
+    for call, args in takes.items():
+        for name in args.split():
+            good = names[name]
+            if good is None:
+                continue
+            bad = [good[:-1]]                                                            # a page, a row or a channel less
+            if name in ("qw", "kw", "kc", "vc", "ks", "vs"):
+                bad += [good.to(torch.float16), good.to(torch.float32), torch.stack([good, good], -1)[..., 0]]
+            for b in bad:
+                with pytest.raises(ValueError):
+                    calls(dict(names, **{name: b}))[call]()
+
+
 def test_the_oracles_format_against_torch():
     rng = np.random.default_rng(0)
     x = rng.standard_normal((50, 128)) * 2.0 ** rng.integers(-20, 20, (50, 1))
