@@ -565,11 +565,11 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
     const int rows = (int)std::min<long long>(route.rows, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group);
     const dim3 grid(a.cut_units, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
     if (sh.dtype == 0) {
-        if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows);
-        else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows);
+        if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows, grid.y);
+        else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows, grid.y);
     } else {
-        if (rows <= 16) hipLaunchKernelGGL((join_kernel<__bf16, false, 8>), grid, dim3(256), 0, st, a, route.rows);
-        else hipLaunchKernelGGL((join_kernel<__bf16, false, 4>), grid, dim3(256), 0, st, a, route.rows);
+        if (rows <= 16) hipLaunchKernelGGL((join_kernel<__bf16, false, 8>), grid, dim3(256), 0, st, a, route.rows, grid.y);
+        else hipLaunchKernelGGL((join_kernel<__bf16, false, 4>), grid, dim3(256), 0, st, a, route.rows, grid.y);
     }
     return hipGetLastError();
 }

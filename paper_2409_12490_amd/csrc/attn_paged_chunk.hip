@@ -550,11 +550,13 @@ hipError_t launch(const PagedArgs& a, int rows, hipStream_t st) {
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((paged_chunk_kernel<MX, RUNS>), dim3(a.workgroups), dim3(512), kSmem, st, a);
     if (a.whole) return hipGetLastError();
-    // A workgroup of the join takes half of the channels of 32 rows, or where these are few a sixteenth, its waves every fourth part; more rows than were said come in turn.
-    // us, half / sixteenth: 1 x 20 tokens after 100000 (48 workgroups of the first kind) 11.1 / 5.7, 1 x 64 after 4000 (128) 7.5 / 9.9, after 16000 10.2 / 11.6, 1 x 256 9.6 / 18.
+    // A workgroup of the join takes half of the channels of 32 rows, or where these are fewer workgroups than the chip has compute units a sixteenth, its waves every fourth part;
+    // more rows than were said come in turn.  us of the whole call, half / sixteenth (bf16, pages of 64): 32 workgroups of the first kind (4/1 heads, 1 x 64 tokens of 20000) 47.5 / 26.6,
+    // 48 (32/8, 1 x 20 of 100000) 89.6 / 86.9, 64 (8/2, 1 x 64 of 16000) 44.4 / 29.2, 128 (32/8, 30 of 40000 and 20 of 9000) 53.5 / 52.3, 160 (8/2, 1 x 256 of 9000) 31.7 / 31.3,
+    // (8/1, 1 x 300 of 20000) 45.5 / 45.8, 192 (32/4, 1 x 64 of 30000) 51.0 / 50.3, 256 (32/8, 1 x 64 of 16000) 37.9 / 39.0, 640 (32/8, 1 x 256 of 16000) 80.9 / 86.8.
     const unsigned pieces = ((unsigned)rows + 31) / 32;
-    if (2 * pieces * a.cut_units < 64) hipLaunchKernelGGL((join_kernel<__bf16, true, 4>), dim3(a.cut_units, 16 * pieces), dim3(256), 0, st, a, kChunkRows);
-    else hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.cut_units, 2 * pieces), dim3(256), 0, st, a, kChunkRows);
+    if (2 * pieces * a.cut_units < 256) hipLaunchKernelGGL((join_kernel<__bf16, true, 4>), dim3(a.cut_units, 16 * pieces), dim3(256), 0, st, a, kChunkRows, 16 * pieces);
+    else hipLaunchKernelGGL((join_kernel<__bf16, true, 1>), dim3(a.cut_units, 2 * pieces), dim3(256), 0, st, a, kChunkRows, 2 * pieces);
     return hipGetLastError();
 }
 

@@ -256,20 +256,20 @@ struct Run {
 // The grid has a place for each unit that can be cut, and a workgroup finds the record of its own among all: with a place for each workgroup of the first kernel the
 // units of 32 parts, all their pieces, were all on one XCD (1 x 64 tokens after 16000, 32/8 heads: 42 us, now 10; 1 x 256 17 and 9.6, 1 x 512 12.3 and 9.6).
 template <typename T, bool WIDE, int GROUPS>
-__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
-    // at once: rows, fours of channels, and of each thread
+__global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows, unsigned grid_y) {
+    // threadIdx and its like are calls where this is compiled without IEEE mode: attn_bf16.h.  at once: rows, fours of channels, and of each thread
     constexpr int kRowsAtOnce = WIDE ? 32 : 8 / GROUPS, kAcross = WIDE ? 8 / GROUPS : 32, kPieces = WIDE && GROUPS == 1 ? 2 : 1, kAhead = kPieces == 2 ? 4 : 8;
     constexpr int kParts = 32 / (kAcross * kPieces);               // of a row's channels, a workgroup each
     __shared__ __attribute__((aligned(16))) float rest[GROUPS > 1 ? 8 * 128 : 4];
     __shared__ float rest_m[GROUPS * kRowsAtOnce], rest_l[GROUPS * kRowsAtOnce];
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = (int)__builtin_amdgcn_workitem_id_x(), lane = tid & 63;
     // the blockIdx.x-th unit that was cut: there are no more of them than units, where workgroups are up to 512
     constexpr int kRecords = WIDE ? 4 : 8;                         // of a lane
     const unsigned used = (unsigned)a.record[0];
     int4 all[kRecords];
 #pragma unroll
     for (int i = 0; i < kRecords; ++i) all[i] = *(const int4*)(a.record + 4 + 4 * min(64u * i + lane, a.workgroups - 1));
-    unsigned rank = blockIdx.x, w = ~0u;
+    unsigned rank = __builtin_amdgcn_workgroup_id_x(), w = ~0u;
     int4 rec{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < kRecords; ++i) {
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows) {
     const int local = WIDE ? tid & 31 : (tid >> 5) % kRowsAtOnce, group = tid / (256 / GROUPS), across = WIDE ? (tid >> 5) % kAcross : tid & 31;
     const float c = a.scale_log2e;
     auto slot = [&](int x) { return 2 * (int64_t)(w + x) + (x == 0 ? 1 : 0); };
-    const int half = blockIdx.y % kParts;
-    for (int first = blockIdx.y / kParts * kRowsAtOnce; first < live; first += gridDim.y / kParts * kRowsAtOnce) {     // uniform
+    const int half = (int)(__builtin_amdgcn_workgroup_id_y() % kParts), turn = (int)(__builtin_amdgcn_workgroup_id_y() / kParts), turns = (int)(grid_y / kParts);
+    for (int first = turn * kRowsAtOnce; first < live; first += turns * kRowsAtOnce) {     // uniform
         const int r = min(first + local, live - 1);
         auto channel = [&](int j) { return 4 * (kAcross * (kPieces * half + j) + across); };
         auto place = [&](int j) {
