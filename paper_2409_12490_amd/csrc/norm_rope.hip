@@ -9,7 +9,7 @@
 // Sixteen lanes take a head of a token, 8 neighbouring channels each (16 bytes of bf16), so that
 // sums over a head and maxima over 32 channels are DPP exchanges.  A wave stays with one token: its 64 lanes work out the token's angles once, one
 // pair each, in 64 bits (a far position times a frequency loses its turn in 32: 131072 * 2^-24 is 0.008 radians) and hand them round through LDS.
-// Sums, angles' sines and products are 32 bits; an output is rounded once, keys to e4m3 from 32 bits and not by way of bf16.
+// Sums, angles' sines (with what an angle loses as it becomes 32 bits) and products are 32 bits; an output is rounded once, keys to e4m3 from 32 bits and not by way of bf16.
 // (A head of four tokens to a wave, so that rows and scales follow each other in a page, took 97 us for 85 at 65536 tokens; the four scales of a row in one store: no difference.)
 // Scales are powers of two: e4m3 keeps its 4 significant bits under any of them, while x8 * 2^e is exact in bf16, which is what attention multiplies.
 #include "cache.h"
@@ -135,9 +135,11 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     float cs[8], sn[8];                                            // of the lane's channels; of its four pairs
     if (TURN != TURN_NONE) {
         const double angle = lane < a.half ? (double)a.pos[token] * a.freq[lane] * 0.15915494309189533577 : 0.0;   // in whole turns
+        const double half_turns = 2.0 * (angle - rint(angle));
+        const float near = (float)half_turns, rest = (float)(half_turns - near) * 3.14159265f;   // what the cast leaves out, up to 9e-8, which a small sine is made of
         float s, c;
-        sincospif((float)(2.0 * (angle - rint(angle))), &s, &c);
-        turns[wave][lane] = f32x2{c, s};
+        sincospif(near, &s, &c);
+        turns[wave][lane] = f32x2{fmaf(-s, rest, c), fmaf(c, rest, s)};
         __builtin_amdgcn_wave_barrier();
         if (TURN == TURN_PAIRS) {
 #pragma unroll

@@ -205,3 +205,23 @@ def test_another_stream():
     B.critiprefill_norm_rope(p, q, k, None, None, freq, pos, outs[2], outs[3], stream=side)
     side.synchronize()
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_small_sines_and_cosines(interleaved):
+    """Unit vectors turn into the sine and cosine themselves, in fp32.  Each is allowed 4 units of its own last place (what such functions are commonly specified to), and 2^-30 for
+    the angle, which fp64 has to 2^-53 of 2^20 positions' 1.7 * 10^5 turns, three roundings: nothing for an angle that was rounded to fp32 on the way, which is up to 2^-23.3 off near half a turn, where
+    the sine is small."""
+    tokens = 20000
+    gen = torch.Generator().manual_seed(11)
+    x = torch.zeros((tokens, 1, 128), device=DEV)
+    c = torch.arange(64)
+    x[:, 0, (2 * c if interleaved else c).to(DEV)] = 1.0
+    pos, freq = torch.randint(0, 1 << 20, (tokens,), generator=gen).int().to(DEV), B.rotary_frequencies()
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    p = B.make_cache_params(1, 1, x.dtype, q=x, k=x, out=y, k_out=z, rotary_dim=128, interleaved=interleaved)
+    B.critiprefill_norm_rope(p, x, x, None, None, freq, pos, y, z)
+    want, _ = O.norm_rope(f64(x), None, pos.cpu().numpy(), f64(freq), 128, interleaved, 0.0)
+    bound = 4 * 2.0 ** -23 * np.abs(want) + 2.0 ** -30
+    for got in (f64(y), f64(z)):
+        assert np.max(np.abs(got - want) / bound) <= 1.0, f"{np.max(np.abs(got - want) / bound):.2f} of the bound"
