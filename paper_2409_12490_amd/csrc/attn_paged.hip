@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
     if (run.logical < run.used && tid == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;
-    const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
+    const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
     const int page_mask = (1 << a.page_shift) - 1;
 
     while (true) {

@@ -45,7 +45,7 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
 // 8192 new tokens of 32768 (32/8 heads), pages of 64, 3571 us with four and 3310 with one.
 template <bool MX, int RUNS, bool ROTATED>
 __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
-    const float c = a.scale_log2e, lazy_raw = kLazyLog2 / c;
+    const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
     if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
     __syncthreads();
     while (true) {

@@ -103,6 +103,16 @@ def test_far_logits_and_a_scale(dtype, hint):
     check_attention(pool, q, start, total, out, lse, scale=0.5)
 
 
+@pytest.mark.parametrize("hint", [1, 0])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [1e-38, 2e-30])
+def test_a_scale_next_to_nothing(scale, dtype, hint):
+    """All keys weigh the same; units of several steps that are not cut."""
+    pool, q, start, total = _case(dtype, False, 4, 2, 16, [(1, 900), (20, 700)])
+    out, lse = attend(pool, q, start, total, max_q_len=hint, max_kv_len=100, scale=scale)
+    check_attention(pool, q, start, total, out, lse, scale=scale)
+
+
 @pytest.mark.parametrize("dtype,mxfp8,hint", [("bf16", False, 1), ("bf16", True, 1), ("bf16", False, 0), ("bf16", True, 0), ("fp32", False, 1), ("fp32", True, 0)])
 def test_pages_outside_the_pool_hold_nothing(dtype, mxfp8, hint):
     pool, q, start, total = _case(dtype, mxfp8, 8, 2, 16, [(1, 200), (1, 40), (30, 150), (1, 9)])
