@@ -6,7 +6,7 @@ A prompt's queries and keys get their norms and positions (critiprefill_norm_rop
 and its keys and values into the pages of a cache, in 8 bits unless --plain (critiprefill_cache_write).  A follow-up of some hundred tokens goes on from there
 as a chunk, then single tokens: norms, positions and the write in one call (critiprefill_norm_rope_write), then attention over the pages
 (critiprefill_paged_attn).  The single step is captured into a graph that follows the lengths on the device.  Prints the time of each part, and how far the
-follow-up's rows over the cache are from the same rows of dense attention over the keys and values as they were.
+rows of the follow-up and of the captured steps over the cache are from the same rows of dense attention over the keys and values as they were.
 """
 from __future__ import annotations
 
@@ -40,7 +40,7 @@ class Layer:
         """qkv [tokens, HQ + 2 HKV, D] as a joint projection writes it.  Returns the output [tokens, HQ, D] and the keys as attention saw them."""
         n = qkv.shape[0]
         q, k, v = qkv.split([HQ, HKV, HKV], 1)
-        qr, kr, out = torch.empty_like(q.contiguous()), torch.empty_like(k.contiguous()), torch.empty((n, HQ, D), dtype=q.dtype, device=self.device)
+        qr, kr, out = (torch.empty((n, heads, D), dtype=q.dtype, device=self.device) for heads in (HQ, HKV, HQ))
         p = B.make_cache_params(HQ, HKV, q.dtype, q=q, k=k, out=qr, k_out=kr, rotary_dim=D, norm_eps=1e-5)
         pos = torch.arange(n, dtype=torch.int32, device=self.device)
         B.critiprefill_norm_rope(p, q, k, *self.weights, self.freq, pos, qr, kr)
@@ -95,8 +95,37 @@ def _timed(f):
     return a.elapsed_time(b) * 1e3, r
 
 
+def decode(layer: Layer, tokens: torch.Tensor):
+    """One token after another through a captured step, which reads positions, slots and the length from tensors.  Outputs [steps, HQ, D], and the time of each step in us."""
+    token = tokens[:1].clone()
+    s = layer.plan(token)
+    held = layer.held
+    layer.place(s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer.extend(s)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.extend(s)
+    layer.held = held
+    outs, us = [], []
+    for i in range(tokens.shape[0]):
+        token.copy_(tokens[i:i + 1])
+        layer.place(s)
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        graph.replay()
+        b.record()
+        torch.cuda.synchronize()
+        us.append(a.elapsed_time(b) * 1e3)
+        outs.append(s["out"].clone())
+    return torch.cat(outs), us
+
+
 def _dense_rows(layer: Layer, kr: torch.Tensor, qkv: torch.Tensor, follow: torch.Tensor):
-    """The follow-up's rows by dense attention over keys and values that no cache has held."""
+    """The rows of all tokens behind the prompt by dense attention over keys and values that no cache has held."""
     n, m = kr.shape[0], follow.shape[0]
     q, k, v = follow.split([HQ, HKV, HKV], 1)
     qr, kn = torch.empty((m, HQ, D), dtype=q.dtype, device=q.device), torch.empty((m, HKV, D), dtype=q.dtype, device=q.device)
@@ -120,45 +149,24 @@ def run(prompt: int = 16384, follow: int = 700, steps: int = 16, mxfp8: bool = T
         return (x + 0.1 * torch.randn((n, HQ + 2 * HKV, D), generator=gen, device="cuda").cumsum(0)).bfloat16()
 
     layer = Layer(prompt + follow + steps + 1, mxfp8, seed=seed)
-    qkv, more, token = projected(prompt), projected(follow), projected(1).clone()
+    qkv, more = projected(prompt), projected(follow)
     prefill_us, (_, kr) = _timed(lambda: layer.prefill(qkv))
 
     s = layer.plan(more)
     layer.place(s)
     chunk_us, out = _timed(lambda: layer.extend(s))
-    dense = _dense_rows(layer, kr, qkv, more)
-    off = float((out.float() - dense.float()).norm() / dense.float().norm())
 
-    # one token at a time; the captured step reads positions, slots and the length from tensors
-    s1 = layer.plan(token)
-    side = torch.cuda.Stream()
-    held = layer.held
-    layer.place(s1)
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        layer.extend(s1)
-    torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        layer.extend(s1)
-    layer.held = held
-    outs, step_us = [], []
-    for _ in range(steps):
-        token.copy_(projected(1))
-        layer.place(s1)
-        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        a.record()
-        graph.replay()
-        b.record()
-        torch.cuda.synchronize()
-        step_us.append(a.elapsed_time(b) * 1e3)
-        outs.append(s1["out"].clone())
-    found = {"prefill_us": prefill_us, "chunk_us": chunk_us, "step_us": sorted(step_us)[len(step_us) // 2], "off": off, "held": layer.held,
-             "finite": bool(torch.isfinite(torch.cat(outs)).all() and torch.isfinite(out).all())}
+    tokens = torch.cat([projected(1) for _ in range(steps)])
+    outs, step_us = decode(layer, tokens)
+    dense = _dense_rows(layer, kr, qkv, torch.cat([more, tokens])).float()
+    off = float((out.float() - dense[:follow]).norm() / dense[:follow].norm())
+    step_off = ((outs.float() - dense[follow:]).flatten(1).norm(dim=1) / dense[follow:].flatten(1).norm(dim=1)).tolist()
+    found = {"prefill_us": prefill_us, "chunk_us": chunk_us, "step_us": sorted(step_us)[steps // 2], "off": off, "step_off": step_off, "held": layer.held,
+             "finite": bool(torch.isfinite(outs).all() and torch.isfinite(out).all())}
     if verbose:
         print(f"prompt of {prompt}: norms, positions, pruned prefill and cache {prefill_us:.0f} us")
         print(f"follow-up of {follow} over the cache ({'8 bits' if mxfp8 else 'bf16'}): {chunk_us:.0f} us, {off:.2e} from dense attention over what was cached")
-        print(f"single tokens, captured: {found['step_us']:.1f} us each; {layer.held} tokens held")
+        print(f"single tokens, captured: {found['step_us']:.1f} us each, {max(step_off):.2e} at most from dense attention; {layer.held} tokens held")
     return found
 
 
