@@ -23,6 +23,7 @@ struct CachePtr {
     uint8_t *ks, *vs;
 };
 
+bool cache_call_streams(const CacheShape& sh, int rows, int held);
 hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
                             const double* inv_freq, const int32_t* positions, const int32_t* slots, void* q_out, void* k_out, const CachePtr* cache, hipStream_t st);
 hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v, const int32_t* slots, const CachePtr& cache, hipStream_t st);

@@ -270,12 +270,6 @@ RopeArgs common(const CacheShape& sh, int heads, const CachePtr* cache) {
 
 unsigned grid_of(const RopeArgs& a) { return (unsigned)(((long long)a.tokens * a.waves + 3) / 4); }
 
-// bytes read and written: `rows` of each token as elements of dtype, `held` of each in the cache
-bool past_caches(const CacheShape& sh, int rows, int held) {
-    const long long e = sh.dtype == 1 ? 2 : 4;
-    return (long long)sh.tokens * kHeadDim * (rows * e + held * (sh.mxfp8 ? 1 : e)) > kStreamBytes;
-}
-
 template <typename T, int TURN, int TO>
 hipError_t launch(const RopeArgs& a, bool stream, hipStream_t st) {
     if (stream) hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
@@ -295,13 +289,19 @@ hipError_t launch_read(const RopeArgs& a, bool stream, hipStream_t st) {
 
 }  // namespace
 
+// Whether a call goes past the caches: bytes read and written, `rows` of each token as elements of dtype, `held` of each in the cache.
+bool cache_call_streams(const CacheShape& sh, int rows, int held) {
+    const long long e = sh.dtype == 1 ? 2 : 4;
+    return (long long)sh.tokens * kHeadDim * (rows * e + held * (sh.mxfp8 ? 1 : e)) > kStreamBytes;
+}
+
 hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
                             const double* inv_freq, const int32_t* positions, const int32_t* slots, void* q_out, void* k_out, const CachePtr* cache, hipStream_t st) {
     RopeArgs a = common(sh, sh.hq + sh.hkv + (cache ? sh.hkv : 0), cache);
     a.q = q; a.k = k; a.v = v; a.qw = q_weight; a.kw = k_weight; a.freq = inv_freq; a.pos = positions; a.slots = slots; a.q_out = q_out; a.k_out = k_out;
     a.half = sh.rotary / 2;
     const int turn = sh.interleaved ? TURN_PAIRS : (sh.rotary == kHeadDim ? TURN_WHOLE : TURN_HALVES);
-    const bool stream = past_caches(sh, 2 * sh.hq + 2 * sh.hkv, cache ? 2 * sh.hkv : 0);
+    const bool stream = cache_call_streams(sh, 2 * sh.hq + 2 * sh.hkv, cache ? 2 * sh.hkv : 0);
     if (sh.dtype == 1)
         return !cache ? launch_turn<__bf16, TO_TENSOR>(a, turn, stream, st)
                       : sh.mxfp8 ? launch_turn<__bf16, TO_MXFP8>(a, turn, stream, st) : launch_turn<__bf16, TO_PLAIN>(a, turn, stream, st);
@@ -312,7 +312,7 @@ hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, 
 hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v, const int32_t* slots, const CachePtr& cache, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.hq = 0; a.k = k; a.v = v; a.slots = slots;
-    const bool stream = past_caches(sh, 2 * sh.hkv, 2 * sh.hkv);
+    const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
     if (sh.dtype == 1) return sh.mxfp8 ? launch<__bf16, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<__bf16, TURN_NONE, TO_PLAIN>(a, stream, st);
     return sh.mxfp8 ? launch<float, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<float, TURN_NONE, TO_PLAIN>(a, stream, st);
 }
@@ -320,7 +320,7 @@ hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v
 hipError_t launch_cache_read(const CacheShape& sh, const int32_t* slots, const CachePtr& cache, void* k, void* v, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.slots = slots; a.k_out = k; a.q_out = v;
-    const bool stream = past_caches(sh, 2 * sh.hkv, 2 * sh.hkv);
+    const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
     if (sh.dtype == 1) return sh.mxfp8 ? launch_read<__bf16, true>(a, stream, st) : launch_read<__bf16, false>(a, stream, st);
     return sh.mxfp8 ? launch_read<float, true>(a, stream, st) : launch_read<float, false>(a, stream, st);
 }

@@ -1,6 +1,8 @@
 """Shared plumbing of the tests of the cache operators: pools, page tables, calls through the binding.  No arithmetic of the operators lives here."""
 from __future__ import annotations
 
+import ctypes
+
 import numpy as np
 import torch
 
@@ -90,3 +92,27 @@ def check_attention(pool, q, q_start, kv_len, out, lse, table=None, scale=128 **
     assert (got_lse[empty] == -np.inf).all() and (got[empty] == 0).all()
     err = np.abs(np.where(empty, 0.0, got_lse) - np.where(empty, 0.0, want_lse))
     assert (err <= 2 * delta).all(), f"lse: {np.max(err / delta) / 2:.2f} of the bound"
+
+
+class Shape(ctypes.Structure):                   # cp::CacheShape of csrc/cache.h
+    _fields_ = ([(x, ctypes.c_int) for x in ("hq", "hkv", "group", "dtype", "mxfp8", "page", "page_shift", "n_pages", "tokens", "n_seqs", "max_pages", "max_q")]
+                + [("max_kv", ctypes.c_longlong)] + [(x, ctypes.c_int) for x in ("rotary", "interleaved")] + [(x, ctypes.c_float) for x in ("eps", "scale")]
+                + [(x, ctypes.c_int64 * 2) for x in ("qs", "ks", "vs", "os", "kos")])
+
+
+class Route(ctypes.Structure):                   # cp::PagedRoute of csrc/cache.h
+    _fields_ = [(x, ctypes.c_int) for x in ("chunk", "rows", "tile_shift", "step_shift", "workgroups", "least", "setup", "whole")]
+
+
+def streams(dtype, mxfp8, tokens, rows, held):
+    """Whether the library takes a call past the caches: its own rule."""
+    f = B.load()._ZN2cp18cache_call_streamsERKNS_10CacheShapeEii
+    f.argtypes, f.restype = [ctypes.POINTER(Shape), ctypes.c_int, ctypes.c_int], ctypes.c_bool
+    return f(Shape(dtype=int(dtype == "bf16"), mxfp8=int(mxfp8), tokens=tokens), rows, held)
+
+
+def route(dtype, mxfp8, hq, hkv, seqs, max_q, max_kv):
+    """Which kernel attention over pages takes, and how it cuts the work, as far as the host decides: its own rule."""
+    f = B.load()._ZN2cp11paged_routeERKNS_10CacheShapeE
+    f.argtypes, f.restype = [ctypes.POINTER(Shape)], Route
+    return f(Shape(dtype=int(dtype == "bf16"), mxfp8=int(mxfp8), hq=hq, hkv=hkv, group=hq // hkv, n_seqs=seqs, max_q=max_q, max_kv=max_kv))
