@@ -116,8 +116,7 @@ struct Run {
             const Sequence one = s.of_lane(0);
             if (__builtin_amdgcn_ballot_w64(s.tokens != one.tokens || s.keys != one.keys) == 0 && units >= a.workgroups) {
                 const unsigned last = one.steps_of(a, one.tiles - 1);
-                rounds = first_lane((int)(units / a.workgroups));
-                if (16 * (last - min(last, one.steps_of(a, 0))) > last) rounds &= ~1;     // to and fro, unless the tiles are of nearly one length
+                rounds = first_lane((int)whole_rounds(units, a.workgroups, one.steps_of(a, 0), last));
             }
             if (rounds) {
                 const unsigned cut = (unsigned)rounds * a.workgroups, heads = (unsigned)first_lane((int)(cut / (unsigned)one.tiles));
@@ -133,13 +132,8 @@ struct Run {
         };
         deal();
         if (ROUNDS && !whole && total) {
-            // Cutting evens the work out but is not free: what is left for the join is written and read again, 9 steps' worth where every workgroup leaves some and 4 in
-            // any case, and in plain pages a step of a run takes a quarter longer than one of a whole unit.  Where whole units take no longer they are not cut.
-            // us, cut / whole (32/8 heads): 4 x 300 new tokens of 600 40.5 / 29.6, of 1000 47.8 / 38.9, of 4000 102 / 106; 16 x 64 of 600 43.2 / 30.9, of 2000 59.9 / 63.2;
-            // 1 x 2000 of 2400 78.3 / 74.6; 16 x 300 of 600 (two rounds and a half) 78.1 / 72.3; 8 bits 4 x 300 of 1000 50.7 / 42.7, of 2000 67.7 / 68.6.
             const unsigned rest = units - (unsigned)rounds * a.workgroups, turns = (unsigned)first_lane((int)((rest + a.workgroups - 1) / a.workgroups));
-            const unsigned cut = 4 + 9 * used / 256 + share + (turns == 1 && !a.mxfp8 ? share / 4 : 0);
-            if (first_lane(turns * longest <= cut)) {
+            if (first_lane(uncut_pays(turns, longest, used, share, a.mxfp8))) {
                 if (rounds) { rounds += (int)turns; total = used = 0; }        // the last round not full
                 else {
                     whole = 1; again = true; total = units;

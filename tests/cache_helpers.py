@@ -2,6 +2,11 @@
 from __future__ import annotations
 
 import ctypes
+import functools
+import os
+import shutil
+import subprocess
+import tempfile
 
 import numpy as np
 import torch
@@ -116,3 +121,66 @@ def route(dtype, mxfp8, hq, hkv, seqs, max_q, max_kv):
     f = B.load()._ZN2cp11paged_routeERKNS_10CacheShapeE
     f.argtypes, f.restype = [ctypes.POINTER(Shape)], Route
     return f(Shape(dtype=int(dtype == "bf16"), mxfp8=int(mxfp8), hq=hq, hkv=hkv, group=hq // hkv, n_seqs=seqs, max_q=max_q, max_kv=max_kv))
+
+
+# How the kernel of 256-row tiles deals its units out, from the header that it takes its rules from; what is written out here is the sum over sequences, units in order.
+_DEALING = """
+#define __host__
+#define __device__
+#define __forceinline__ inline
+#include "paged_steps.h"
+extern "C" void dealing(int n, const int* tokens, const int* keys, int hkv, int tile_shift, int step_shift, unsigned workgroups, unsigned least, unsigned setup, int mxfp8, unsigned* found) {
+    unsigned units = 0, total = 0, longest = 0, first = 0, last = 0;
+    bool alike = n <= 64;
+    for (int i = 0; i < n; ++i) {
+        const cp::TileSteps t(tokens[i], keys[i], step_shift);
+        const unsigned tiles = (tokens[i] + (1u << tile_shift) - 1) >> tile_shift;
+        if (tiles == 0) { alike = false; continue; }
+        first = t.of(0, tile_shift, step_shift); last = t.of(tiles - 1, tile_shift, step_shift);
+        units += tiles * hkv; total += (tiles * setup + t.before(tiles, tile_shift, step_shift)) * hkv;
+        if (setup + last > longest) longest = setup + last;
+        alike = alike && tokens[i] == tokens[0] && keys[i] == keys[0];
+    }
+    unsigned rounds = alike && units >= workgroups ? cp::whole_rounds(units, workgroups, first, last) : 0;
+    if (rounds) {                                                  // all are as the first
+        const cp::TileSteps t(tokens[0], keys[0], step_shift);
+        const unsigned tiles = (tokens[0] + (1u << tile_shift) - 1) >> tile_shift, cut = rounds * workgroups, heads = cut / tiles, rest = cut - heads * tiles;
+        total -= heads * (tiles * setup + t.before(tiles, tile_shift, step_shift)) + rest * setup + t.before(rest, tile_shift, step_shift);
+    }
+    unsigned share = (total + workgroups - 1) / workgroups;
+    if (share < least) share = least;
+    const unsigned used = (total + share - 1) / share, over = units - rounds * workgroups, turns = (over + workgroups - 1) / workgroups;
+    const bool uncut = total && cp::uncut_pays(turns, longest, used, share, mxfp8);
+    found[0] = units; found[1] = rounds; found[2] = over; found[3] = uncut; found[4] = turns; found[5] = used; found[6] = share;
+}
+"""
+
+
+@functools.lru_cache(maxsize=None)
+def _dealing_library():
+    compiler = shutil.which("g++") or shutil.which("clang++") or shutil.which("c++")
+    assert compiler, "no C++ compiler"
+    csrc = os.path.join(os.path.dirname(os.path.abspath(B.__file__)), "csrc")
+    with tempfile.TemporaryDirectory() as where:
+        with open(os.path.join(where, "f.cpp"), "w") as f:
+            f.write(_DEALING)
+        subprocess.run([compiler, "-O1", "-std=c++17", "-shared", "-fPIC", "-I", csrc, os.path.join(where, "f.cpp"), "-o", os.path.join(where, "f.so")], check=True)
+        return ctypes.CDLL(os.path.join(where, "f.so"))
+
+
+def dealing(dtype, mxfp8, hq, hkv, seqs, max_kv, max_q=None):
+    """How the units of sequences (new tokens, tokens in all) are dealt: "rows" (the kernel whose waves split the keys), or of the other "host" (not cut, the host says so), "whole" (not cut,
+    as the lengths turn out), "cut", or rounds and "+ nothing", "+ cut", "+ whole" for what they leave over."""
+    r = route(dtype, mxfp8, hq, hkv, len(seqs), max_q or max(n for n, _ in seqs), max_kv)
+    if not r.chunk:
+        return "rows"
+    if r.whole:
+        return "host"
+    found = (ctypes.c_uint * 7)()
+    array = ctypes.c_int * len(seqs)
+    _dealing_library().dealing(len(seqs), array(*[n for n, _ in seqs]), array(*[k for _, k in seqs]), hkv, r.tile_shift, r.step_shift, r.workgroups, r.least, r.setup,
+                               int(mxfp8), found)
+    _, rounds, over, uncut, turns, _, _ = found
+    if not rounds:
+        return "whole" if uncut else "cut"
+    return f"{rounds} + " + ("nothing" if not over else f"{turns} whole" if uncut else "cut")
