@@ -500,7 +500,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             }
             const unsigned r = WQ * wave + l32, t = a.by_group.div(r);
             if (a.lse && hh == 0 && (int)r < rows_live)
-                a.lse[(int64_t)(seq.start + t0 + (int)t) * a.hq + head * a.group + (int)(r - t * a.group)] = l_tot == 0.f ? -INFINITY : m_run * a.scale + __logf(l_tot);
+                a.lse[(int64_t)(seq.start + t0 + (int)t) * a.hq + head * a.group + (int)(r - t * a.group)] = l_tot == 0.f ? -INFINITY : m_run * a.scale + logf(l_tot);
         } else {                                                     // [wave][dt][gg][lane] of 16 bytes: whole kilobytes
             const int64_t slot = 2 * (int64_t)home + (began ? 1 : 0);
             float* to = a.parts + slot * kChunkRows * kHeadDim + wave * (WQ * kHeadDim) + lane * 4;

@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows, unsign
                 *(four*)((__bf16*)a.out + to) = four{(__bf16)y.x, (__bf16)y.y, (__bf16)y.z, (__bf16)y.w};
             }
         }
-        if (a.lse && channel(0) == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + __logf(L);
+        if (a.lse && channel(0) == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
     }
 }
 
