@@ -47,7 +47,7 @@ enum {
     CP_ERR_NULL = -1,        /* a required pointer is NULL */
     CP_ERR_SHAPE = -2,       /* non-positive size, n_q_heads % n_kv_heads != 0, block_size does not divide segment_size */
     CP_ERR_UNSUPPORTED = -3, /* head_dim != 128, unknown dtype, softmax_domain or cache_format, n2 > 8192, list longer than the API allows,
-                                bf16 estimate with batch * n_q_heads > 65535, sizes of the cache beyond the limits named below */
+                                bf16 estimate with batch * n_q_heads > 65535, sizes of the cache beyond the limits named there */
     CP_ERR_ALIGN = -4,       /* a pointer is not 16-byte aligned or a stride is not a multiple of 8 elements */
     CP_ERR_WORKSPACE = -5,   /* workspace smaller than critiprefill_workspace_bytes(), critiprefill_paged_workspace_bytes() */
     CP_ERR_LAUNCH = -6       /* the HIP runtime refused a launch */
@@ -171,9 +171,11 @@ typedef struct critiprefill_cache_params {
     int32_t tokens;                           /* rows of the tensors */
     int32_t cache_format;                     /* CP_CACHE_* */
     int32_t page_size, n_pages;               /* page_size: a power of two, 16 or more; n_pages * page_size < 2^31 */
-    int32_t n_seqs, max_pages;                /* paged_attn: sequences, and the pitch of the page table */
+    int32_t n_seqs, max_pages;                /* paged_attn: sequences, and the pitch of the page table; max_pages * page_size < 2^30, and all tiles of new tokens
+                                                 (16 rows or more each) by the steps over max_pages * page_size keys (64 or more each) by n_kv_heads < 2^31 */
     int32_t max_q_len, max_kv_len;            /* paged_attn: new tokens, and tokens in all, that a sequence has at most, 0: not known (tokens, and
-                                                 max_pages * page_size).  They choose the kernel and the way the work is cut; more are right too */
+                                                 max_pages * page_size).  They choose the kernel and the way the work is cut; more are right too.  A table much
+                                                 wider than the sequences are long hides that these are short: 32 single tokens of 760 keys 26 us, with max_kv_len 20 */
     int32_t rotary_dim, rotary_interleaved;   /* norm_rope: channels that turn (0 .. 128, a multiple of 16), and how they pair */
     float norm_eps, attn_scale;               /* attn_scale: 0 -> 1/sqrt(head_dim) */
     int64_t q_stride[2], k_stride[2], v_stride[2]; /* token, head.  cache_read: k_stride, v_stride are the outputs' */
@@ -202,7 +204,7 @@ int critiprefill_cache_read(const critiprefill_cache_params *p, const int32_t *s
                             const uint8_t *v_scale, void *k, void *v, void *hip_stream);
 
 /* Bytes of scratch critiprefill_paged_attn needs: parts of results that several workgroups work on.  It depends on heads, dtype, cache_format and max_q_len
- * (tokens where that is 0) alone, not on lengths.  Contents do not matter before a call; calls that may overlap need one each. */
+ * (tokens where that is 0) alone, not on lengths.  Contents do not matter before a call; calls that may overlap need one each.  0 for a block that paged_attn refuses. */
 size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
 
 /*
@@ -214,6 +216,8 @@ size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
  * Whatever they hold, nothing outside the tensors is touched: rows and lengths are cut to the tensors' sizes, tokens of a page outside the pool are seen
  * by no row, and with a q_start that does not ascend nothing is done.  Rows of no sequence are not written.  out must not overlap q or the cache.  At most 64
  * query heads for a KV head.
+ * Logits, maxima and sums are fp32.  With dtype bf16 a weight is rounded to bf16 for its product with V (not for the sum of weights), and out once at the end.
+ * The same call on the same contents gives the same bits.  Where a row's sum over keys is cut depends on the other sequences of the call, max_q_len and max_kv_len, and so do its last bits.
  */
 int critiprefill_paged_attn(const critiprefill_cache_params *p, const void *q, const void *k_cache, const void *v_cache, const uint8_t *k_scale,
                             const uint8_t *v_scale, const int32_t *page_table, const int32_t *q_start, const int32_t *kv_len, void *out, float *lse,

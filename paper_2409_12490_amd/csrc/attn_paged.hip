@@ -15,8 +15,8 @@
 // of the SIMD works meanwhile (both a whole step ahead in registers of their own: as fast for one token, 20 % slower for 32 rows, where a second wave then has no room).
 // 8-bit keys and values become bf16 (exact: their scales are powers of two) or fp32 in registers.
 //
-// What bounds it, 32/8 heads: the memory, with all of K and V read once: one token after 131071 in bf16 95 us and 5.6 TB/s (a copy moves 4.9, half of it written), 48 single tokens
-// of up to 32769 each over 8-bit pages 75 us and 5.2 TB/s; MFMA and vector units are busy for a twentieth of that.  After 1999 tokens it is latency: 7 us, of which an empty launch
+// What bounds it, 32/8 heads: the memory, with all of K and V read once: one token after 131071 in bf16 95 us and 5.7 TB/s (reads past the caches reach 7.0), 48 single tokens
+// of up to 32769 each over 8-bit pages 74 us and 5.3 TB/s; MFMA and vector units are busy for a twentieth of that.  After 1999 tokens it is latency: 7 us, of which an empty launch
 // takes 3, then lengths, page table, keys and the join's launch one after another (4 more).  fp32, 4/2 heads: the matrix units (16x16x4 fp32 MFMAs, 154 TFLOP/s in a large product)
 // for two thirds of 20 x 200 tokens after 8000 (684 us); of 3 x up to 200 after 3000 (32 us) for 15, the rest are the beginnings and ends of runs of eight steps.  Two workgroups of
 // 32 fp32 rows to a compute unit, within 256 registers: no faster for 20 x 200 after 8000, up to 40 % slower for less.
@@ -474,6 +474,7 @@ int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        //
 PagedRoute paged_route(const CacheShape& sh) {
     PagedRoute r;
     const bool f32 = sh.dtype == 0;
+    // All of these lines were measured at 32/8 heads (fp32: 4/2), and go by rows, units and keys alone.
     // Tiles of 256 rows pay from more than 16 rows on, 8-bit pages from 32; up to 32 rows not for few units and keys (and not where a token alone has more than 16).  us, 32/8 heads, waves that split the keys / tiles of 256 rows:
     // 1 x 4 tokens of 2000 10.8 / 16.1, of 60000 44 / 56, 8 x 4 of 2000 23.6 / 26.3, of 16000 102 / 105; 1 x 8 of 2000 14.1 / 16.3, of 16000 24.6 / 29.1, of 60000 78 / 57, 8 x 8 of 2000
     // 32.5 / 26.3, of 16000 127 / 104; 8 bits: 1 x 8 of 16000 19.9 / 28.9, 8 x 8 55 / 106, 8 x 16 114 / 112.

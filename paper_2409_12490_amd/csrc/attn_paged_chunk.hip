@@ -12,7 +12,8 @@
 //
 // What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
 // library reaches 1.24; the MFMA pipe is busy for 55 % of the launch, the vector units for 43 %, 96 % of the reads come from L2.  Over 8-bit pages 3.38 ms: 14 % more vector
-// instructions.  512 after 16384: 139 us, 1.01 PFLOP/s, with four parts to a unit and 10 us to join them.
+// instructions.  512 after 16384: 138 us, 1.01 PFLOP/s, 64 units in 314 pieces and 10 us to join them.  Mixed batches and short follow-ups: the beginnings and ends of pieces, 5 steps' worth each
+// (12 sequences of 1 to 300 new tokens, 32/4 heads, 8 bits: 388 pieces for 156 units, 98 us and 9.5 to join; 1 x 64 of 2000 21 us in all, MFMA busy for a twentieth of it).
 // Not kept: 8-bit bytes by way of LDS, three tiles in flight (no faster at 109 us for 8 x 4 tokens after 16000, 4 % slower in mixed batches); conversion that writes to LDS without bank
 // conflicts at the price of selections (257 conflict cycles a step less, 3 % slower); the places of the key loops within 32 bytes (1 % between the best and the worst).
 #include "attn_bf16.h"
@@ -41,6 +42,7 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
 
 // All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
 // around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
+// What is left of it: all forms keep 174 to 292 times a scalar in a lane of a vector register, and that over 8-bit pages of 16 one vector register in memory (8 bytes of scratch).
 // RUNS: pages that a tile of 64 keys lies in: 1 (pages of 64 and more), 2 or 4 (of 16).  Four look-ups and what follows from them are 80 scalar instructions a step more than one:
 // 8192 new tokens of 32768 (32/8 heads), pages of 64, 3571 us with four and 3310 with one.
 template <bool MX, int RUNS, bool ROTATED>

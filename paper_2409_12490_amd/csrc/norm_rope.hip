@@ -4,7 +4,7 @@
 //   (y1, y2) -> (y1 cos a - y2 sin a, y2 cos a + y1 sin a),  a = position * inv_freq[c],  c < rotary / 2, of channels (c, c + rotary / 2) or (2c, 2c + 1)
 //   e4m3 rows: of each 32 channels the smallest 2^e with max |y| <= 448 * 2^e; y / 2^e rounded to nearest even
 //
-// Everything is bound by memory: 10 operations an element.  16384 tokens of 32/8 heads (336 MB) 61 to 64 us, 5.3 to 5.5 TB/s (a large copy 4.9); 65536 tokens' K and V
+// Everything is bound by memory: 10 operations an element.  16384 tokens of 32/8 heads (336 MB) 61 to 64 us, 5.3 to 5.5 TB/s (a large copy past the caches 5.9); 65536 tokens' K and V
 // into 8-bit pages (407 MB) 83, 20001 back (62 MB) 11.5; 64 tokens into 8-bit pages 3.4 us in a graph, a launch.
 // Sixteen lanes take a head of a token, 8 neighbouring channels each (16 bytes of bf16), so that
 // sums over a head and maxima over 32 channels are DPP exchanges.  A wave stays with one token: its 64 lanes work out the token's angles once, one

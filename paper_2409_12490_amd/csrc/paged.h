@@ -5,8 +5,8 @@
 // took four times as long as the others).  All steps of all units laid end to end, units in order of sequence, KV head, tile, are dealt to the
 // workgroups in equal runs: no workgroup has more than its share, whatever the lengths, and the device alone reads the lengths.  A workgroup
 // finishes units that lie in its run; of one that began before it or goes on behind it, it leaves (sum, maximum, weighted V) in the workspace, and
-// a second kernel adds these up in order.  (The last workgroup of a unit to arrive adding them up instead, with a ticket and fences between the XCDs' L2: 39 us where the two
-// kernels take 11, 350 for 101.)
+// a second kernel adds these up in order.  (The last workgroup of a unit to arrive adding them up instead, with a ticket and fences that write the XCDs' L2 back: 39 us where the two
+// kernels take 11, 350 for 101.  Parts that go past L2, without such fences: not tried.)
 //
 // Where all sequences are alike and there are units for every workgroup, workgroups first take whole units, round by round to and fro, and share what
 // the rounds leave over as above: the 32 workgroups of an XCD then read the keys of one head at the same time, from its L2 (runs of equal length begin anywhere in
