@@ -13,7 +13,7 @@
  *
  *   critiprefill_norm_rope         norms of queries and keys for each head and the position rotation, in one pass
  *   critiprefill_norm_rope_write   the same, with keys and values going straight into the cache
- *   critiprefill_cache_write / critiprefill_cache_read   keys and values into the cache and back, as they are or in 8 bits
+ *   critiprefill_cache_write / critiprefill_cache_read   keys and values into the cache and back, as they are, in 8 or in 4 bits
  *   critiprefill_paged_attn        attention of each sequence's new tokens, one or many, over its pages
  *
  * Conventions common to all entry points
@@ -152,10 +152,14 @@ int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, 
  * The cache
  * ---------
  * K and V of all sequences lie in pages of page_size tokens: k_cache and v_cache are [n_pages, n_kv_heads, page_size, row],
- * contiguous, so that a head's tokens of a page are one piece.  A row is 128 elements of `dtype` (CP_CACHE_PLAIN), or 128
- * OCP e4m3 elements with one power of two for each 32 channels (CP_CACHE_MXFP8): the bytes e of k_scale and v_scale, [n_pages,
+ * contiguous, so that a head's tokens of a page are one piece.  A row is 128 elements of `dtype` (CP_CACHE_PLAIN), or (CP_CACHE_MXFP8) 128
+ * OCP e4m3 elements with one power of two for each 32 channels: the bytes e of k_scale and v_scale, [n_pages,
  * n_kv_heads, page_size, 4], stand for 2^(e - 127); 2^e is the smallest with max |x| <= 448 * 2^e, e in 1 .. 254.  Values that are not
  * finite have no part in the maximum and are held as NaN.  With CP_CACHE_PLAIN the scales are not read and may be NULL.
+ * CP_CACHE_MXFP4: a row is 128 OCP e2m1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), 64 bytes, the even channel of two in the lower half of their byte, and
+ * scales as above: 2^e is the smallest with max |x| <= 7 * 2^e, e in 2 .. 252.  An element is rounded to the nearest, ties to the even code; what lies above 6 is off by a unit at
+ * most, no more than rounding costs between 4 and 6, where the next scale's steps would be two units.  (e == 252 alone holds larger maxima, as 6 * 2^125.)  32 channels that
+ * are not all finite have e = 255 and are NaN together; that is what e = 255 stands for under any elements.
  * A token's place is its slot, page * page_size + offset; a token whose slot is not in 0 .. n_pages * page_size - 1 has no place: it is
  * not written, and read as zeros.  Two tokens of one written call must not have the same slot: what it then holds is made of both.
  *
@@ -163,7 +167,7 @@ int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, 
  * parameter block (elements, multiples of 8; channels lie together), so that the parts of a joint projection are read where they are.
  * Written tensors: strides of at least 128 that leave every row its own place.  tokens == 0 (and n_seqs == 0) is no error: nothing is launched or looked at.
  */
-enum { CP_CACHE_PLAIN = 0, CP_CACHE_MXFP8 = 1 };
+enum { CP_CACHE_PLAIN = 0, CP_CACHE_MXFP8 = 1, CP_CACHE_MXFP4 = 4 };     /* 2 and 3 are not formats */
 
 typedef struct critiprefill_cache_params {
     int32_t n_q_heads, n_kv_heads, head_dim;  /* head_dim must be 128; n_q_heads is not read by cache_write and cache_read */
@@ -192,7 +196,7 @@ typedef struct critiprefill_cache_params {
 int critiprefill_norm_rope(const critiprefill_cache_params *p, const void *q, const void *k, const void *q_weight, const void *k_weight,
                            const double *inv_freq, const int32_t *positions, void *q_out, void *k_out, void *hip_stream);
 
-/* The same for q; k goes, and v as it is, to slots[token] of the cache (int32[tokens]).  With CP_CACHE_MXFP8 k is quantised from fp32. */
+/* The same for q; k goes, and v as it is, to slots[token] of the cache (int32[tokens]).  With CP_CACHE_MXFP8 and CP_CACHE_MXFP4 k is quantised from fp32. */
 int critiprefill_norm_rope_write(const critiprefill_cache_params *p, const void *q, const void *k, const void *v, const void *q_weight, const void *k_weight,
                                  const double *inv_freq, const int32_t *positions, const int32_t *slots, void *q_out, void *k_cache, void *v_cache,
                                  uint8_t *k_scale, uint8_t *v_scale, void *hip_stream);

@@ -1,4 +1,4 @@
-"""fp64 oracle of the operators around the paged cache: head norms with the position rotation, the 8-bit format, attention of new tokens.
+"""fp64 oracle of the operators around the paged cache: head norms with the position rotation, the formats of 8 and 4 bits, attention of new tokens.
 
 Written from the formulas, in numpy, without the library's code.  Functions return the result and, where it helps a test to derive how far an
 fp32 evaluation may be off, the sizes of the terms it is made of.
@@ -69,6 +69,46 @@ def mx_values(codes, e):
     mag = np.where((codes & 127) == 127, np.nan, _GRID[np.minimum(codes & 127, 126)])
     v = np.where(codes & 128, -mag, mag)
     return (v.reshape(*e.shape, 32) * 2.0 ** (np.asarray(e, dtype=np.float64) - 127.0)[..., None]).reshape(codes.shape)
+
+
+_LEVELS4 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx4_scale(x):
+    """Bytes e [..., 4]: 2^(e - 127) is the smallest power of two with max |x| <= 7 * 2^(e - 127) over 32 channels, 2 <= e <= 252; 255 where any of them is not finite."""
+    a = np.abs(np.asarray(x, dtype=np.float64)).reshape(*x.shape[:-1], 4, 32)
+    finite = np.isfinite(a).all(-1)
+    most = np.where(finite[..., None], a, 0.0).max(-1)
+    e = np.full(most.shape, 2, dtype=np.int64)
+    nz = most > 0
+    k = np.floor(np.log2(most[nz])).astype(np.int64) - 4    # surely too small; then up until it fits
+    for _ in range(6):
+        k = np.where(most[nz] > 7.0 * 2.0 ** k, k + 1, k)
+    e[nz] = np.clip(k + 127, 2, 252)
+    return np.where(finite, e, 255).astype(np.uint8)
+
+
+def mx4_quantise(x):
+    """Bytes (uint8 [..., 64], the even channel in the lower half) and scale bytes of x: the nearest of e2m1's values, ties to the even code; 32 channels that are not all finite are zeros."""
+    x = np.asarray(x, dtype=np.float64)
+    e = mx4_scale(x)
+    odd = e == 255
+    units = np.where(odd[..., None], 0.0, x.reshape(*e.shape, 32)) * 2.0 ** (127.0 - np.where(odd, 127, e).astype(np.float64))[..., None]
+    a = np.minimum(np.abs(units), 6.0)
+    hi = np.searchsorted(_LEVELS4, a)                       # the first code at or above
+    lo = np.maximum(hi - 1, 0)
+    up, down = _LEVELS4[hi] - a, a - _LEVELS4[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo) | np.where(np.signbit(units), 8, 0)
+    code = code.reshape(x.shape)
+    return (code[..., ::2] | code[..., 1::2] << 4).astype(np.uint8), e
+
+
+def mx4_values(held, e):
+    held = np.asarray(held).astype(np.int64)
+    code = np.stack([held & 15, held >> 4], -1).reshape(*e.shape, 32)
+    v = np.where(code & 8, -1.0, 1.0) * _LEVELS4[code & 7]
+    scale = np.where(np.asarray(e) == 255, np.nan, 2.0 ** (np.asarray(e, dtype=np.float64) - 127.0))
+    return (v * scale[..., None]).reshape(*e.shape[:-1], 128)
 
 
 def paged_attention(q, held_k, held_v, page_size, table, q_start, kv_len, scale):

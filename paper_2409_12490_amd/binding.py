@@ -15,7 +15,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcritipr
 _lib = None
 
 CP_DTYPE_FP32, CP_DTYPE_BF16 = 0, 1
-CP_CACHE_PLAIN, CP_CACHE_MXFP8 = 0, 1
+CP_CACHE_PLAIN, CP_CACHE_MXFP8, CP_CACHE_MXFP4 = 0, 1, 4
 EXPORTS = ["critiprefill_list_len", "critiprefill_workspace_bytes", "critiprefill_estimate",
            "critiprefill_estimate_static", "critiprefill_select", "critiprefill_sparse_attn", "critiprefill_select_shared",
            "critiprefill_sparse_attn_shared", "critiprefill_dense_causal_attn",
@@ -191,12 +191,14 @@ def _dtype_code(dtype: torch.dtype) -> int:
 
 def make_cache_params(n_q_heads: int, n_kv_heads: int, dtype: torch.dtype, *, q=None, k=None, v=None, out=None, k_out=None, k_cache=None,
                       mxfp8: bool = False, page_table=None, max_q_len: int = 0, max_kv_len: int = 0, rotary_dim: int = 0, interleaved: bool = False,
-                      norm_eps: float = 0.0, attn_scale: float = 0.0) -> CacheParams:
+                      norm_eps: float = 0.0, attn_scale: float = 0.0, mxfp4: bool = False) -> CacheParams:
     """Fill the parameter block from the tensors of a call: q, k, v, out (q_out or the attention's) and k_out are [tokens, heads, 128], each with
-    strides of its own; k_cache [n_pages, n_kv_heads, page_size, 128] says the pool's size, page_table [n_seqs, max_pages] the sequences."""
+    strides of its own; k_cache [n_pages, n_kv_heads, page_size, 128], with mxfp4 64 bytes a row, says the pool's size, page_table [n_seqs, max_pages] the sequences."""
     p = CacheParams()
     p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype = n_q_heads, n_kv_heads, 128, _dtype_code(dtype)
-    p.cache_format = CP_CACHE_MXFP8 if mxfp8 else CP_CACHE_PLAIN
+    if mxfp8 and mxfp4:
+        raise ValueError("mxfp8 and mxfp4: a cache has one format")
+    p.cache_format = CP_CACHE_MXFP8 if mxfp8 else CP_CACHE_MXFP4 if mxfp4 else CP_CACHE_PLAIN
     tokens = None
     for t, heads, stride, name in ((q, n_q_heads, p.q_stride, "q"), (k, n_kv_heads, p.k_stride, "k"), (v, n_kv_heads, p.v_stride, "v"),
                                    (out, n_q_heads, p.o_stride, "out"), (k_out, n_kv_heads, p.ko_stride, "k_out")):
@@ -214,9 +216,10 @@ def make_cache_params(n_q_heads: int, n_kv_heads: int, dtype: torch.dtype, *, q=
             stride[i] = t.stride(i) if t.shape[i] > 1 else max(128, heads * 128 if i == 0 else 128)
     p.tokens = tokens or 0
     if k_cache is not None:
-        if k_cache.dim() != 4 or k_cache.shape[1] != n_kv_heads or k_cache.shape[3] != 128 or not k_cache.is_contiguous():
-            raise ValueError(f"k_cache: expected a contiguous [n_pages, {n_kv_heads}, page_size, 128], got {tuple(k_cache.shape)}")
-        if k_cache.dtype != (torch.uint8 if mxfp8 else dtype):
+        row = 64 if mxfp4 else 128
+        if k_cache.dim() != 4 or k_cache.shape[1] != n_kv_heads or k_cache.shape[3] != row or not k_cache.is_contiguous():
+            raise ValueError(f"k_cache: expected a contiguous [n_pages, {n_kv_heads}, page_size, {row}], got {tuple(k_cache.shape)}")
+        if k_cache.dtype != (torch.uint8 if mxfp8 or mxfp4 else dtype):
             raise TypeError(f"k_cache: {k_cache.dtype}")
         p.n_pages, p.page_size = k_cache.shape[0], k_cache.shape[2]
     if page_table is not None:
@@ -256,13 +259,14 @@ def _few(tokens, *tensors):
 def _pool(p, k_cache, v_cache, k_scale, v_scale):
     """The addresses of the pool's four tensors, which the library takes to be as large as n_pages says."""
     rows = p.n_pages * p.n_kv_heads * p.page_size
-    size, mxfp8 = rows * 128, p.cache_format == CP_CACHE_MXFP8
-    dtype = torch.uint8 if mxfp8 else _TYPES.get(p.dtype)
+    scaled = p.cache_format != CP_CACHE_PLAIN
+    size = rows * (64 if p.cache_format == CP_CACHE_MXFP4 else 128)
+    dtype = torch.uint8 if scaled else _TYPES.get(p.dtype)
     if k_cache.dtype is not dtype or k_cache.numel() < size or not k_cache.is_contiguous():
         _refuse(k_cache, dtype, size)
     if v_cache.dtype is not dtype or v_cache.numel() < size or not v_cache.is_contiguous():
         _refuse(v_cache, dtype, size)
-    if not mxfp8 or k_scale is None or v_scale is None:                  # not read, or refused by the library
+    if not scaled or k_scale is None or v_scale is None:                  # not read, or refused by the library
         return k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale)
     if k_scale.dtype is not torch.uint8 or k_scale.numel() < 4 * rows or not k_scale.is_contiguous():
         _refuse(k_scale, torch.uint8, 4 * rows)
@@ -372,11 +376,13 @@ def alloc_workspace(p: Params, device="cuda") -> torch.Tensor:
     return torch.empty((max(16, critiprefill_workspace_bytes(p)),), dtype=torch.uint8, device=device)
 
 
-def alloc_cache(n_pages: int, n_kv_heads: int, page_size: int, dtype: torch.dtype = torch.bfloat16, mxfp8: bool = False, device="cuda"):
-    """(k_cache, v_cache, k_scale, v_scale) of a pool of pages; the scales are None without mxfp8."""
-    shape = (n_pages, n_kv_heads, page_size)
-    caches = [torch.empty((*shape, 128), dtype=torch.uint8 if mxfp8 else dtype, device=device) for _ in range(2)]
-    scales = [torch.empty((*shape, 4), dtype=torch.uint8, device=device) if mxfp8 else None for _ in range(2)]
+def alloc_cache(n_pages: int, n_kv_heads: int, page_size: int, dtype: torch.dtype = torch.bfloat16, mxfp8: bool = False, device="cuda", mxfp4: bool = False):
+    """(k_cache, v_cache, k_scale, v_scale) of a pool of pages; the scales are None without mxfp8 and mxfp4."""
+    if mxfp8 and mxfp4:
+        raise ValueError("mxfp8 and mxfp4: a cache has one format")
+    shape, scaled = (n_pages, n_kv_heads, page_size), mxfp8 or mxfp4
+    caches = [torch.empty((*shape, 64 if mxfp4 else 128), dtype=torch.uint8 if scaled else dtype, device=device) for _ in range(2)]
+    scales = [torch.empty((*shape, 4), dtype=torch.uint8, device=device) if scaled else None for _ in range(2)]
     return (*caches, *scales)
 
 

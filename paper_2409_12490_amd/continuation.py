@@ -1,9 +1,9 @@
 """A sequence past its prefill: the operators around the paged cache, together, on one Llama3-8B-shaped attention layer.
 
-    python -m paper_2409_12490_amd.continuation [--prompt 16384] [--follow 700] [--steps 16] [--plain]
+    python -m paper_2409_12490_amd.continuation [--prompt 16384] [--follow 700] [--steps 16] [--plain | --four]
 
 A prompt's queries and keys get their norms and positions (critiprefill_norm_rope), go through the pruned prefill (estimate, select, block-sparse attention),
-and its keys and values into the pages of a cache, in 8 bits unless --plain (critiprefill_cache_write).  A follow-up of some hundred tokens goes on from there
+and its keys and values into the pages of a cache, in 8 bits unless --plain or --four (critiprefill_cache_write).  A follow-up of some hundred tokens goes on from there
 as a chunk, then single tokens: norms, positions and the write in one call (critiprefill_norm_rope_write), then attention over the pages
 (critiprefill_paged_attn).  The single step is captured into a graph that follows the lengths on the device.  Prints the time of each part, and how far the
 rows of the follow-up and of the captured steps over the cache are from the same rows of dense attention over the keys and values as they were.
@@ -23,11 +23,12 @@ SEGMENT, BLOCK, BUDGET, LOCAL = 512, 64, 32, 1
 class Layer:
     """One sequence's cache of one layer, and what its calls need beside the tensors."""
 
-    def __init__(self, longest: int, mxfp8: bool = True, device: str = "cuda", seed: int = 0):
-        self.device, self.mxfp8, self.held = device, mxfp8, 0
+    def __init__(self, longest: int, mxfp8: bool = True, device: str = "cuda", seed: int = 0, mxfp4: bool = False):
+        self.device, self.held = device, 0
+        self.format = {"mxfp4": True} if mxfp4 else {"mxfp8": mxfp8}
         pages = -(-longest // PAGE)
         gen = torch.Generator().manual_seed(seed)
-        self.cache = B.alloc_cache(pages, HKV, PAGE, mxfp8=mxfp8, device=device)
+        self.cache = B.alloc_cache(pages, HKV, PAGE, device=device, **self.format)
         self.table = torch.randperm(pages, generator=gen).int().view(1, pages).to(device)          # any pages, in any order
         self.freq = B.rotary_frequencies(D, device=device)
         self.weights = [(1 + 0.1 * torch.randn(D, generator=gen)).bfloat16().to(device) for _ in range(2)]
@@ -52,7 +53,7 @@ class Layer:
         B.critiprefill_estimate(a, heads(qr), heads(kr), None, scores, B.alloc_workspace(a, self.device))
         B.critiprefill_select(a, scores, idx, cnt)
         B.critiprefill_sparse_attn(a, heads(qr), heads(kr), heads(vc), idx, cnt, heads(out))
-        p = B.make_cache_params(HQ, HKV, q.dtype, k=kr, v=v, k_cache=self.cache[0], mxfp8=self.mxfp8)
+        p = B.make_cache_params(HQ, HKV, q.dtype, k=kr, v=v, k_cache=self.cache[0], **self.format)
         B.critiprefill_cache_write(p, kr, v, self.slots(0, n), *self.cache)
         self.held = n
         return out, kr
@@ -62,8 +63,8 @@ class Layer:
         n = qkv.shape[0]
         q, k, v = qkv.split([HQ, HKV, HKV], 1)
         s = {"q": q, "k": k, "v": v, "qr": torch.empty((n, HQ, D), dtype=q.dtype, device=self.device), "out": torch.empty((n, HQ, D), dtype=q.dtype, device=self.device)}
-        s["p"] = B.make_cache_params(HQ, HKV, q.dtype, q=q, k=k, v=v, out=s["qr"], k_cache=self.cache[0], mxfp8=self.mxfp8, rotary_dim=D, norm_eps=1e-5)
-        s["pa"] = B.make_cache_params(HQ, HKV, q.dtype, q=s["qr"], out=s["out"], k_cache=self.cache[0], mxfp8=self.mxfp8, page_table=self.table, max_q_len=n)
+        s["p"] = B.make_cache_params(HQ, HKV, q.dtype, q=q, k=k, v=v, out=s["qr"], k_cache=self.cache[0], rotary_dim=D, norm_eps=1e-5, **self.format)
+        s["pa"] = B.make_cache_params(HQ, HKV, q.dtype, q=s["qr"], out=s["out"], k_cache=self.cache[0], page_table=self.table, max_q_len=n, **self.format)
         s["workspace"] = B.alloc_paged_workspace(s["pa"], self.device)
         s["start"] = torch.tensor([0, n], dtype=torch.int32, device=self.device)
         s["pos"], s["slots"], s["kv"] = (torch.zeros(c, dtype=torch.int32, device=self.device) for c in (n, n, 1))
@@ -141,14 +142,14 @@ def _dense_rows(layer: Layer, kr: torch.Tensor, qkv: torch.Tensor, follow: torch
     return out[n:]
 
 
-def run(prompt: int = 16384, follow: int = 700, steps: int = 16, mxfp8: bool = True, seed: int = 0, verbose: bool = True) -> dict:
+def run(prompt: int = 16384, follow: int = 700, steps: int = 16, mxfp8: bool = True, seed: int = 0, verbose: bool = True, mxfp4: bool = False) -> dict:
     gen = torch.Generator(device="cuda").manual_seed(seed)
 
     def projected(n):
         x = torch.randn((n, HQ + 2 * HKV, D), generator=gen, device="cuda")
         return (x + 0.1 * torch.randn((n, HQ + 2 * HKV, D), generator=gen, device="cuda").cumsum(0)).bfloat16()
 
-    layer = Layer(prompt + follow + steps + 1, mxfp8, seed=seed)
+    layer = Layer(prompt + follow + steps + 1, mxfp8, seed=seed, mxfp4=mxfp4)
     qkv, more = projected(prompt), projected(follow)
     prefill_us, (_, kr) = _timed(lambda: layer.prefill(qkv))
 
@@ -165,7 +166,7 @@ def run(prompt: int = 16384, follow: int = 700, steps: int = 16, mxfp8: bool = T
              "finite": bool(torch.isfinite(outs).all() and torch.isfinite(out).all())}
     if verbose:
         print(f"prompt of {prompt}: norms, positions, pruned prefill and cache {prefill_us:.0f} us")
-        print(f"follow-up of {follow} over the cache ({'8 bits' if mxfp8 else 'bf16'}): {chunk_us:.0f} us, {off:.2e} from dense attention over what was cached")
+        print(f"follow-up of {follow} over the cache ({'4 bits' if mxfp4 else '8 bits' if mxfp8 else 'bf16'}): {chunk_us:.0f} us, {off:.2e} from dense attention over what was cached")
         print(f"single tokens, captured: {found['step_us']:.1f} us each, {max(step_off):.2e} at most from dense attention; {layer.held} tokens held")
     return found
 
@@ -175,6 +176,8 @@ if __name__ == "__main__":
     ap.add_argument("--prompt", type=int, default=16384)
     ap.add_argument("--follow", type=int, default=700)
     ap.add_argument("--steps", type=int, default=16)
-    ap.add_argument("--plain", action="store_true", help="pages of bf16")
+    pages = ap.add_mutually_exclusive_group()
+    pages.add_argument("--plain", action="store_true", help="pages of bf16")
+    pages.add_argument("--four", action="store_true", help="pages of 4 bits")
     args = ap.parse_args()
-    run(args.prompt, args.follow, args.steps, not args.plain)
+    run(args.prompt, args.follow, args.steps, not args.plain, mxfp4=args.four)

@@ -7,7 +7,7 @@
 // four pages, looked up by scalar loads a step ahead (pages are whole multiples of 16 tokens, so the rows of one load lie together); rows past the sequence's end lie in
 // its last page and may hold anything, so rows of V that no row sees are zeroed in LDS; the row sum adds P before it is rounded, since the log-sum-exp is an
 // output in its own right here (32 additions a step for 16 dot products).
-// 8-bit pages: a thread takes 16 channels of a row of K and of V into registers, a step ahead, and writes them to LDS as bf16 (exact: the scales are powers of two).
+// Pages of 8 and 4 bits: a thread takes 16 channels of a row of K and of V into registers, a step ahead, and writes them to LDS as bf16 (exact: the scales are powers of two).
 // Every wave converts an eighth of a tile, where conversion at the reads from LDS would have each wave convert all of it.
 //
 // What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
@@ -20,9 +20,12 @@
 #include "paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cp {
 namespace {
+
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 
 constexpr int kChunkRows = 256, WQ = 32, TK = 64, NBUF = 4;
 constexpr int kTileBytes = TK * 256;
@@ -40,13 +43,22 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
     return r;
 }
 
+// half h of 16 channels as a thread has them of a row, to bf16: e4m3, e2m1 (a scale of 255 makes them NaN)
+__device__ __forceinline__ u32x4 widen_half(u32x4 x, int h, float scale) { return widen8(x[2 * h], x[2 * h + 1], scale); }
+__device__ __forceinline__ u32x4 widen_half(u32x2 x, int h, float scale) {
+    return u32x4{packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 0)), packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 1)),
+                 packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 2)), packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 3))};
+}
+
 // All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
 // around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
 // What is left of it: all forms keep 174 to 292 times a scalar in a lane of a vector register, and that over 8-bit pages of 16 one vector register in memory (8 bytes of scratch).
 // RUNS: pages that a tile of 64 keys lies in: 1 (pages of 64 and more), 2 or 4 (of 16).  Four look-ups and what follows from them are 80 scalar instructions a step more than one:
 // 8192 new tokens of 32768 (32/8 heads), pages of 64, 3571 us with four and 3310 with one.
-template <bool MX, int RUNS, bool ROTATED>
+template <int HELD, int RUNS, bool ROTATED>
 __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
+    constexpr bool MX = HELD != HELD_PLAIN, MX4 = HELD == HELD_MXFP4;
+    constexpr int kRowBytes = row_bytes(HELD, 2);
     const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
     if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
     __syncthreads();
@@ -65,7 +77,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             v_addr[dt] = lds0 + kVOff + (4 * hh + (i16 >> 2)) * 256 + ((((unsigned)(dt ^ (i16 >> 2)) << 2) + 2 * gbit + ((i16 & 3) >> 1)) << 4) + (i16 & 1) * 8;
         // copies: wave w fills rows 4 w .. 4 w + 3 and 32 + 4 w .. of a tile; physical chunk pch of row r4
         const unsigned lane_k = (unsigned)r4 * 256 + (unsigned)(pch ^ ((4 * wave + r4) & 15)) * 16, lane_v = (unsigned)r4 * 256 + (unsigned)(pch ^ (4 * r4)) * 16;
-        // 8-bit: thread tid has 16 channels 16 * (tid & 7) of row tid >> 3
+        // 8 and 4 bits: thread tid has 16 channels 16 * (tid & 7) of row tid >> 3
         const int xrow = tid >> 3, xpiece = tid & 7;
 
         const Sequence seq = run.now;
@@ -171,12 +183,13 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
                 *LDS_PTR(u32x4, at) = clean(*LDS_PTR(const u32x4, at), base(x) + row, (bits >> (row >> 4)) & 1);
             }
         };
-        // 8-bit: the tile in flight
-        u32x4 raw_k, raw_v; unsigned scale_k = 0, scale_v = 0;
+        // 8 and 4 bits: the tile in flight
+        typedef typename std::conditional<MX4, u32x2, u32x4>::type raw_row;
+        raw_row raw_k, raw_v; unsigned scale_k = 0, scale_v = 0;
         auto load_raw = [&]() __attribute__((always_inline)) {       // of the tile described last
-            const unsigned in_rows = (unsigned)lane * 16, in_scales = (unsigned)(lane >> 3) * 4 + (unsigned)((lane & 7) >> 1);   // eight rows of a wave
-            raw_k = *(const u32x4*)(uniform_ptr((const char*)a.cache.k + at[0] * 128) + in_rows);
-            raw_v = *(const u32x4*)(uniform_ptr((const char*)a.cache.v + at[0] * 128) + in_rows);
+            const unsigned in_rows = (unsigned)lane * (kRowBytes / 8), in_scales = (unsigned)(lane >> 3) * 4 + (unsigned)((lane & 7) >> 1);   // eight rows of a wave
+            raw_k = *(const raw_row*)(uniform_ptr((const char*)a.cache.k + at[0] * kRowBytes) + in_rows);
+            raw_v = *(const raw_row*)(uniform_ptr((const char*)a.cache.v + at[0] * kRowBytes) + in_rows);
             scale_k = (uniform_ptr(a.cache.ks + at[0] * 4))[in_scales];
             scale_v = (uniform_ptr(a.cache.vs + at[0] * 4))[in_scales];
         };
@@ -185,9 +198,9 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             const unsigned row = lds0 + slot * kTileBytes + xrow * 256;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                *LDS_PTR(u32x4, row + kKOff + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = widen8(raw_k[2 * h], raw_k[2 * h + 1], sk);
+                *LDS_PTR(u32x4, row + kKOff + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = widen_half(raw_k, h, sk);
             __builtin_amdgcn_sched_barrier(0);                       // registers of one at a time
-            u32x4 v2[2] = {widen8(raw_v[0], raw_v[1], sv), widen8(raw_v[2], raw_v[3], sv)};
+            u32x4 v2[2] = {widen_half(raw_v, 0, sv), widen_half(raw_v, 1, sv)};
             if (partly(x, bits)) {
                 const bool there = (bits >> (xrow >> 4)) & 1;
                 v2[0] = clean(v2[0], base(x) + xrow, there); v2[1] = clean(v2[1], base(x) + xrow, there);
@@ -368,11 +381,11 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
         const int bits0 = ok[3];
         if (MX) {
             load_raw();
-            const u32x4 k0 = raw_k, v0 = raw_v;
+            const raw_row k0 = raw_k, v0 = raw_v;
             const unsigned sk0 = scale_k, sv0 = scale_v;
             describe_first(1);
             load_raw();
-            const u32x4 k1 = raw_k, v1 = raw_v;
+            const raw_row k1 = raw_k, v1 = raw_v;
             const unsigned sk1 = scale_k, sv1 = scale_v;
             raw_k = k0; raw_v = v0; scale_k = sk0; scale_v = sv0;
             store_raw(0, bits0, 0);
@@ -462,7 +475,8 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {                       // channels 8 j + 4 hh ..
                     unsigned w[2];
-                    if (MX) {
+                    if (MX4) w[0] = w[1] = a.cache.vs[row * 4 + (j >> 2)] == 0xff ? 0x7fc07fc0u : 0u;
+                    else if (MX) {
                         const unsigned b = *(const unsigned*)((const char*)a.cache.v + row * 128 + 8 * j + 4 * hh);
                         const float scale = __uint_as_float((unsigned)a.cache.vs[row * 4 + (j >> 2)] << 23);
                         w[0] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false));
@@ -532,7 +546,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
     }
 }
 
-template <bool MX, int RUNS>
+template <int HELD, int RUNS>
 __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
@@ -542,15 +556,15 @@ __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     if (run.logical < run.used && thread_id() == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;
     const unsigned home = run.logical;
-    if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<MX, RUNS, false>(a, run, home, lds0);
-    else work<MX, RUNS, true>(a, run, home, lds0);
+    if (__builtin_amdgcn_readfirstlane(thread_id() >> 6) < 4) work<HELD, RUNS, false>(a, run, home, lds0);
+    else work<HELD, RUNS, true>(a, run, home, lds0);
 }
 
-template <bool MX, int RUNS>
+template <int HELD, int RUNS>
 hipError_t launch(const PagedArgs& a, int rows, hipStream_t st) {
-    const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<MX, RUNS>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const hipError_t e = hipFuncSetAttribute((const void*)paged_chunk_kernel<HELD, RUNS>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_chunk_kernel<MX, RUNS>), dim3(a.workgroups), dim3(512), kSmem, st, a);
+    hipLaunchKernelGGL((paged_chunk_kernel<HELD, RUNS>), dim3(a.workgroups), dim3(512), kSmem, st, a);
     if (a.whole) return hipGetLastError();
     // A workgroup of the join takes half of the channels of 32 rows, or where these are fewer workgroups than the chip has compute units a sixteenth, its waves every fourth part;
     // more rows than were said come in turn.  us of the whole call, half / sixteenth (bf16, pages of 64): 32 workgroups of the first kind (4/1 heads, 1 x 64 tokens of 20000) 47.5 / 26.6,
@@ -562,13 +576,17 @@ hipError_t launch(const PagedArgs& a, int rows, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <int HELD>
+hipError_t launch_runs(int runs, const PagedArgs& a, int rows, hipStream_t st) {
+    return runs == 1 ? launch<HELD, 1>(a, rows, st) : runs == 2 ? launch<HELD, 2>(a, rows, st) : launch<HELD, 4>(a, rows, st);
+}
+
 }  // namespace
 
 hipError_t launch_paged_chunk(const CacheShape& sh, const PagedArgs& a, hipStream_t st) {
     const int rows = std::min(sh.max_q, 1 << a.tile_shift) * sh.group;       // of a tile, as far as is known
-    if (sh.page_shift >= 6) return sh.mxfp8 ? launch<true, 1>(a, rows, st) : launch<false, 1>(a, rows, st);
-    if (sh.page_shift == 5) return sh.mxfp8 ? launch<true, 2>(a, rows, st) : launch<false, 2>(a, rows, st);
-    return sh.mxfp8 ? launch<true, 4>(a, rows, st) : launch<false, 4>(a, rows, st);
+    const int runs = sh.page_shift >= 6 ? 1 : sh.page_shift == 5 ? 2 : 4;
+    return sh.held == HELD_MXFP4 ? launch_runs<HELD_MXFP4>(runs, a, rows, st) : sh.held == HELD_MXFP8 ? launch_runs<HELD_MXFP8>(runs, a, rows, st) : launch_runs<HELD_PLAIN>(runs, a, rows, st);
 }
 
 }  // namespace cp

@@ -1,14 +1,18 @@
-// What the kernels around the paged cache share: the parameter block, where a token's row lies, the 8-bit format.
+// What the kernels around the paged cache share: the parameter block, where a token's row lies, the formats of 8 and 4 bits.
 #pragma once
 #include "kernels.h"
 
 namespace cp {
 
+// How the cache holds a row: elements of dtype, or e4m3 or e2m1 elements with a scale per 32 channels.
+enum { HELD_PLAIN = 0, HELD_MXFP8 = 1, HELD_MXFP4 = 2 };
+constexpr int row_bytes(int held, int element) { return held == HELD_MXFP4 ? kHeadDim / 2 : held == HELD_MXFP8 ? kHeadDim : kHeadDim * element; }
+
 // The parameter block of the cache operators, checked.
 struct CacheShape {
     int hq, hkv, group;                       // group = hq / hkv
     int dtype;                                // 0 fp32, 1 bf16
-    int mxfp8;                                // the cache holds e4m3 elements and a scale per 32 channels, else elements of dtype
+    int held;                                 // HELD_*
     int page, page_shift, n_pages;            // tokens of a page, a power of two of at least 16
     int tokens, n_seqs, max_pages, max_q;
     long long max_kv;
@@ -17,7 +21,8 @@ struct CacheShape {
     int64_t qs[2], ks[2], vs[2], os[2], kos[2];   // element strides: token, head
 };
 
-// A cache: K and V pages [n_pages][hkv][page][128], and with mxfp8 the scales [n_pages][hkv][page][4], one byte e for 2^(e - 127).
+// A cache: K and V pages [n_pages][hkv][page][row_bytes], and where it holds 8 or 4 bits the scales [n_pages][hkv][page][4], one byte e for 2^(e - 127).  Of e2m1 elements the even
+// channel of two is the lower half of their byte.
 struct CachePtr {
     void *k, *v;
     uint8_t *ks, *vs;

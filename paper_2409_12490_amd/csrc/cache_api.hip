@@ -24,10 +24,10 @@ int make_cache_shape(const critiprefill_cache_params* p, int uses, cp::CacheShap
     if (sh->hq > 65535 || sh->hkv > 65535) return CP_ERR_UNSUPPORTED;
     if (uses & USES_PAGES) {
         if (p->n_pages <= 0 || p->page_size <= 0) return CP_ERR_SHAPE;
-        if (p->cache_format != CP_CACHE_PLAIN && p->cache_format != CP_CACHE_MXFP8) return CP_ERR_UNSUPPORTED;
+        if (p->cache_format != CP_CACHE_PLAIN && p->cache_format != CP_CACHE_MXFP8 && p->cache_format != CP_CACHE_MXFP4) return CP_ERR_UNSUPPORTED;
         if (p->page_size < 16 || (p->page_size & (p->page_size - 1))) return CP_ERR_UNSUPPORTED;
         if ((long long)p->n_pages * p->page_size >= (1ll << 31)) return CP_ERR_UNSUPPORTED;    // a slot is an int32
-        sh->mxfp8 = p->cache_format == CP_CACHE_MXFP8;
+        sh->held = p->cache_format == CP_CACHE_MXFP4 ? cp::HELD_MXFP4 : p->cache_format == CP_CACHE_MXFP8 ? cp::HELD_MXFP8 : cp::HELD_PLAIN;
         sh->page = p->page_size; sh->n_pages = p->n_pages;
         while ((1 << sh->page_shift) < sh->page) ++sh->page_shift;
     }
@@ -73,8 +73,9 @@ int check_output(const void* p, const int64_t* stride, int tokens, int heads) {
 }
 
 int check_cache(const cp::CacheShape& sh, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs) {
-    if (!k || !v || (sh.mxfp8 && (!ks || !vs))) return CP_ERR_NULL;
-    if (!aligned16(k) || !aligned16(v) || (sh.mxfp8 && (!aligned16(ks) || !aligned16(vs)))) return CP_ERR_ALIGN;
+    const bool scaled = sh.held != cp::HELD_PLAIN;
+    if (!k || !v || (scaled && (!ks || !vs))) return CP_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || (scaled && (!aligned16(ks) || !aligned16(vs)))) return CP_ERR_ALIGN;
     return CP_OK;
 }
 

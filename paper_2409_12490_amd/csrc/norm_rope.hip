@@ -40,7 +40,7 @@ struct RopeArgs {
 };
 
 enum { TURN_NONE = 0, TURN_WHOLE = 1, TURN_HALVES = 2, TURN_PAIRS = 3 };    // WHOLE: halves of all 128 channels
-enum { TO_TENSOR = 0, TO_PLAIN = 1, TO_MXFP8 = 2 };
+enum { TO_TENSOR = 0, TO_PLAIN = 1, TO_MXFP8 = 2, TO_MXFP4 = 3 };
 
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
@@ -119,6 +119,29 @@ __device__ __forceinline__ u32x2 quantise8(float (&x)[8], int& exponent) {
         w[e] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e + 2] * scale, x[4 * e + 3] * scale, d, true);
     }
     return w;
+}
+
+// The same in e2m1, two to a byte.  The smallest 2^e with max |x| <= 7 * 2^e: what lies above the largest element, 6, becomes it and is off by a unit at most, as much as rounding costs
+// between 4 and 6; the next scale's steps there are two units.  e in 2 .. 252: half a unit is a normal number, and 6 of the largest are finite (larger maxima saturate).  e2m1 has no
+// NaN: 32 channels of which any value is not finite get the scale's, 255, and are held as NaN together.
+__device__ __forceinline__ unsigned quantise8_to_4(const float (&x)[8], int& exponent) {
+    float most = 0.f, nothing = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        most = fmaxf(most, fabsf(x[e]));
+        nothing = fmaf(x[e], 0.f, nothing);                        // NaN of what is not finite
+    }
+    most = max4(most);
+    nothing += dpp<0xB1>(nothing);
+    nothing += dpp<0x4E>(nothing);
+    const unsigned bits = __float_as_uint(most);
+    exponent = min(max((int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 2), 252);        // 7 = 1.75 * 2^2
+    if (nothing != 0.f) { exponent = 255; return 0; }
+    const float scale = __uint_as_float((unsigned)exponent << 23);
+    unsigned w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], scale, 0);                       // of x / scale, to nearest even, at most 6
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
 template <typename T, int TURN, int TO, bool STREAM>
@@ -209,6 +232,13 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
             const int64_t row = (((int64_t)(slot >> a.page_shift) * a.hkv + h) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
             if (TO == TO_PLAIN) {
                 if (kept) store8<STREAM>((T*)(kind == 1 ? a.cache.k : a.cache.v) + row * kHeadDim + 8 * c16, x);
+            } else if (TO == TO_MXFP4) {
+                int e;
+                const unsigned w = quantise8_to_4(x, e);
+                if (kept) {
+                    put<STREAM>((uint8_t*)(kind == 1 ? a.cache.k : a.cache.v) + row * (kHeadDim / 2) + 4 * c16, w);
+                    if ((c16 & 3) == 0) (kind == 1 ? a.cache.ks : a.cache.vs)[row * 4 + (c16 >> 2)] = (uint8_t)e;
+                }
             } else {
                 int e;
                 const u32x2 w = quantise8(x, e);
@@ -221,7 +251,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     }
 }
 
-template <typename T, bool MX, bool STREAM>
+template <typename T, int HELD, bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15;
     const unsigned index = blockIdx.x * 4u + wave;
@@ -238,7 +268,14 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f;                    // a token without a place in the cache
         if (held) {
-            if (MX) {
+            if (HELD == HELD_MXFP4) {
+                const unsigned w = get<STREAM, unsigned>((const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * (kHeadDim / 2) + 4 * c16);
+                const float scale = __uint_as_float((unsigned)(is_v ? a.cache.vs : a.cache.ks)[row * 4 + (c16 >> 2)] << 23);       // of 255: NaN
+                const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3)};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = y[e >> 1][e & 1];
+            } else if (HELD == HELD_MXFP8) {
                 const u32x2 w = get<STREAM, u32x2>((const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16);
                 const float scale = __uint_as_float((unsigned)(is_v ? a.cache.vs : a.cache.ks)[row * 4 + (c16 >> 2)] << 23);
 #pragma unroll
@@ -280,11 +317,24 @@ template <typename T, int TO>
 hipError_t launch_turn(const RopeArgs& a, int turn, bool stream, hipStream_t st) {
     return turn == TURN_WHOLE ? launch<T, TURN_WHOLE, TO>(a, stream, st) : turn == TURN_HALVES ? launch<T, TURN_HALVES, TO>(a, stream, st) : launch<T, TURN_PAIRS, TO>(a, stream, st);
 }
-template <typename T, bool MX>
+template <typename T, int HELD>
 hipError_t launch_read(const RopeArgs& a, bool stream, hipStream_t st) {
-    if (stream) hipLaunchKernelGGL((cache_read_kernel<T, MX, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((cache_read_kernel<T, MX, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    if (stream) hipLaunchKernelGGL((cache_read_kernel<T, HELD, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_read_kernel<T, HELD, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
     return hipGetLastError();
+}
+// a kernel for each way that the cache may hold rows
+template <typename T>
+hipError_t launch_rope_write(const RopeArgs& a, int turn, int held, bool stream, hipStream_t st) {
+    return held == HELD_MXFP4 ? launch_turn<T, TO_MXFP4>(a, turn, stream, st) : held == HELD_MXFP8 ? launch_turn<T, TO_MXFP8>(a, turn, stream, st) : launch_turn<T, TO_PLAIN>(a, turn, stream, st);
+}
+template <typename T>
+hipError_t launch_write(const RopeArgs& a, int held, bool stream, hipStream_t st) {
+    return held == HELD_MXFP4 ? launch<T, TURN_NONE, TO_MXFP4>(a, stream, st) : held == HELD_MXFP8 ? launch<T, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<T, TURN_NONE, TO_PLAIN>(a, stream, st);
+}
+template <typename T>
+hipError_t launch_back(const RopeArgs& a, int held, bool stream, hipStream_t st) {
+    return held == HELD_MXFP4 ? launch_read<T, HELD_MXFP4>(a, stream, st) : held == HELD_MXFP8 ? launch_read<T, HELD_MXFP8>(a, stream, st) : launch_read<T, HELD_PLAIN>(a, stream, st);
 }
 
 }  // namespace
@@ -292,7 +342,7 @@ hipError_t launch_read(const RopeArgs& a, bool stream, hipStream_t st) {
 // Whether a call goes past the caches: bytes read and written, `rows` of each token as elements of dtype, `held` of each in the cache.
 bool cache_call_streams(const CacheShape& sh, int rows, int held) {
     const long long e = sh.dtype == 1 ? 2 : 4;
-    return (long long)sh.tokens * kHeadDim * (rows * e + held * (sh.mxfp8 ? 1 : e)) > kStreamBytes;
+    return (long long)sh.tokens * (rows * kHeadDim * e + held * row_bytes(sh.held, (int)e)) > kStreamBytes;
 }
 
 hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight,
@@ -302,27 +352,22 @@ hipError_t launch_norm_rope(const CacheShape& sh, const void* q, const void* k, 
     a.half = sh.rotary / 2;
     const int turn = sh.interleaved ? TURN_PAIRS : (sh.rotary == kHeadDim ? TURN_WHOLE : TURN_HALVES);
     const bool stream = cache_call_streams(sh, 2 * sh.hq + 2 * sh.hkv, cache ? 2 * sh.hkv : 0);
-    if (sh.dtype == 1)
-        return !cache ? launch_turn<__bf16, TO_TENSOR>(a, turn, stream, st)
-                      : sh.mxfp8 ? launch_turn<__bf16, TO_MXFP8>(a, turn, stream, st) : launch_turn<__bf16, TO_PLAIN>(a, turn, stream, st);
-    return !cache ? launch_turn<float, TO_TENSOR>(a, turn, stream, st)
-                  : sh.mxfp8 ? launch_turn<float, TO_MXFP8>(a, turn, stream, st) : launch_turn<float, TO_PLAIN>(a, turn, stream, st);
+    if (sh.dtype == 1) return !cache ? launch_turn<__bf16, TO_TENSOR>(a, turn, stream, st) : launch_rope_write<__bf16>(a, turn, sh.held, stream, st);
+    return !cache ? launch_turn<float, TO_TENSOR>(a, turn, stream, st) : launch_rope_write<float>(a, turn, sh.held, stream, st);
 }
 
 hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v, const int32_t* slots, const CachePtr& cache, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.hq = 0; a.k = k; a.v = v; a.slots = slots;
     const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
-    if (sh.dtype == 1) return sh.mxfp8 ? launch<__bf16, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<__bf16, TURN_NONE, TO_PLAIN>(a, stream, st);
-    return sh.mxfp8 ? launch<float, TURN_NONE, TO_MXFP8>(a, stream, st) : launch<float, TURN_NONE, TO_PLAIN>(a, stream, st);
+    return sh.dtype == 1 ? launch_write<__bf16>(a, sh.held, stream, st) : launch_write<float>(a, sh.held, stream, st);
 }
 
 hipError_t launch_cache_read(const CacheShape& sh, const int32_t* slots, const CachePtr& cache, void* k, void* v, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.slots = slots; a.k_out = k; a.q_out = v;
     const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
-    if (sh.dtype == 1) return sh.mxfp8 ? launch_read<__bf16, true>(a, stream, st) : launch_read<__bf16, false>(a, stream, st);
-    return sh.mxfp8 ? launch_read<float, true>(a, stream, st) : launch_read<float, false>(a, stream, st);
+    return sh.dtype == 1 ? launch_back<__bf16>(a, sh.held, stream, st) : launch_back<float>(a, sh.held, stream, st);
 }
 
 }  // namespace cp

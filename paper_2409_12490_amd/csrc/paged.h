@@ -30,7 +30,7 @@ struct PagedArgs {
     unsigned workgroups, least, setup;
     unsigned cut_units;                       // that there can be: a workgroup leaves one at most
     int whole;                                // units are not cut: a unit counts as one, whatever its steps
-    int mxfp8;
+    int held;
     FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
@@ -133,7 +133,7 @@ struct Run {
         deal();
         if (ROUNDS && !whole && total) {
             const unsigned rest = units - (unsigned)rounds * a.workgroups, turns = (unsigned)first_lane((int)((rest + a.workgroups - 1) / a.workgroups));
-            if (first_lane(uncut_pays(turns, longest, used, share, a.mxfp8))) {
+            if (first_lane(uncut_pays(turns, longest, used, share, a.held != HELD_PLAIN))) {
                 if (rounds) { rounds += (int)turns; total = used = 0; }        // the last round not full
                 else {
                     whole = 1; again = true; total = units;

@@ -1,0 +1,201 @@
+"""Attention of new tokens over pages of 4 bits against fp64: the cases of the other formats, what hidden places hold, arrays that say nonsense, captured calls."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as O
+from paper_2409_12490_amd import binding as B
+from tests.cache4_helpers import Pool4, attend4
+from tests.cache_helpers import DEV, check_attention, f64, randn
+from tests.test_gpu_paged import CASES, DEALT, _starts
+
+pytestmark = pytest.mark.gpu
+
+
+def _case(dtype, hq, hkv, page, seqs, seed=0, scale=1.0):
+    """seqs: (new tokens, tokens in all)."""
+    gen = torch.Generator().manual_seed(seed + 17 * len(seqs) + hq)
+    new, total = zip(*seqs)
+    pool = Pool4(gen, total, hkv, page, dtype, scale=scale)
+    q = randn(gen, max(sum(new), 1), hq + 1, 128, dtype=dtype).to(DEV)[:sum(new), :hq]        # with a gap behind the heads
+    return pool, q, _starts(new), list(total)
+
+
+@pytest.mark.parametrize("case", CASES + DEALT, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}x{c[3]}x{len(c[4])}x{c[4][0][0]}x{c[4][0][1]}")
+def test_against_fp64(case):
+    dtype, hq, hkv, page, seqs = case
+    pool, q, start, total = _case(dtype, hq, hkv, page, seqs)
+    out, lse = attend4(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("keys", [0, 1, 100000])
+@pytest.mark.parametrize("hint", [0, 1, 7, 40, 2000])
+def test_any_hint_of_the_longest_chunk_and_sequence_is_right(hint, keys):
+    pool, q, start, total = _case("bf16", 8, 2, 32, [(1, 90), (33, 150), (300, 420), (1, 1700)])
+    out, lse = attend4(pool, q, start, total, max_q_len=hint, max_kv_len=keys)
+    check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hint", [("bf16", 1), ("bf16", 0), ("fp32", 1), ("fp32", 0)])
+def test_units_that_are_not_cut(dtype, hint):
+    """Sequences said to be short, whatever they are: more units than workgroups, empty ones among them."""
+    seqs = [(1, 1 + 5 * i % 111) if i % 7 else (0, 0) for i in range(100)] + [(40, 900), (1, 0), (3, 2)]
+    pool, q, start, total = _case(dtype, 12, 6, 16, seqs)
+    out, lse = attend4(pool, q, start, total, max_q_len=hint, max_kv_len=100)
+    check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("hint", [1, 0])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("keys,scale", [(20.0, 0.5), (1.0, 1e-38), (1.0, 2e-30)])
+def test_far_logits_and_scales(dtype, hint, keys, scale):
+    """Logits of hundreds, and a scale next to nothing, under which all keys weigh the same."""
+    pool, q, start, total = _case(dtype, 4, 2, 16, [(1, 900), (20, 700)], scale=keys)
+    out, lse = attend4(pool, q, start, total, max_q_len=hint, scale=scale)
+    check_attention(pool, q, start, total, out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,hint", [("bf16", 1), ("bf16", 0), ("fp32", 1), ("fp32", 0)])
+def test_pages_outside_the_pool_hold_nothing(dtype, hint):
+    pool, q, start, total = _case(dtype, 8, 2, 16, [(1, 200), (1, 40), (30, 150), (1, 9)])
+    table = pool.table.clone()
+    table[0, 3], table[0, 12], table[1, :] = -1, pool.n_pages, 2 ** 31 - 1
+    table[2, 0], table[2, 8], table[3, 0] = -2 ** 31, -7, pool.n_pages
+    out, lse = attend4(pool, q, start, total, table=table, max_q_len=hint)
+    check_attention(pool, q, start, total, out, lse, table=table)
+
+
+def test_arrays_that_say_nonsense_stay_inside_the_tensors():
+    pool, q, start, total = _case("bf16", 8, 2, 16, [(3, 60), (2, 30), (4, 100)])
+    guard = torch.full((q.shape[0] + 8, 8, 128), 5.0, dtype=q.dtype, device=DEV)
+    out = guard[4:-4]
+    for hint in (4, 0):
+        for start_, total_ in (([-5, 3, 4, 2 ** 31 - 1], total), ([-2 ** 31, -7, 0, 9], [2 ** 31 - 1, -1, 2 ** 31 - 1]), ([0, 0, 2 ** 30, 2 ** 31 - 1], [-2 ** 31, 2 ** 31 - 1, 5])):
+            attend4(pool, q, start_, total_, max_q_len=hint, out=out)
+        out.fill_(5.0)
+        for start_ in ([0, 9, 3, 9], [9, 9, 9, 0], [0, 3, 2, 9], [9, 9, 9, 9], [0, 0, 0, 0]):      # not ascending: nothing is done; or nothing to do
+            attend4(pool, q, start_, total, max_q_len=hint, out=out)
+        assert (guard == 5).all()
+        out.fill_(7.0)
+    assert (guard[:4] == 5).all() and (guard[-4:] == 5).all()
+
+
+def test_rows_of_no_sequence_are_left_alone():
+    pool, q, _, total = _case("bf16", 8, 2, 16, [(3, 60), (2, 30)])
+    for hint in (4, 1000):
+        out = torch.full((5, 8, 128), 5.0, dtype=q.dtype, device=DEV)
+        got, lse = attend4(pool, q, [1, 2, 4], total, max_q_len=hint, out=out)
+        assert (got[0] == 5).all() and (got[4] == 5).all() and torch.isnan(lse[0]).all() and torch.isfinite(lse[1:4]).all()
+
+
+def test_pages_beyond_32_bits_of_offset():
+    hkv, page, n_pages = 8, 64, 140000                              # 4.6 GB of K
+    cache = B.alloc_cache(n_pages, hkv, page, mxfp4=True)
+    gen = torch.Generator().manual_seed(1)
+    pool = Pool4(gen, [300, 1000], hkv, page)
+    pages = torch.arange(n_pages - pool.n_pages, n_pages, device=DEV)
+    for mine, far in zip(pool.cache, cache):
+        far[pages] = mine
+    for new in ([1, 1], [200, 100]):
+        q = randn(gen, sum(new), 32, 128).to(DEV)
+        want = attend4(pool, q, _starts(new), [300, 1000], max_q_len=max(new))
+        table = torch.where((pool.table >= 0) & (pool.table < pool.n_pages), pool.table + (n_pages - pool.n_pages), -1)
+        far_pool = type("Far", (), dict(vars(pool), cache=list(cache), table=table))
+        got = attend4(far_pool, q, _starts(new), [300, 1000], max_q_len=max(new))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 7), ("bf16", 70), ("fp32", 1), ("fp32", 20)])
+def test_a_captured_call_follows_the_lengths(dtype, new):
+    gen = torch.Generator().manual_seed(5)
+    pool = Pool4(gen, [900, 400, 50 + new], 2, 16, dtype)
+    table = pool.table.to(DEV)
+    q = randn(gen, 3 * new, 8, 128, dtype=dtype).to(DEV)
+    out, lse = torch.empty((3 * new, 8, 128), dtype=q.dtype, device=DEV), torch.empty((3 * new, 8), device=DEV)
+    start = torch.tensor(_starts([new] * 3), dtype=torch.int32, device=DEV)
+    lens = torch.tensor([900, 400, 50 + new], dtype=torch.int32, device=DEV)
+    p = B.make_cache_params(8, 2, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp4=True, page_table=table, max_q_len=new)
+    ws = B.alloc_paged_workspace(p)
+
+    def call():
+        B.critiprefill_paged_attn(p, q, *pool.cache, table, start, lens, out, lse, ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for held in ([900, 400, 50 + new], [new, 130, 17], [500, 399, new], [0, 1, 2], [900, 400, 50 + new]):
+        lens.copy_(torch.tensor(held, dtype=torch.int32))
+        q.copy_(randn(gen, 3 * new, 8, 128, dtype=dtype))
+        call()
+        torch.cuda.synchronize()
+        eager = out.clone(), lse.clone()
+        out.zero_(); lse.zero_(); ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        check_attention(pool, q, _starts([new] * 3), held, out, lse)
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 8), ("bf16", 300), ("fp32", 9)])
+def test_the_same_twice_and_beside_other_work(dtype, new):
+    pool, q, start, total = _case(dtype, 8, 2, 64, [(new, 3000), (new, 700)])
+    first = attend4(pool, q, start, total, max_q_len=new)
+    side = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device=DEV)
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            busy = busy @ busy * 1e-3
+        again = attend4(pool, q, start, total, max_q_len=new)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    torch.cuda.synchronize()
+
+
+def _compare(pool, q, start, total, out, lse, dtype):
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, _ = O.paged_attention(f64(q), pool.held_k, pool.held_v, pool.page, pool.table.numpy(), start, total, 128 ** -0.5)
+    got, got_lse = f64(out), f64(lse)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isnan(got_lse), np.isnan(want_lse)) and not np.isinf(got).any()
+    fine = np.isfinite(want)
+    assert fine.any() and not fine.all()
+    # bf16: P and out rounded, 2^-8 of a term and of the result each at most, and fp32's roundings; both as shares of the largest
+    assert np.abs(got[fine] - want[fine]).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-5) * np.abs(want[fine]).max()
+
+
+ODD = [("bf16", 4, 1, 16, [(4, 40), (2, 9)]), ("bf16", 8, 2, 64, [(100, 230), (5, 5)]), ("bf16", 8, 2, 16, [(70, 70), (1, 40)]), ("fp32", 4, 2, 16, [(6, 50), (40, 40)]),
+       ("fp32", 1, 1, 64, [(16, 16)]), ("bf16", 4, 1, 64, [(300, 5000)]), ("bf16", 8, 1, 32, [(4, 900)])]
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,page,seqs", ODD)
+def test_blocks_of_nan_stay_with_the_rows_that_see_them(dtype, hq, hkv, page, seqs):
+    """32 channels of K or V of some new tokens are NaN: the rows before them must not notice, those that see them are NaN, of V in these channels alone."""
+    pool, q, start, total = _case(dtype, hq, hkv, page, seqs)
+    for i, (n, t) in enumerate(seqs):
+        if n < 2:
+            continue
+        for u, which, block in ((t - 1, 0, 0), (t - n // 2, 1, 2), (t - n // 3 - 1, 1, 0), (t - n + 1, 1, 3)):
+            slot = int(pool.slots[i][u])
+            pool.spoil(which, slot // page, i % hkv, slot % page, block)
+    out, lse = attend4(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    _compare(pool, q, start, total, out, lse, dtype)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,page,seqs", [("bf16", 8, 2, 64, [(100, 230), (70, 5000)]), ("bf16", 16, 1, 16, [(40, 200), (33, 33)]), ("bf16", 1, 1, 32, [(700, 1000)]),
+                                                     ("bf16", 4, 1, 16, [(4, 600)]), ("bf16", 8, 1, 16, [(4, 600)]), ("fp32", 4, 1, 16, [(40, 300)])])
+@pytest.mark.parametrize("before", [0, 70])
+def test_blocks_of_nan_at_any_key(dtype, hq, hkv, page, seqs, before):
+    """Key after key of the new tokens, and of some before them, one block of V each; the fourth stays finite."""
+    pool, q, start, total = _case(dtype, hq, hkv, page, seqs)
+    for i, (n, t) in enumerate(seqs):
+        for u in range(max(0, t - n + 1 - before), t, 1 if n < 60 else 7):
+            slot = int(pool.slots[i][u])
+            for h in range(hkv):
+                pool.spoil(1, slot // page, h, slot % page, u % 3)
+    out, lse = attend4(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    _compare(pool, q, start, total, out, lse, dtype)
