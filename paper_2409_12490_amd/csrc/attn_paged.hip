@@ -1,4 +1,4 @@
-// Attention of the new tokens of each sequence over the pages of a cache, for few rows a KV head (single tokens above all) and for fp32:
+// Attention of the new tokens of each sequence over the pages of a cache, for few rows a KV head (single tokens above all) and for fp32 (bf16 over pages of 4 bits: attn_paged_fp4.hip):
 //
 //   o_t = sum_u p_tu v_u / sum_u p_tu,  p_tu = exp(q_t k_u scale - m_t),  u <= keys - tokens + t;  no such u: o_t = 0, lse_t = -inf
 //
@@ -13,7 +13,7 @@
 //                                 n is channel 8 c + n.  B = P^T, the S^T accumulators as they stand.
 // Nothing goes through LDS and no wave waits for another in the key loop: K of the next step is asked for when QK has read this one's, V when PV has, and the other wave
 // of the SIMD works meanwhile (both a whole step ahead in registers of their own: as fast for one token, 20 % slower for 32 rows, where a second wave then has no room).
-// Keys and values of 8 and 4 bits become bf16 (exact: their scales are powers of two) or fp32 in registers.
+// Keys and values of 8 bits become bf16 (exact: their scales are powers of two) or fp32 in registers, those of 4 bits fp32.
 //
 // What bounds it, 32/8 heads: the memory, with all of K and V read once: one token after 131071 in bf16 95 us and 5.7 TB/s (reads past the caches reach 7.0), 48 single tokens
 // of up to 32769 each over 8-bit pages 74 us and 5.3 TB/s; MFMA and vector units are busy for a twentieth of that.  After 1999 tokens it is latency: 7 us, of which an empty launch
@@ -68,22 +68,17 @@ __device__ __forceinline__ f32x4 widen4f(unsigned w, float scale) {     // to fp
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-// Four neighbouring e2m1 of a word's bytes BYTE and BYTE + 1, and all eight; a scale of 255 makes them NaN.
+// Four neighbouring e2m1 of a word's bytes BYTE and BYTE + 1; a scale of 255 makes them NaN.
 template <int BYTE>
 __device__ __forceinline__ f32x4 half4f(unsigned w, float scale) {
     const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, BYTE), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, BYTE + 1);
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
-}
-__device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {
-    return u32x4{as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-                 as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
 }
 
 // What a wave has of a step: K and V as they come from memory.
 template <bool F32, int HELD> struct Raw;
 template <> struct Raw<false, HELD_PLAIN> { u32x4 k[2][4]; u32x4 v[8]; };                      // [16 keys][64 bytes]; [token]
 template <> struct Raw<false, HELD_MXFP8> { u32x4 k[2][2]; u32x2 v[8]; unsigned ks[2]; u32x4 vs[2]; };
-template <> struct Raw<false, HELD_MXFP4> { u32x4 k[2]; unsigned v[8]; unsigned ks[2]; u32x4 vs[2]; };
 template <> struct Raw<true, HELD_PLAIN> { f32x4 k[8]; f32x4 v[4][2]; };
 template <> struct Raw<true, HELD_MXFP8> { u32x4 k[2]; unsigned v[4][2]; unsigned ks[1]; u32x4 vs[1]; };
 template <> struct Raw<true, HELD_MXFP4> { u32x4 k[1]; unsigned v[4][2]; unsigned ks[1]; u32x4 vs[1]; };
@@ -190,8 +185,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                 if constexpr (!F32) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if constexpr (MX4) raw.v[4 * g + i] = *(const unsigned*)(vp + (4 * kg + i) * kRowBytes + 4 * c16);
-                        else if constexpr (MX) raw.v[4 * g + i] = *(const u32x2*)(vp + (4 * kg + i) * kRowBytes + 8 * c16);
+                        if constexpr (MX) raw.v[4 * g + i] = *(const u32x2*)(vp + (4 * kg + i) * kRowBytes + 8 * c16);
                         else raw.v[4 * g + i] = *(const u32x4*)(vp + (4 * kg + i) * kRowBytes + 16 * c16);
                     }
                     if constexpr (kScaled) raw.vs[g] = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);   // of four tokens
@@ -231,8 +225,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks) {
                         u32x4 kw;
-                        if constexpr (MX4) kw = widen8(raw.k[g][ks], mx_scale(raw.ks[g]));
-                        else if constexpr (MX) {
+                        if constexpr (MX) {
                             const float scale = mx_scale(raw.ks[g]);
                             const u32x2 lo = widen4(raw.k[g][ks >> 1][2 * (ks & 1)], scale), hi = widen4(raw.k[g][ks >> 1][2 * (ks & 1) + 1], scale);
                             kw = u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -289,13 +282,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                         };
                         if constexpr (MX4) {
                             unsigned scales = raw.vs[g][i];
-                            if constexpr (F32) {
-                                if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; scales = 0x7f7f7f7fu; }
-                                else if (i > sure) { clean4(raw.v[i][0], scales, c16 >> 3); clean4(raw.v[i][1], scales, 2 + (c16 >> 3)); }
-                            } else {
-                                if (i > lim) { raw.v[4 * g + i] = 0; scales = 0x7f7f7f7fu; }
-                                else if (i > sure) clean4(raw.v[4 * g + i], scales, c16 >> 2);
-                            }
+                            if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; scales = 0x7f7f7f7fu; }
+                            else if (i > sure) { clean4(raw.v[i][0], scales, c16 >> 3); clean4(raw.v[i][1], scales, 2 + (c16 >> 3)); }
                             raw.vs[g][i] = scales;
                         } else if constexpr (!F32 && MX) {
                             if (i > lim) { raw.v[4 * g + i] = u32x2{0, 0}; raw.vs[g][i] = 0x7f7f7f7fu; }
@@ -354,11 +342,10 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                 }
             }
             if constexpr (!F32) {
-                u32x4 v[8];                                                    // [token][two channels a word]
+                u32x4 v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if constexpr (MX4) v[j] = widen8(raw.v[j], mx_scale((raw.vs[j >> 2][j & 3] >> (8 * (c16 >> 2))) & 0xff));
-                    else if constexpr (MX) {
+                    if constexpr (MX) {
                         const float scale = mx_scale((raw.vs[j >> 2][j & 3] >> (8 * (c16 >> 2))) & 0xff);
                         const u32x2 lo = widen4(raw.v[j][0], scale), hi = widen4(raw.v[j][1], scale);
                         v[j] = u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -578,7 +565,7 @@ hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, cons
         if (sh.held == HELD_MXFP8) return nq == 1 ? launch<true, HELD_MXFP8, 1>(a, st) : nq == 2 ? launch<true, HELD_MXFP8, 2>(a, st) : launch<true, HELD_MXFP8, 4>(a, st);
         return nq == 1 ? launch<true, HELD_PLAIN, 1>(a, st) : nq == 2 ? launch<true, HELD_PLAIN, 2>(a, st) : launch<true, HELD_PLAIN, 4>(a, st);
     }
-    if (sh.held == HELD_MXFP4) return nq == 1 ? launch<false, HELD_MXFP4, 1>(a, st) : launch<false, HELD_MXFP4, 2>(a, st);
+    if (sh.held == HELD_MXFP4) return launch_paged_fp4(sh, route, a, st);
     if (sh.held == HELD_MXFP8) return nq == 1 ? launch<false, HELD_MXFP8, 1>(a, st) : launch<false, HELD_MXFP8, 2>(a, st);
     return launch<false, HELD_PLAIN, 1>(a, st);
 }

@@ -1,0 +1,356 @@
+// Attention of the new tokens of each sequence over pages of 4 bits, for few rows a KV head and bf16: the formulas, tiles and operand layouts of attn_paged.hip (S^T = K . Q^T and
+// O^T += V^T . P^T in 16x16 MFMAs, waves split the keys, nothing by way of LDS before the merge), with a key loop for half of the 8-bit bytes.
+//
+//   K   a lane takes one key's 32 channels of one scale, 16 bytes, and makes them bf16 (exact) by 16 conversions that apply the scale
+//   V   a lane takes 8 channels of 8 tokens, 4 bytes each; 32 conversions, and 32 v_perm that bring two tokens' together
+//   e2m1 has no NaN: what may be one is seen in the scales alone, and a key that no row sees needs no zeros in place of its V
+//
+// A step's loads are half as many bytes as over 8-bit pages for as much work, so what a wave waits for counts: K of the next step is asked for when QK has read this one's, V when
+// PV has, and neither by a branch.  Where the loads stand behind a branch the compiler has to wait for all of them at the first use of any (one token of 10^6 keys 203 us, 64 of 8000 108; without
+// 195 and 103, and past the caches 170 and 91).  Not kept: two steps at a time (64 single tokens of all lengths up to 32769: 90 us for 72, units are short), three workgroups to a
+// compute unit (64 of 8000: 101 us for 91), K as 4-bit operand of a scaled MFMA with Q in two e4m3 pieces (its sums are good to 2^-17 of their terms only).
+#include "paged.h"
+
+#include <type_traits>
+
+namespace cp {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef const __attribute__((address_space(4))) int32_t* scalar_list;   // read through scalar loads: wave-uniform addresses
+
+constexpr float kLazyLog2 = 8.0f;             // how far a row's max may outgrow its reference point before O is rescaled
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { union { u32x4 u; bf16x8 b; } c; c.u = v; return c.b; }
+__device__ __forceinline__ unsigned as_u32(bf16x2 v) { union { bf16x2 b; unsigned u; } c; c.b = v; return c.u; }
+
+// max and sum over the four lanes that share a column: l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float column_max(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// eight neighbouring e2m1 to bf16
+__device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {
+    return u32x4{as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                 as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+// Elements go past the caches: a call reads them once.  us, ordinary loads / past the caches (32/8 heads, pages of 64, caches that no other call has left in the chip): one token of 8000 keys
+// 12.5 / 11.4, of 131072 34.6 / 31.2, of 10^6 194.9 / 170.0; 8 of 2000 15.1 / 14.1, 64 of 8000 102.6 / 91.5.  Scales, 16 tokens' to 64 bytes, by ordinary loads.
+template <typename V>
+__device__ __forceinline__ V get(const char* p) { return __builtin_nontemporal_load((const V*)p); }
+
+constexpr int kWaveKeys = 32;                 // of a step, to each wave
+
+// SMALL: pages of 16 tokens, of which a wave's keys of a step lie in two.
+template <int NQ, bool SMALL>
+__global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
+    constexpr int kRows = 16 * NQ, kGroups = kWaveKeys / 16, RUNS = SMALL ? 2 : 1, kRunGroups = kGroups / RUNS;
+    extern __shared__ __attribute__((aligned(16))) float merge[];              // [wave][row][128], then (max, sum) [wave][row]
+    float* const wave_stats = merge + 4 * kRows * kHeadDim;
+
+    const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, kg = lane >> 4;
+    const int wave = first_lane(tid >> 6);
+    Run<false> run;
+    const bool any = run.find(a, blockIdx.x, lane);
+    if (blockIdx.x == 0 && tid == 0) a.record[0] = (int)run.used;
+    if (run.logical < run.used && tid == 0) a.record[4 + 4 * run.logical + 3] = 0;
+    if (!any) return;
+    const unsigned home = run.logical;
+    const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
+    const int page_mask = (1 << a.page_shift) - 1;
+    const unsigned in_k = (unsigned)c16 * 64 + (unsigned)kg * 16, in_v = (unsigned)kg * 256 + (unsigned)c16 * 4, in_ks = (unsigned)c16 * 4, in_vs = (unsigned)kg * 16;
+    // rotations to the right that bring a block's byte to the exponent's bits: the lane's 32 channels of K, its 8 of V.  What else is in the word is not looked at.
+    const unsigned turn_k = 8u * (unsigned)kg + 9, turn_v = 8u * ((unsigned)c16 >> 2) + 9;
+
+    while (true) {
+        const Sequence seq = run.now;
+        const int tile_tokens = 1 << a.tile_shift, t0 = run.tile << a.tile_shift;
+        const int live = min(tile_tokens, seq.tokens - t0);                    // tokens of the tile
+        unsigned first, count, unit;
+        run.piece(a, first, count, unit);
+        const int head = run.head;
+        const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)run.seq * a.max_pages);
+        const int past = seq.keys - seq.tokens;                                // position of the sequence's first new token
+        const int low = min(past + t0, seq.keys - 1), high = min(past + t0 + live, seq.keys) - 1;   // last keys that its first and its last row see
+
+        // ---- pages are looked up a step ahead; one that is not in the pool holds nothing: its keys are hidden, and read from page 0
+        int entry[RUNS];
+        auto key_of = [&](unsigned x, int r) { return (int)((first + x) << a.step_shift) + wave * kWaveKeys + 16 * r; };        // first key of run r of the unit's step x
+        auto look_up = [&](unsigned x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < RUNS; ++r) entry[r] = table[max(min(key_of(x, r), high), 0) >> a.page_shift];      // no branch; whether the keys are there is asked in load
+        };
+        int seen[RUNS], seen_next[RUNS];                                       // keys of a run that exist, of this step and the next
+        int64_t at[RUNS];                                                      // first row of the runs asked for last
+        u32x4 rk[kGroups], rvs[kGroups]; unsigned rks[kGroups], rv[4 * kGroups];
+        auto load_k = [&](unsigned x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < RUNS; ++r) {
+                const int u = key_of(x, r);
+                const bool there = (unsigned)entry[r] < (unsigned)a.n_pages && u <= high;
+                seen_next[r] = there ? seq.keys - u : 0;
+                at[r] = (((int64_t)(there ? entry[r] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
+            }
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int r = g / kRunGroups, more = g % kRunGroups;
+                rk[g] = get<u32x4>((const char*)a.cache.k + at[r] * 64 + 1024 * more + in_k);
+                rks[g] = *(const unsigned*)((const char*)a.cache.ks + at[r] * 4 + 64 * more + in_ks);         // of a token
+            }
+        };
+        auto load_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int r = g / kRunGroups, more = g % kRunGroups;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) rv[4 * g + i] = get<unsigned>((const char*)a.cache.v + at[r] * 64 + 1024 * more + 64 * i + in_v);
+                rvs[g] = *(const u32x4*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
+            }
+        };
+        look_up(0);
+
+        // ---- Q: lane's column is a row, 8 channels at 32 kg + 8 ks
+        bf16x8 qf[NQ][4];
+        int last[NQ];                                                          // the last key that the row sees
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, live - 1), g = r - of * a.group;
+            last[nq] = min(past + t0 + t, seq.keys - 1);
+            const int64_t from = (seq.start + t0 + t) * a.qs0 + (int64_t)(head * a.group + g) * a.qs1 + 32 * kg;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)((const __bf16*)a.q + from + 8 * ks);
+        }
+        __builtin_amdgcn_sched_barrier(0);                                     // in the loop's order, or its waits are for what is older in either
+        load_k(0);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v();
+        __builtin_amdgcn_sched_barrier(0);
+        look_up(1);
+
+        f32x4 o[NQ][8];
+        float m_run[NQ], l_run[NQ];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            m_run[nq] = -INFINITY; l_run[nq] = 0.f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) o[nq][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        bool odd = false;
+
+        // The last step stands apart: where a wave asks for the next one's keys or does not, by a branch, it can only wait for all that it has asked for.
+        auto work = [&](unsigned x, auto more) __attribute__((always_inline)) {
+#pragma unroll
+            for (int r = 0; r < RUNS; ++r) seen[r] = seen_next[r];
+            f32x4 s[NQ][kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const float scale = __uint_as_float(__builtin_amdgcn_alignbit(rks[g], rks[g], turn_k));
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) s[nq][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {
+                    const bf16x8 kw = as_bf16x8(widen8(rk[g][ks], scale));
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) s[nq][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, qf[nq][ks], s[nq][g], 0, 0, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more.value) load_k(x + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            // Hidden keys: behind the row's own, or without a page.
+            bool whole = key_of(x, RUNS - 1) + 16 * kRunGroups - 1 <= low;
+#pragma unroll
+            for (int r = 0; r < RUNS; ++r) whole = whole && seen[r] > 0;
+            if (!whole) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const int r = g / kRunGroups, u = key_of(x, r) + 16 * (g % kRunGroups) + 4 * kg;
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq) {
+                        const int lim = seen[r] > 0 ? last[nq] - u : -1;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[nq][g][i] = i > lim ? -INFINITY : s[nq][g][i];
+                    }
+                }
+            }
+            bf16x8 pf[NQ];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) mx = fmaxf(fmaxf(fmaxf(s[nq][g][0], s[nq][g][1]), fmaxf(s[nq][g][2], s[nq][g][3])), mx);
+                mx = column_max(mx);
+                // the reference point moves only when the maximum has outgrown it by 2^kLazyLog2: P <= 2^8 meanwhile, the same factor in O and l
+                const float m_new = mx > m_run[nq] + lazy_raw ? mx : m_run[nq];
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = __builtin_amdgcn_exp2f((m_run[nq] - m_safe) * c);
+                const float ms = m_safe * c;
+                m_run[nq] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[nq][g][i], c, -ms));
+                        sum += p;                                              // before P is rounded for the product: lse is as exact as fp32 allows
+                        pf[nq][4 * g + i] = (__bf16)p;
+                    }
+                l_run[nq] = l_run[nq] * alpha + sum;
+                if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) o[nq][n] *= alpha;
+                }
+            }
+            // A weight of 0 keeps everything of a hidden key out of a sum but NaN, which only a scale can bring: it becomes another there.  `odd` says that some rows see
+            // such a key and others do not; the unit's end adds it for those that do.
+            unsigned scales[kGroups][4];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) scales[g][i] = __builtin_amdgcn_alignbit(rvs[g][i], rvs[g][i], turn_v);
+            if (!whole) {
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const int r = g / kRunGroups, u = key_of(x, r) + 16 * (g % kRunGroups) + 4 * kg;
+                    const int lim = seen[r] > 0 ? high - u : -1, sure = seen[r] > 0 ? low - u : -1;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool nan = (scales[g][i] & 0x7f800000u) == 0x7f800000u;
+                        if (i > sure && nan) { scales[g][i] = 0x3f800000u; if (i <= lim) odd = true; }
+                    }
+                }
+            }
+            u32x4 v[8];                                                        // [token][two channels a word]
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = widen8(rv[j], __uint_as_float(scales[j >> 2][j & 3]));
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                u32x4 w;                                                       // channel n of the lane's 8 tokens
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(v[2 * e + 1][n >> 1], v[2 * e][n >> 1], n & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pf[nq], o[nq][n], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more.value) { load_v(); look_up(x + 2); }
+        };
+        for (unsigned x = 0; x + 1 < count; ++x) work(x, std::true_type());
+        work(count - 1, std::false_type());
+
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+            for (unsigned x = 0; x < count; ++x)
+                for (int i = 0; i < kWaveKeys; ++i) {                          // once in a blue moon: a key after another, from memory
+                    const int u = (int)((first + x) << a.step_shift) + wave * kWaveKeys + i;
+                    if (u <= low || u > high) continue;
+                    const int page = table[u >> a.page_shift];
+                    if ((unsigned)page >= (unsigned)a.n_pages) continue;
+                    const int64_t row = (((int64_t)page * a.hkv + head) << a.page_shift) + (u & page_mask);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {                              // channels 32 kg + 8 e ..
+                        if (a.cache.vs[row * 4 + kg] != 0xff) continue;
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                            for (int n = 0; n < 8; ++n)
+                                if (u <= last[nq]) o[nq][n][e] = NAN;
+                    }
+                }
+        }
+
+        // ---- merge the four waves: sum_w 2^(c (m_w - M)) O_w; 16-byte pieces of a row swizzled by the row
+        __syncthreads();                                                       // the unit before has been read
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + c16;
+            const float l = column_sum(l_run[nq]);
+            if (kg == 0) { wave_stats[2 * (wave * kRows + r)] = m_run[nq]; wave_stats[2 * (wave * kRows + r) + 1] = l; }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {                         // channels 8 (4 kg + i) + 4 half ..
+                    const int piece = 2 * (4 * kg + i) + half;
+                    f32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = o[nq][4 * half + e][i];
+                    *(f32x4*)(merge + (wave * kRows + r) * kHeadDim + 4 * (piece ^ c16)) = w;
+                }
+        }
+        __syncthreads();
+        const bool began = first == 0, ended = first + count == unit;
+        const int64_t slot = 2 * (int64_t)home + (began ? 1 : 0);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int r = 16 * nq + (tid >> 4), piece = tid & 15;              // 8 channels
+            const int t = (int)a.by_group.div((unsigned)r), g = r - t * a.group;
+            if (t >= live) continue;
+            float M = -INFINITY, L = 0.f, sum[8];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) M = fmaxf(M, wave_stats[2 * (w * kRows + r)]);
+            const float M_safe = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f((wave_stats[2 * (w * kRows + r)] - M_safe) * c);
+                L = fmaf(f, wave_stats[2 * (w * kRows + r) + 1], L);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const f32x4 v = *(const f32x4*)(merge + (w * kRows + r) * kHeadDim + 4 * ((2 * piece + half) ^ (r & 15)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[4 * half + e] = fmaf(f, v[e], sum[4 * half + e]);
+                }
+            }
+            if (began && ended) {
+                const float inv = L == 0.f ? 0.f : 1.0f / L;
+                const int64_t row = seq.start + t0 + t;
+                const int h = head * a.group + g;
+                const int64_t to = row * a.os0 + h * a.os1 + 8 * piece;
+                bf16x8 w;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = (__bf16)(sum[e] * inv);
+                *(bf16x8*)((__bf16*)a.out + to) = w;
+                if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
+            } else {
+                float* to = a.parts + (slot * kRows + r) * kHeadDim + 8 * piece;
+                *(f32x4*)to = f32x4{sum[0], sum[1], sum[2], sum[3]};
+                *(f32x4*)(to + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+                if (piece == 0) *(f32x2*)(a.stats + 2 * (slot * kRows + r)) = f32x2{M, L};
+            }
+        }
+        if (began && !ended && tid == 0) {
+            const unsigned rest = unit - first - count;                        // of whole runs, the last perhaps not whole
+            int32_t* rec = a.record + 4 + 4 * home;
+            rec[0] = seq.start + t0; rec[1] = live; rec[2] = head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
+        }
+        if (!run.next_steps(a)) break;
+    }
+}
+
+template <int NQ, bool SMALL>
+hipError_t launch(const PagedArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((paged_fp4_kernel<NQ, SMALL>), dim3(a.workgroups), dim3(kThreads), 4 * 16 * NQ * (kHeadDim + 2) * 4, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_fp4(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st) {
+    const bool small = sh.page_shift < 5;
+    if (route.rows == 16) return small ? launch<1, true>(a, st) : launch<1, false>(a, st);
+    return small ? launch<2, true>(a, st) : launch<2, false>(a, st);
+}
+
+}  // namespace cp

@@ -369,6 +369,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int rows, unsign
 }  // namespace
 
 hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st);
+hipError_t launch_paged_fp4(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st);
 hipError_t launch_paged_chunk(const CacheShape& sh, const PagedArgs& a, hipStream_t st);
 
 }  // namespace cp
