@@ -54,6 +54,44 @@ __device__ __forceinline__ V get(const char* p) { return __builtin_nontemporal_l
 
 constexpr int kWaveKeys = 32;                 // of a step, to each wave
 
+// One unit, or the piece of it that lies in a workgroup's run.  All the same for a workgroup.
+struct Unit {
+    int seq, head, row, live;                 // row: its first token's, live: its tokens
+    int keys, past, low, high;                // of the sequence; position of the unit's first token; last keys that its first and its last row see
+    unsigned first, count, steps;             // steps first .. first + count - 1 of `steps`
+    // the first key of a wave's r-th 16 (of pages of 16), in step x of the piece
+    __device__ __forceinline__ int key(const PagedArgs& a, unsigned x, int wave, int r) const { return (int)((first + x) << a.step_shift) + wave * kWaveKeys + 16 * r; }
+};
+__device__ __forceinline__ Unit unit_of(const PagedArgs& a, const Run<false>& run) {
+    Unit n;
+    const int t0 = run.tile << a.tile_shift;
+    n.seq = run.seq; n.head = run.head; n.row = run.now.start + t0; n.live = min(1 << a.tile_shift, run.now.tokens - t0);
+    n.keys = run.now.keys; n.past = run.now.keys - run.now.tokens + t0;
+    n.low = min(n.past, n.keys - 1); n.high = min(n.past + n.live, n.keys) - 1;
+    run.piece(a, n.first, n.count, n.steps);
+    return n;
+}
+// Run::next_steps with scalar loads: a vector load's wait would be one for all keys and values that are under way.
+__device__ __forceinline__ bool next_unit(const PagedArgs& a, Run<false>& run) {
+    const unsigned rest = run.whole ? 1u : a.setup + run.now.steps_of(a, run.tile) - run.at;
+    if (run.left <= rest) return false;
+    run.left -= rest;
+    run.at = 0;
+    if (++run.tile == run.now.tiles) {
+        run.tile = 0;
+        if (++run.head == a.hkv) {
+            run.head = 0;
+            do {
+                if (++run.seq >= a.n_seqs) return false;
+                run.now.load_uniform(a, run.seq, run.whole);
+            } while (run.now.tiles == 0);
+        }
+    }
+    return run.has_steps(a);
+}
+
+enum { NOTHING = 0, SAME_UNIT = 1, NEXT_UNIT = 2 };
+
 // SMALL: pages of 16 tokens, of which a wave's keys of a step lie in two.
 template <int NQ, bool SMALL>
 __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
@@ -75,70 +113,74 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
     // rotations to the right that bring a block's byte to the exponent's bits: the lane's 32 channels of K, its 8 of V.  What else is in the word is not looked at.
     const unsigned turn_k = 8u * (unsigned)kg + 9, turn_v = 8u * ((unsigned)c16 >> 2) + 9;
 
-    while (true) {
-        const Sequence seq = run.now;
-        const int tile_tokens = 1 << a.tile_shift, t0 = run.tile << a.tile_shift;
-        const int live = min(tile_tokens, seq.tokens - t0);                    // tokens of the tile
-        unsigned first, count, unit;
-        run.piece(a, first, count, unit);
-        const int head = run.head;
-        const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)run.seq * a.max_pages);
-        const int past = seq.keys - seq.tokens;                                // position of the sequence's first new token
-        const int low = min(past + t0, seq.keys - 1), high = min(past + t0 + live, seq.keys) - 1;   // last keys that its first and its last row see
-
-        // ---- pages are looked up a step ahead; one that is not in the pool holds nothing: its keys are hidden, and read from page 0
-        int entry[RUNS];
-        auto key_of = [&](unsigned x, int r) { return (int)((first + x) << a.step_shift) + wave * kWaveKeys + 16 * r; };        // first key of run r of the unit's step x
-        auto look_up = [&](unsigned x) __attribute__((always_inline)) {
+    // ---- the step that is looked up, the one that is asked for, and the one that is worked on, each ahead of the other, across the ends of units
+    int entry[RUNS];
+    auto look_up = [&](const Unit& n, unsigned x) __attribute__((always_inline)) {
+        const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)n.seq * a.max_pages);
 #pragma unroll
-            for (int r = 0; r < RUNS; ++r) entry[r] = table[max(min(key_of(x, r), high), 0) >> a.page_shift];      // no branch; whether the keys are there is asked in load
-        };
-        int seen[RUNS], seen_next[RUNS];                                       // keys of a run that exist, of this step and the next
-        int64_t at[RUNS];                                                      // first row of the runs asked for last
-        u32x4 rk[kGroups], rvs[kGroups]; unsigned rks[kGroups], rv[4 * kGroups];
-        auto load_k = [&](unsigned x) __attribute__((always_inline)) {
+        for (int r = 0; r < RUNS; ++r) entry[r] = table[max(min(n.key(a, x, wave, r), n.high), 0) >> a.page_shift];    // no branch; whether the keys are there is asked in load_k
+    };
+    int seen[RUNS], seen_next[RUNS];                                           // keys of a run that exist, of this step and the next
+    int64_t at[RUNS];                                                          // first row of the runs asked for last
+    u32x4 rk[kGroups], rvs[kGroups]; unsigned rks[kGroups], rv[4 * kGroups];
+    auto load_k = [&](const Unit& n, unsigned x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < RUNS; ++r) {
-                const int u = key_of(x, r);
-                const bool there = (unsigned)entry[r] < (unsigned)a.n_pages && u <= high;
-                seen_next[r] = there ? seq.keys - u : 0;
-                at[r] = (((int64_t)(there ? entry[r] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
-            }
+        for (int r = 0; r < RUNS; ++r) {                                       // a page that is not in the pool holds nothing: its keys are hidden, and read from page 0
+            const int u = n.key(a, x, wave, r);
+            const bool there = (unsigned)entry[r] < (unsigned)a.n_pages && u <= n.high;
+            seen_next[r] = there ? n.keys - u : 0;
+            at[r] = (((int64_t)(there ? entry[r] : 0) * a.hkv + n.head) << a.page_shift) + (u & page_mask);
+        }
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int r = g / kRunGroups, more = g % kRunGroups;
-                rk[g] = get<u32x4>((const char*)a.cache.k + at[r] * 64 + 1024 * more + in_k);
-                rks[g] = *(const unsigned*)((const char*)a.cache.ks + at[r] * 4 + 64 * more + in_ks);         // of a token
-            }
-        };
-        auto load_v = [&]() __attribute__((always_inline)) {
+        for (int g = 0; g < kGroups; ++g) {
+            const int r = g / kRunGroups, more = g % kRunGroups;
+            rk[g] = get<u32x4>((const char*)a.cache.k + at[r] * 64 + 1024 * more + in_k);
+            rks[g] = *(const unsigned*)((const char*)a.cache.ks + at[r] * 4 + 64 * more + in_ks);             // of a token
+        }
+    };
+    auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int r = g / kRunGroups, more = g % kRunGroups;
+        for (int g = 0; g < kGroups; ++g) {
+            const int r = g / kRunGroups, more = g % kRunGroups;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) rv[4 * g + i] = get<unsigned>((const char*)a.cache.v + at[r] * 64 + 1024 * more + 64 * i + in_v);
-                rvs[g] = *(const u32x4*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
-            }
-        };
-        look_up(0);
-
-        // ---- Q: lane's column is a row, 8 channels at 32 kg + 8 ks
-        bf16x8 qf[NQ][4];
-        int last[NQ];                                                          // the last key that the row sees
+            for (int i = 0; i < 4; ++i) rv[4 * g + i] = get<unsigned>((const char*)a.cache.v + at[r] * 64 + 1024 * more + 64 * i + in_v);
+            rvs[g] = *(const u32x4*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
+        }
+    };
+    bf16x8 qf[NQ][4];                                                          // lane's column is a row, 8 channels at 32 kg + 8 ks
+    auto load_q = [&](const Unit& n) __attribute__((always_inline)) {
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
-            const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, live - 1), g = r - of * a.group;
-            last[nq] = min(past + t0 + t, seq.keys - 1);
-            const int64_t from = (seq.start + t0 + t) * a.qs0 + (int64_t)(head * a.group + g) * a.qs1 + 32 * kg;
+            const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, n.live - 1), g = r - of * a.group;
+            const int64_t from = (int64_t)(n.row + t) * a.qs0 + (int64_t)(n.head * a.group + g) * a.qs1 + 32 * kg;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)((const __bf16*)a.q + from + 8 * ks);
         }
+    };
+    auto begin = [&](const Unit& n) __attribute__((always_inline)) {
+        look_up(n, 0);
+        load_q(n);
         __builtin_amdgcn_sched_barrier(0);                                     // in the loop's order, or its waits are for what is older in either
-        load_k(0);
+        load_k(n, 0);
         __builtin_amdgcn_sched_barrier(0);
         load_v();
         __builtin_amdgcn_sched_barrier(0);
-        look_up(1);
+        look_up(n, 1);
+    };
+    // The first step of the next unit is asked for in this one's last: what a unit begins and ends with, some 3 us, passes meanwhile (64 single tokens of up to 32769 keys 73.7 us, now 66.9).
+    // With 32 rows there are no registers for it.
+    constexpr bool kAcross = NQ == 1;
+    Unit now = unit_of(a, run);
+    begin(now);
+
+    while (true) {
+        const bool another = kAcross && next_unit(a, run);
+        const Unit then = another ? unit_of(a, run) : now;
+        if (another && now.count == 1) look_up(then, 0);
+        const int high = now.high, low = now.low;
+        int last[NQ];                                                          // the last key that the row sees
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) last[nq] = min(now.past + min((int)a.by_group.div((unsigned)(16 * nq + c16)), now.live - 1), now.keys - 1);
 
         f32x4 o[NQ][8];
         float m_run[NQ], l_run[NQ];
@@ -150,8 +192,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
         }
         bool odd = false;
 
-        // The last step stands apart: where a wave asks for the next one's keys or does not, by a branch, it can only wait for all that it has asked for.
-        auto work = [&](unsigned x, auto more) __attribute__((always_inline)) {
+        // What is asked for: the next step, that of another unit with its queries, or nothing.  Each has code of its own: where a wave asks by a branch it can only wait for all.
+        auto work = [&](unsigned x, auto asks) __attribute__((always_inline)) {
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) seen[r] = seen_next[r];
             f32x4 s[NQ][kGroups];
@@ -168,16 +210,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (more.value) load_k(x + 1);
+            if constexpr (asks.value == SAME_UNIT) load_k(now, x + 1);
+            if constexpr (asks.value == NEXT_UNIT) { load_q(then); load_k(then, 0); }
             __builtin_amdgcn_sched_barrier(0);
             // Hidden keys: behind the row's own, or without a page.
-            bool whole = key_of(x, RUNS - 1) + 16 * kRunGroups - 1 <= low;
+            bool whole = now.key(a, x, wave, RUNS - 1) + 16 * kRunGroups - 1 <= low;
 #pragma unroll
             for (int r = 0; r < RUNS; ++r) whole = whole && seen[r] > 0;
             if (!whole) {
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int r = g / kRunGroups, u = key_of(x, r) + 16 * (g % kRunGroups) + 4 * kg;
+                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + 4 * kg;
 #pragma unroll
                     for (int nq = 0; nq < NQ; ++nq) {
                         const int lim = seen[r] > 0 ? last[nq] - u : -1;
@@ -224,7 +267,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
             if (!whole) {
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int r = g / kRunGroups, u = key_of(x, r) + 16 * (g % kRunGroups) + 4 * kg;
+                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + 4 * kg;
                     const int lim = seen[r] > 0 ? high - u : -1, sure = seen[r] > 0 ? low - u : -1;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -245,19 +288,25 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pf[nq], o[nq][n], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (more.value) { load_v(); look_up(x + 2); }
+            if constexpr (asks.value != NOTHING) load_v();
+            if constexpr (asks.value == SAME_UNIT) { if (kAcross && x + 2 >= now.count) look_up(then, 0); else look_up(now, x + 2); }
+            if constexpr (asks.value == NEXT_UNIT) look_up(then, 1);
         };
-        for (unsigned x = 0; x + 1 < count; ++x) work(x, std::true_type());
-        work(count - 1, std::false_type());
+        for (unsigned x = 0; x + 1 < now.count; ++x) work(x, std::integral_constant<int, SAME_UNIT>());
+        if constexpr (kAcross) {
+            if (another) work(now.count - 1, std::integral_constant<int, NEXT_UNIT>());
+            else work(now.count - 1, std::integral_constant<int, NOTHING>());
+        } else work(now.count - 1, std::integral_constant<int, NOTHING>());
 
         if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-            for (unsigned x = 0; x < count; ++x)
+            const scalar_list table = (scalar_list)(unsigned long long)(a.table + (int64_t)now.seq * a.max_pages);
+            for (unsigned x = 0; x < now.count; ++x)
                 for (int i = 0; i < kWaveKeys; ++i) {                          // once in a blue moon: a key after another, from memory
-                    const int u = (int)((first + x) << a.step_shift) + wave * kWaveKeys + i;
+                    const int u = now.key(a, x, wave, 0) + i;
                     if (u <= low || u > high) continue;
                     const int page = table[u >> a.page_shift];
                     if ((unsigned)page >= (unsigned)a.n_pages) continue;
-                    const int64_t row = (((int64_t)page * a.hkv + head) << a.page_shift) + (u & page_mask);
+                    const int64_t row = (((int64_t)page * a.hkv + now.head) << a.page_shift) + (u & page_mask);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {                              // channels 32 kg + 8 e ..
                         if (a.cache.vs[row * 4 + kg] != 0xff) continue;
@@ -289,13 +338,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 }
         }
         __syncthreads();
-        const bool began = first == 0, ended = first + count == unit;
+        const bool began = now.first == 0, ended = now.first + now.count == now.steps;
         const int64_t slot = 2 * (int64_t)home + (began ? 1 : 0);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
             const int r = 16 * nq + (tid >> 4), piece = tid & 15;              // 8 channels
             const int t = (int)a.by_group.div((unsigned)r), g = r - t * a.group;
-            if (t >= live) continue;
+            if (t >= now.live) continue;
             float M = -INFINITY, L = 0.f, sum[8];
 #pragma unroll
             for (int w = 0; w < 4; ++w) M = fmaxf(M, wave_stats[2 * (w * kRows + r)]);
@@ -315,8 +364,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
             }
             if (began && ended) {
                 const float inv = L == 0.f ? 0.f : 1.0f / L;
-                const int64_t row = seq.start + t0 + t;
-                const int h = head * a.group + g;
+                const int64_t row = now.row + t;
+                const int h = now.head * a.group + g;
                 const int64_t to = row * a.os0 + h * a.os1 + 8 * piece;
                 bf16x8 w;
 #pragma unroll
@@ -331,11 +380,18 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
             }
         }
         if (began && !ended && tid == 0) {
-            const unsigned rest = unit - first - count;                        // of whole runs, the last perhaps not whole
+            const unsigned rest = now.steps - now.first - now.count;                        // of whole runs, the last perhaps not whole
             int32_t* rec = a.record + 4 + 4 * home;
-            rec[0] = seq.start + t0; rec[1] = live; rec[2] = head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
+            rec[0] = now.row; rec[1] = now.live; rec[2] = now.head; rec[3] = 1 + (int)((rest + run.share - 1) / run.share);
         }
-        if (!run.next_steps(a)) break;
+        if constexpr (kAcross) {
+            if (!another) break;
+            now = then;
+        } else {
+            if (!next_unit(a, run)) break;
+            now = unit_of(a, run);
+            begin(now);
+        }
     }
 }
 

@@ -56,7 +56,15 @@ struct Sequence {                             // one sequence, checked: whatever
         return TileSteps(tokens, keys, a.step_shift).of((unsigned)j, a.tile_shift, a.step_shift);
     }
     __device__ __forceinline__ bool load(const PagedArgs& a, int s, int whole) {       // whether its rows ascend
-        const int from = a.q_start[s], to = a.q_start[s + 1], held = a.kv_len[s];
+        return set(a, a.q_start[s], a.q_start[s + 1], a.kv_len[s], whole);
+    }
+    // the same for a number that all lanes share, through scalar loads
+    __device__ __forceinline__ void load_uniform(const PagedArgs& a, int s, int whole) {
+        typedef const __attribute__((address_space(4))) int32_t* list;
+        const list starts = (list)(unsigned long long)a.q_start, lengths = (list)(unsigned long long)a.kv_len;
+        set(a, starts[s], starts[s + 1], lengths[s], whole);
+    }
+    __device__ __forceinline__ bool set(const PagedArgs& a, int from, int to, int held, int whole) {
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
