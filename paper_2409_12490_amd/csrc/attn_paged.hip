@@ -1,4 +1,4 @@
-// Attention of the new tokens of each sequence over the pages of a cache, for few rows a KV head (single tokens above all) and for fp32 (bf16 over pages of 4 bits: attn_paged_fp4.hip):
+// Attention of the new tokens of each sequence over the pages of a cache, plain and of 8 bits, for few rows a KV head (single tokens above all) and for fp32:
 //
 //   o_t = sum_u p_tu v_u / sum_u p_tu,  p_tu = exp(q_t k_u scale - m_t),  u <= keys - tokens + t;  no such u: o_t = 0, lse_t = -inf
 //
@@ -13,7 +13,7 @@
 //                                 n is channel 8 c + n.  B = P^T, the S^T accumulators as they stand.
 // Nothing goes through LDS and no wave waits for another in the key loop: K of the next step is asked for when QK has read this one's, V when PV has, and the other wave
 // of the SIMD works meanwhile (both a whole step ahead in registers of their own: as fast for one token, 20 % slower for 32 rows, where a second wave then has no room).
-// Keys and values of 8 bits become bf16 (exact: their scales are powers of two) or fp32 in registers, those of 4 bits fp32.
+// 8-bit keys and values become bf16 (exact: their scales are powers of two) or fp32 in registers.
 //
 // What bounds it, 32/8 heads: the memory, with all of K and V read once: one token after 131071 in bf16 95 us and 5.7 TB/s (reads past the caches reach 7.0), 48 single tokens
 // of up to 32769 each over 8-bit pages 74 us and 5.3 TB/s; MFMA and vector units are busy for a twentieth of that.  After 1999 tokens it is latency: 7 us, of which an empty launch
@@ -68,26 +68,17 @@ __device__ __forceinline__ f32x4 widen4f(unsigned w, float scale) {     // to fp
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-// Four neighbouring e2m1 of a word's bytes BYTE and BYTE + 1; a scale of 255 makes them NaN.
-template <int BYTE>
-__device__ __forceinline__ f32x4 half4f(unsigned w, float scale) {
-    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, BYTE), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, BYTE + 1);
-    return f32x4{lo[0], lo[1], hi[0], hi[1]};
-}
-
 // What a wave has of a step: K and V as they come from memory.
-template <bool F32, int HELD> struct Raw;
-template <> struct Raw<false, HELD_PLAIN> { u32x4 k[2][4]; u32x4 v[8]; };                      // [16 keys][64 bytes]; [token]
-template <> struct Raw<false, HELD_MXFP8> { u32x4 k[2][2]; u32x2 v[8]; unsigned ks[2]; u32x4 vs[2]; };
-template <> struct Raw<true, HELD_PLAIN> { f32x4 k[8]; f32x4 v[4][2]; };
-template <> struct Raw<true, HELD_MXFP8> { u32x4 k[2]; unsigned v[4][2]; unsigned ks[1]; u32x4 vs[1]; };
-template <> struct Raw<true, HELD_MXFP4> { u32x4 k[1]; unsigned v[4][2]; unsigned ks[1]; u32x4 vs[1]; };
+template <bool F32, bool MX> struct Raw;
+template <> struct Raw<false, false> { u32x4 k[2][4]; u32x4 v[8]; };                           // [16 keys][64 bytes]; [token]
+template <> struct Raw<false, true> { u32x4 k[2][2]; u32x2 v[8]; unsigned ks[2]; u32x4 vs[2]; };
+template <> struct Raw<true, false> { f32x4 k[8]; f32x4 v[4][2]; };
+template <> struct Raw<true, true> { u32x4 k[2]; unsigned v[4][2]; unsigned ks; u32x4 vs; };
 
-template <bool F32, int HELD, int NQ>
+template <bool F32, bool MX, int NQ>
 __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_kernel(PagedArgs a) {
     constexpr int kRows = 16 * NQ, kWaveKeys = F32 ? 16 : 32, kGroups = kWaveKeys / 16;
-    constexpr bool MX = HELD == HELD_MXFP8, MX4 = HELD == HELD_MXFP4, kScaled = MX || MX4;
-    constexpr int kRowBytes = row_bytes(HELD, F32 ? 4 : 2);
+    constexpr int kRowBytes = MX ? kHeadDim : (F32 ? 512 : 256);
     extern __shared__ __attribute__((aligned(16))) float merge[];              // [wave][row][128], then (max, sum) [wave][row]
     float* const wave_stats = merge + 4 * kRows * kHeadDim;
 
@@ -151,7 +142,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                 entry[g] = table[max(min(u, high), 0) >> a.page_shift];        // no branch; whether the keys are there is asked in load
             }
         };
-        Raw<F32, HELD> raw;
+        Raw<F32, MX> raw;
         int seen[kGroups], seen_next[kGroups];                                 // keys of a group that exist, of this step and the next
         int64_t at[kGroups];                                                   // first row of the groups asked for last
         auto load_k = [&](unsigned step) __attribute__((always_inline)) {
@@ -162,20 +153,19 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                 seen_next[g] = there ? seq.keys - u : 0;
                 at[g] = (((int64_t)(there ? entry[g] : 0) * a.hkv + head) << a.page_shift) + (u & page_mask);
                 const char* kp = (const char*)a.cache.k + at[g] * kRowBytes;
-                if constexpr (MX4) {
-                    raw.k[g] = *(const u32x4*)(kp + c16 * kRowBytes + kg * 16);
-                } else if constexpr (!F32) {
+                if constexpr (!F32) {
                     const int per = MX ? 32 : 64;
 #pragma unroll
                     for (int x = 0; x < (MX ? 2 : 4); ++x) raw.k[g][x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * per + 16 * x);
+                    if constexpr (MX) raw.ks[g] = (a.cache.ks + at[g] * 4)[c16 * 4 + kg];
                 } else if constexpr (MX) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x) raw.k[x] = *(const u32x4*)(kp + c16 * kRowBytes + kg * 32 + 16 * x);
+                    raw.ks = (a.cache.ks + at[g] * 4)[c16 * 4 + kg];
                 } else {
 #pragma unroll
                     for (int x = 0; x < 8; ++x) raw.k[x] = *(const f32x4*)(kp + c16 * kRowBytes + kg * 128 + 16 * x);
                 }
-                if constexpr (kScaled) raw.ks[g] = (a.cache.ks + at[g] * 4)[c16 * 4 + kg];
             }
         };
         auto load_v = [&]() __attribute__((always_inline)) {
@@ -188,16 +178,13 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                         if constexpr (MX) raw.v[4 * g + i] = *(const u32x2*)(vp + (4 * kg + i) * kRowBytes + 8 * c16);
                         else raw.v[4 * g + i] = *(const u32x4*)(vp + (4 * kg + i) * kRowBytes + 16 * c16);
                     }
-                    if constexpr (kScaled) raw.vs[g] = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);   // of four tokens
-                } else if constexpr (kScaled) {
+                    if constexpr (MX) raw.vs[g] = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);   // of four tokens
+                } else if constexpr (MX) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            if constexpr (MX4) raw.v[i][x] = *(const uint16_t*)(vp + (4 * kg + i) * kRowBytes + 2 * c16 + 32 * x);
-                            else raw.v[i][x] = *(const unsigned*)(vp + (4 * kg + i) * kRowBytes + 4 * c16 + 64 * x);
-                        }
-                    raw.vs[g] = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);
+                        for (int x = 0; x < 2; ++x) raw.v[i][x] = *(const unsigned*)(vp + (4 * kg + i) * kRowBytes + 4 * c16 + 64 * x);
+                    raw.vs = *(const u32x4*)(a.cache.vs + at[g] * 4 + 16 * kg);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -237,8 +224,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
                     f32x4 kw;
-                    if constexpr (MX4) kw = x & 1 ? half4f<2>(raw.k[0][x >> 1], mx_scale(raw.ks[0])) : half4f<0>(raw.k[0][x >> 1], mx_scale(raw.ks[0]));
-                    else if constexpr (MX) kw = widen4f(raw.k[x >> 2][x & 3], mx_scale(raw.ks[0]));
+                    if constexpr (MX) kw = widen4f(raw.k[x >> 2][x & 3], mx_scale(raw.ks));
                     else kw = raw.k[x];
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -276,16 +262,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                             any = any || ~keep;
                             return x & keep;
                         };
-                        // e2m1: blocks whose scale is NaN's, of the lane's channels
-                        auto clean4 = [&](unsigned& x, unsigned& scales, int byte) {
-                            if (((scales >> (8 * byte)) & 0xff) == 0xff) { any = true; x = 0; scales ^= 0x80u << (8 * byte); }
-                        };
-                        if constexpr (MX4) {
-                            unsigned scales = raw.vs[g][i];
-                            if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; scales = 0x7f7f7f7fu; }
-                            else if (i > sure) { clean4(raw.v[i][0], scales, c16 >> 3); clean4(raw.v[i][1], scales, 2 + (c16 >> 3)); }
-                            raw.vs[g][i] = scales;
-                        } else if constexpr (!F32 && MX) {
+                        if constexpr (!F32 && MX) {
                             if (i > lim) { raw.v[4 * g + i] = u32x2{0, 0}; raw.vs[g][i] = 0x7f7f7f7fu; }
                             else if (i > sure) { raw.v[4 * g + i][0] = clean8(raw.v[4 * g + i][0]); raw.v[4 * g + i][1] = clean8(raw.v[4 * g + i][1]); }
                         } else if constexpr (!F32) {
@@ -300,7 +277,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                                 }
                             }
                         } else if constexpr (MX) {
-                            if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; raw.vs[g][i] = 0x7f7f7f7fu; }
+                            if (i > lim) { raw.v[i][0] = raw.v[i][1] = 0; raw.vs[i] = 0x7f7f7f7fu; }
                             else if (i > sure) { raw.v[i][0] = clean8(raw.v[i][0]); raw.v[i][1] = clean8(raw.v[i][1]); }
                         } else {
                             if (i > lim) raw.v[i][0] = raw.v[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -365,8 +342,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                     f32x4 v[2];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        if constexpr (MX4) v[x] = half4f<0>(raw.v[i][x], mx_scale((raw.vs[0][i] >> (16 * x + 8 * (c16 >> 3))) & 0xff));
-                        else if constexpr (MX) v[x] = widen4f(raw.v[i][x], mx_scale((raw.vs[0][i] >> (16 * x + 8 * (c16 >> 3))) & 0xff));
+                        if constexpr (MX) v[x] = widen4f(raw.v[i][x], mx_scale((raw.vs[i] >> (16 * x + 8 * (c16 >> 3))) & 0xff));
                         else v[x] = raw.v[i][x];
                     }
 #pragma unroll
@@ -393,8 +369,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
                         for (int e = 0; e < 4; ++e) {                          // o[][n][e] is this channel's
                             const int ch = F32 ? 64 * (n >> 2) + 4 * (4 * kg + e) + (n & 3) : 8 * (4 * kg + e) + n;
                             float v;
-                            if constexpr (MX4) v = a.cache.vs[row * 4 + (ch >> 5)] == 0xff ? NAN : 0.f;
-                            else if constexpr (MX) {
+                            if constexpr (MX) {
                                 const unsigned b = ((const uint8_t*)a.cache.v)[row * kRowBytes + ch];
                                 v = (b & 0x7f) == 0x7f ? NAN : 0.f;
                             } else if constexpr (F32) v = ((const float*)((const char*)a.cache.v + row * kRowBytes))[ch];
@@ -481,14 +456,14 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || !F32 ? 2 : 1) void paged_rows_
     }
 }
 
-template <bool F32, int HELD, int NQ>
+template <bool F32, bool MX, int NQ>
 hipError_t launch(const PagedArgs& a, hipStream_t st) {
     constexpr int smem = 4 * 16 * NQ * (kHeadDim + 2) * 4;
     if (smem > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void*)paged_rows_kernel<F32, HELD, NQ>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+        const hipError_t e = hipFuncSetAttribute((const void*)paged_rows_kernel<F32, MX, NQ>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((paged_rows_kernel<F32, HELD, NQ>), dim3(a.workgroups), dim3(kThreads), smem, st, a);
+    hipLaunchKernelGGL((paged_rows_kernel<F32, MX, NQ>), dim3(a.workgroups), dim3(kThreads), smem, st, a);
     return hipGetLastError();
 }
 
@@ -498,7 +473,7 @@ int log2_of(int x) { int s = 0; while ((2 << s) <= x) ++s; return s; }        //
 
 PagedRoute paged_route(const CacheShape& sh) {
     PagedRoute r;
-    const bool f32 = sh.dtype == 0, scaled = sh.held != HELD_PLAIN;
+    const bool f32 = sh.dtype == 0, scaled = sh.held != HELD_PLAIN, four = sh.held == HELD_MXFP4;
     // All of these lines were measured at 32/8 heads (fp32: 4/2), and go by rows, units and keys alone.
     // Tiles of 256 rows pay from more than 16 rows on, 8-bit pages from 32; up to 32 rows not for few units and keys (and not where a token alone has more than 16).  us, 32/8 heads, waves that split the keys / tiles of 256 rows:
     // 1 x 4 tokens of 2000 10.8 / 16.1, of 60000 44 / 56, 8 x 4 of 2000 23.6 / 26.3, of 16000 102 / 105; 1 x 8 of 2000 14.1 / 16.3, of 16000 24.6 / 29.1, of 60000 78 / 57, 8 x 8 of 2000
@@ -534,7 +509,7 @@ PagedRoute paged_route(const CacheShape& sh) {
     while (16 * nq < sh.group) nq *= 2;                             // fp32: 33 to 64 query heads a KV head
     r.rows = 16 * nq;
     r.tile_shift = log2_of(r.rows / sh.group);
-    r.step_shift = f32 ? 6 : 7;
+    r.step_shift = f32 && !four ? 6 : 7;
     r.workgroups = nq == 1 || !f32 ? 512 : 256;                     // two to a compute unit, where their registers allow it
     r.least = 1;
     r.setup = 1;
@@ -560,14 +535,14 @@ size_t paged_workspace(const CacheShape& sh) {
 
 hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st) {
     const int nq = route.rows / 16;
-    if (sh.dtype == 0) {
-        if (sh.held == HELD_MXFP4) return nq == 1 ? launch<true, HELD_MXFP4, 1>(a, st) : nq == 2 ? launch<true, HELD_MXFP4, 2>(a, st) : launch<true, HELD_MXFP4, 4>(a, st);
-        if (sh.held == HELD_MXFP8) return nq == 1 ? launch<true, HELD_MXFP8, 1>(a, st) : nq == 2 ? launch<true, HELD_MXFP8, 2>(a, st) : launch<true, HELD_MXFP8, 4>(a, st);
-        return nq == 1 ? launch<true, HELD_PLAIN, 1>(a, st) : nq == 2 ? launch<true, HELD_PLAIN, 2>(a, st) : launch<true, HELD_PLAIN, 4>(a, st);
-    }
     if (sh.held == HELD_MXFP4) return launch_paged_fp4(sh, route, a, st);
-    if (sh.held == HELD_MXFP8) return nq == 1 ? launch<false, HELD_MXFP8, 1>(a, st) : launch<false, HELD_MXFP8, 2>(a, st);
-    return launch<false, HELD_PLAIN, 1>(a, st);
+    const bool mx = sh.held == HELD_MXFP8;
+    if (sh.dtype == 0) {
+        if (mx) return nq == 1 ? launch<true, true, 1>(a, st) : nq == 2 ? launch<true, true, 2>(a, st) : launch<true, true, 4>(a, st);
+        return nq == 1 ? launch<true, false, 1>(a, st) : nq == 2 ? launch<true, false, 2>(a, st) : launch<true, false, 4>(a, st);
+    }
+    if (mx) return nq == 1 ? launch<false, true, 1>(a, st) : launch<false, true, 2>(a, st);
+    return launch<false, false, 1>(a, st);
 }
 
 hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,

@@ -1,14 +1,16 @@
-// Attention of the new tokens of each sequence over pages of 4 bits, for few rows a KV head and bf16: the formulas, tiles and operand layouts of attn_paged.hip (S^T = K . Q^T and
-// O^T += V^T . P^T in 16x16 MFMAs, waves split the keys, nothing by way of LDS before the merge), with a key loop for half of the 8-bit bytes.
+// Attention of the new tokens of each sequence over pages of 4 bits, for few rows a KV head and for fp32: the formulas, tiles and operand layouts of attn_paged.hip (S^T = K . Q^T and
+// O^T += V^T . P^T in 16x16 MFMAs, waves split the keys, nothing but fp32 queries by way of LDS before the merge), with a key loop for half of the 8-bit bytes.
 //
 //   K   a lane takes one key's 32 channels of one scale, 16 bytes, and makes them bf16 (exact) by 16 conversions that apply the scale
 //   V   a lane takes 8 channels of 8 tokens, 4 bytes each; 32 conversions, and 32 v_perm that bring two tokens' together
 //   e2m1 has no NaN: what may be one is seen in the scales alone, and a key that no row sees needs no zeros in place of its V
+//   fp32: Q and P as three bf16 pieces of 8 bits, exactly, so that a product is three bf16 MFMAs where one in fp32 takes the time of 16, with sums in fp32 as there
 //
 // A step's loads are half as many bytes as over 8-bit pages for as much work, so what a wave waits for counts: K of the next step is asked for when QK has read this one's, V when
 // PV has, and neither by a branch.  Where the loads stand behind a branch the compiler has to wait for all of them at the first use of any (one token of 10^6 keys 203 us, 64 of 8000 108; without
 // 195 and 103, and past the caches 170 and 91).  Not kept: two steps at a time (64 single tokens of all lengths up to 32769: 90 us for 72, units are short), three workgroups to a
 // compute unit (64 of 8000: 101 us for 91), K as 4-bit operand of a scaled MFMA with Q in two e4m3 pieces (its sums are good to 2^-17 of their terms only).
+// fp32 with its own MFMAs, 4/2 heads: 3 x up to 200 tokens after 3000 34.5 us, with pieces 20.9; 20 x 200 after 8000 682 and 256; 8/2 heads: 8 x 1 of 20000 37.0 and 19.5.
 #include "paged.h"
 
 #include <type_traits>
@@ -46,6 +48,22 @@ __device__ __forceinline__ float column_sum(float x) {
 __device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {
     return u32x4{as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
                  as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+// Eight fp32 as sums of three bf16 each, exactly: 8 of the 24 bits to a piece, cut off and not rounded, so that the largest stay finite.
+__device__ __forceinline__ void split8(f32x4 lo, f32x4 hi, bf16x8* piece) {
+    u32x4 w[3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float x = e < 2 ? lo[2 * e] : hi[2 * e - 4], y = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const unsigned p = __float_as_uint(x), q = __float_as_uint(y);
+            w[i][e] = __builtin_amdgcn_perm(q, p, 0x07060302u);
+            x -= __uint_as_float(p & 0xffff0000u); y -= __uint_as_float(q & 0xffff0000u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) piece[i] = as_bf16x8(w[i]);
 }
 // Elements go past the caches: a call reads them once.  us, ordinary loads / past the caches (32/8 heads, pages of 64, caches that no other call has left in the chip): one token of 8000 keys
 // 12.5 / 11.4, of 131072 34.6 / 31.2, of 10^6 194.9 / 170.0; 8 of 2000 15.1 / 14.1, 64 of 8000 102.6 / 91.5.  Scales, 16 tokens' to 64 bytes, by ordinary loads.
@@ -93,8 +111,10 @@ __device__ __forceinline__ bool next_unit(const PagedArgs& a, Run<false>& run) {
 enum { NOTHING = 0, SAME_UNIT = 1, NEXT_UNIT = 2 };
 
 // SMALL: pages of 16 tokens, of which a wave's keys of a step lie in two.
-template <int NQ, bool SMALL>
-__global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
+template <typename T, int NQ, bool SMALL>
+__global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void paged_fp4_kernel(PagedArgs a) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int kPieces = F32 ? 3 : 1;
     constexpr int kRows = 16 * NQ, kGroups = kWaveKeys / 16, RUNS = SMALL ? 2 : 1, kRunGroups = kGroups / RUNS;
     extern __shared__ __attribute__((aligned(16))) float merge[];              // [wave][row][128], then (max, sum) [wave][row]
     float* const wave_stats = merge + 4 * kRows * kHeadDim;
@@ -147,14 +167,35 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
             rvs[g] = *(const u32x4*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
         }
     };
-    bf16x8 qf[NQ][4];                                                          // lane's column is a row, 8 channels at 32 kg + 8 ks
+    // Lane's column is a row, 8 channels at 32 kg + 8 ks: of bf16 in registers; the pieces of fp32, three times as many, in LDS, once for the four waves, where the merge comes later.
+    bf16x8 qf[NQ][F32 ? 1 : 4];
+    bf16x8* const q_pieces = (bf16x8*)merge + lane;                            // [nq][ks][piece][lane]
+    auto q_part = [&](const Unit& n, int nq, int ks) __attribute__((always_inline)) {
+        const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, n.live - 1), g = r - of * a.group;
+        return (const T*)a.q + (int64_t)(n.row + t) * a.qs0 + (int64_t)(n.head * a.group + g) * a.qs1 + 32 * kg + 8 * ks;
+    };
     auto load_q = [&](const Unit& n) __attribute__((always_inline)) {
+        if constexpr (F32) {
+            f32x4 x[NQ][2];
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq) {
-            const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, n.live - 1), g = r - of * a.group;
-            const int64_t from = (int64_t)(n.row + t) * a.qs0 + (int64_t)(n.head * a.group + g) * a.qs1 + 32 * kg;
+            for (int nq = 0; nq < NQ; ++nq) {
+                const T* from = q_part(n, nq, wave);
+                x[nq][0] = *(const f32x4*)from; x[nq][1] = *(const f32x4*)(from + 4);
+            }
+            __syncthreads();                                                   // the unit before has been read
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)((const __bf16*)a.q + from + 8 * ks);
+            for (int nq = 0; nq < NQ; ++nq) {
+                bf16x8 piece[3];
+                split8(x[nq][0], x[nq][1], piece);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) q_pieces[((nq * 4 + wave) * 3 + i) * 64] = piece[i];
+            }
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)q_part(n, nq, ks);
         }
     };
     auto begin = [&](const Unit& n) __attribute__((always_inline)) {
@@ -168,8 +209,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
         look_up(n, 1);
     };
     // The first step of the next unit is asked for in this one's last: what a unit begins and ends with, some 3 us, passes meanwhile (64 single tokens of up to 32769 keys 73.7 us, now 66.9).
-    // With 32 rows there are no registers for it.
-    constexpr bool kAcross = NQ == 1;
+    // With 32 rows there are no registers for it, and with fp32 the queries' place is the merge's.
+    constexpr bool kAcross = NQ == 1 && !F32;
     Unit now = unit_of(a, run);
     begin(now);
 
@@ -206,7 +247,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 for (int ks = 0; ks < 4; ++ks) {
                     const bf16x8 kw = as_bf16x8(widen8(rk[g][ks], scale));
 #pragma unroll
-                    for (int nq = 0; nq < NQ; ++nq) s[nq][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, qf[nq][ks], s[nq][g], 0, 0, 0);
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int i = kPieces - 1; i >= 0; --i) {
+                            const bf16x8 q = F32 ? q_pieces[((nq * 4 + ks) * 3 + i) * 64] : qf[nq][F32 ? 0 : ks];
+                            s[nq][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, q, s[nq][g], 0, 0, 0);
+                        }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -229,7 +275,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                     }
                 }
             }
-            bf16x8 pf[NQ];
+            bf16x8 pf[NQ][kPieces];
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
                 float mx = -INFINITY;
@@ -243,14 +289,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 const float ms = m_safe * c;
                 m_run[nq] = m_new;
                 float sum = 0.f;
+                f32x4 p4[kGroups];
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[nq][g][i], c, -ms));
                         sum += p;                                              // before P is rounded for the product: lse is as exact as fp32 allows
-                        pf[nq][4 * g + i] = (__bf16)p;
+                        if constexpr (F32) p4[g][i] = p;
+                        else pf[nq][0][4 * g + i] = (__bf16)p;
                     }
+                if constexpr (F32) split8(p4[0], p4[1], pf[nq]);
                 l_run[nq] = l_run[nq] * alpha + sum;
                 if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
@@ -285,7 +334,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(v[2 * e + 1][n >> 1], v[2 * e][n >> 1], n & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-                for (int nq = 0; nq < NQ; ++nq) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pf[nq], o[nq][n], 0, 0, 0);
+                for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                    for (int x = kPieces - 1; x >= 0; --x) o[nq][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), pf[nq][x], o[nq][n], 0, 0, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (asks.value != NOTHING) load_v();
@@ -367,10 +418,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
                 const int64_t row = now.row + t;
                 const int h = now.head * a.group + g;
                 const int64_t to = row * a.os0 + h * a.os1 + 8 * piece;
-                bf16x8 w;
+                if constexpr (F32) {
+                    *(f32x4*)((float*)a.out + to) = f32x4{sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+                    *(f32x4*)((float*)a.out + to + 4) = f32x4{sum[4] * inv, sum[5] * inv, sum[6] * inv, sum[7] * inv};
+                } else {
+                    bf16x8 w;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (__bf16)(sum[e] * inv);
-                *(bf16x8*)((__bf16*)a.out + to) = w;
+                    for (int e = 0; e < 8; ++e) w[e] = (__bf16)(sum[e] * inv);
+                    *(bf16x8*)((__bf16*)a.out + to) = w;
+                }
                 if (a.lse && piece == 0) a.lse[row * a.hq + h] = L == 0.f ? -INFINITY : M * a.scale + logf(L);
             } else {
                 float* to = a.parts + (slot * kRows + r) * kHeadDim + 8 * piece;
@@ -395,18 +451,24 @@ __global__ __launch_bounds__(kThreads, 2) void paged_fp4_kernel(PagedArgs a) {
     }
 }
 
-template <int NQ, bool SMALL>
+template <typename T, int NQ, bool SMALL>
 hipError_t launch(const PagedArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((paged_fp4_kernel<NQ, SMALL>), dim3(a.workgroups), dim3(kThreads), 4 * 16 * NQ * (kHeadDim + 2) * 4, st, a);
+    constexpr int smem = 4 * 16 * NQ * (kHeadDim + 2) * 4;
+    if (smem > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)paged_fp4_kernel<T, NQ, SMALL>, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((paged_fp4_kernel<T, NQ, SMALL>), dim3(a.workgroups), dim3(kThreads), smem, st, a);
     return hipGetLastError();
 }
+template <typename T, int NQ>
+hipError_t launch_pages(const CacheShape& sh, const PagedArgs& a, hipStream_t st) { return sh.page_shift < 5 ? launch<T, NQ, true>(a, st) : launch<T, NQ, false>(a, st); }
 
 }  // namespace
 
 hipError_t launch_paged_fp4(const CacheShape& sh, const PagedRoute& route, const PagedArgs& a, hipStream_t st) {
-    const bool small = sh.page_shift < 5;
-    if (route.rows == 16) return small ? launch<1, true>(a, st) : launch<1, false>(a, st);
-    return small ? launch<2, true>(a, st) : launch<2, false>(a, st);
+    if (sh.dtype == 1) return route.rows == 16 ? launch_pages<__bf16, 1>(sh, a, st) : launch_pages<__bf16, 2>(sh, a, st);
+    return route.rows == 16 ? launch_pages<float, 1>(sh, a, st) : route.rows == 32 ? launch_pages<float, 2>(sh, a, st) : launch_pages<float, 4>(sh, a, st);
 }
 
 }  // namespace cp
