@@ -159,7 +159,7 @@ int critiprefill_dense_causal_attn(const critiprefill_params *p, const void *q, 
  * CP_CACHE_MXFP4: a row is 128 OCP e2m1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), 64 bytes, the even channel of two in the lower half of their byte, and
  * scales as above: 2^e is the smallest with max |x| <= 7 * 2^e, e in 2 .. 252.  An element is rounded to the nearest, ties to the even code; what lies above 6 is off by a unit at
  * most, no more than rounding costs between 4 and 6, where the next scale's steps would be two units.  (e == 252 alone holds larger maxima, as 6 * 2^125.)  32 channels that
- * are not all finite have e = 255 and are NaN together; that is what e = 255 stands for under any elements.
+ * are not all finite have e = 255 and are NaN together; that is what e = 255 stands for under any elements.  253 and 254 no write gives: what a row that sees a token with them gets has no meaning.
  * A token's place is its slot, page * page_size + offset; a token whose slot is not in 0 .. n_pages * page_size - 1 has no place: it is
  * not written, and read as zeros.  Two tokens of one written call must not have the same slot: what it then holds is made of both.
  *

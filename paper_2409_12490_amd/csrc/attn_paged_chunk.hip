@@ -475,7 +475,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {                       // channels 8 j + 4 hh ..
                     unsigned w[2];
-                    if (MX4) w[0] = w[1] = a.cache.vs[row * 4 + (j >> 2)] == 0xff ? 0x7fc07fc0u : 0u;
+                    if (MX4) w[0] = w[1] = a.cache.vs[row * 4 + (j >> 2)] >= kFarScale ? 0x7fc07fc0u : 0u;
                     else if (MX) {
                         const unsigned b = *(const unsigned*)((const char*)a.cache.v + row * 128 + 8 * j + 4 * hh);
                         const float scale = __uint_as_float((unsigned)a.cache.vs[row * 4 + (j >> 2)] << 23);

@@ -3,7 +3,7 @@
 //
 //   K   a lane takes one key's 32 channels of one scale, 16 bytes, and makes them bf16 (exact) by 16 conversions that apply the scale
 //   V   a lane takes 8 channels of 8 tokens, 4 bytes each; 32 conversions, and 32 v_perm that bring two tokens' together
-//   e2m1 has no NaN: what may be one is seen in the scales alone, and a key that no row sees needs no zeros in place of its V
+//   e2m1 has no infinity or NaN: what may become one is seen in the scales alone, and a key that no row sees needs no zeros in place of its V
 //   fp32: Q and P as three bf16 pieces of 8 bits, exactly, so that a product is three bf16 MFMAs where one in fp32 takes the time of 16, with sums in fp32 as there
 //
 // A step's loads are half as many bytes as over 8-bit pages for as much work, so what a wave waits for counts: K of the next step is asked for when QK has read this one's, V when
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
                     for (int n = 0; n < 8; ++n) o[nq][n] *= alpha;
                 }
             }
-            // A weight of 0 keeps everything of a hidden key out of a sum but NaN, which only a scale can bring: it becomes another there.  `odd` says that some rows see
-            // such a key and others do not; the unit's end adds it for those that do.
+            // A weight of 0 keeps everything of a hidden key out of a sum but what is not finite, which only scales from 253 on can bring (4 * 2^126 is infinite): they become others there.
+            // `odd` says that some rows see such a key and others do not; the unit's end makes it NaN for those that do.
             unsigned scales[kGroups][4];
 #pragma unroll
             for (int g = 0; g < kGroups; ++g)
@@ -320,8 +320,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
                     const int lim = seen[r] > 0 ? high - u : -1, sure = seen[r] > 0 ? low - u : -1;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const bool nan = (scales[g][i] & 0x7f800000u) == 0x7f800000u;
-                        if (i > sure && nan) { scales[g][i] = 0x3f800000u; if (i <= lim) odd = true; }
+                        const bool far = (scales[g][i] & 0x7f800000u) >= kFarScale << 23;
+                        if (i > sure && far) { scales[g][i] = 0x3f800000u; if (i <= lim) odd = true; }
                     }
                 }
             }
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
                     const int64_t row = (((int64_t)page * a.hkv + now.head) << a.page_shift) + (u & page_mask);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {                              // channels 32 kg + 8 e ..
-                        if (a.cache.vs[row * 4 + kg] != 0xff) continue;
+                        if (a.cache.vs[row * 4 + kg] < kFarScale) continue;
 #pragma unroll
                         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll

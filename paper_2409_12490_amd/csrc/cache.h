@@ -6,6 +6,7 @@ namespace cp {
 
 // How the cache holds a row: elements of dtype, or e4m3 or e2m1 elements with a scale per 32 channels.
 enum { HELD_PLAIN = 0, HELD_MXFP8 = 1, HELD_MXFP4 = 2 };
+constexpr unsigned kFarScale = 253;           // of e2m1: the first scale under which elements are infinite; no write gives it or the next, 255 is NaN's
 constexpr int row_bytes(int held, int element) { return held == HELD_MXFP4 ? kHeadDim / 2 : held == HELD_MXFP8 ? kHeadDim : kHeadDim * element; }
 
 // The parameter block of the cache operators, checked.

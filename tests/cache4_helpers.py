@@ -9,7 +9,7 @@ from tests.cache_helpers import DEV, Pool, f64
 
 
 class Pool4(Pool):
-    """A Pool whose pages hold 4 bits: what no token lies in has any elements and the scale of NaN."""
+    """A Pool whose pages hold 4 bits: what no token lies in has any elements, and scales under which these are infinite or NaN."""
 
     def __init__(self, gen, lengths, hkv, page, dtype="bf16", spare=3, scale=1.0):
         super().__init__(gen, lengths, hkv, page, dtype, False, spare, scale)
@@ -20,7 +20,8 @@ class Pool4(Pool):
         (kc, ks), (vc, vs) = (O.mx4_quantise(f64(x)) for x in (self.k, self.v))
         fill = lambda x, w: torch.where(used, torch.from_numpy(x), torch.tensor(w, dtype=torch.uint8))   # noqa: E731
         self.held_k, self.held_v = (torch.where(used, torch.from_numpy(O.mx4_values(c, s)), float("nan")).numpy() for c, s in ((kc, ks), (vc, vs)))
-        self.cache = [fill(kc, 0x7a).to(DEV), fill(vc, 0xf1).to(DEV), fill(ks, 0xff).to(DEV), fill(vs, 0xff).to(DEV)]
+        far = torch.randint(253, 256, (2, *ks.shape), generator=gen, dtype=torch.uint8)
+        self.cache = [fill(kc, 0x7a).to(DEV), fill(vc, 0xf1).to(DEV)] + [torch.where(used, torch.from_numpy(s), f).to(DEV) for s, f in zip((ks, vs), far)]
 
     def spoil(self, which, page, head, offset, block):
         """32 channels of a token's K (0) or V (1) become NaN."""
