@@ -481,6 +481,9 @@ PagedRoute paged_route(const CacheShape& sh) {
     const long long want = (long long)sh.max_q * sh.group;
     const double heads = (double)sh.n_seqs * sh.hkv;
     r.chunk = !f32 && want > (scaled ? 32 : 16) && !(sh.group <= 16 && want <= 32 && heads <= 8 && sh.max_kv <= 24576);
+    // Over pages of 4 bits tiles of 32 rows, as many as it takes, pay further: 1 x 16 tokens of 2000 13.4 / 15.7, of 60000 37.5 / 59.1, 8 x 16 of 8000 40.2 / 63.8, 32 x 16 of 4000 63.7 / 106; 1 x 32
+    // of 2000 15.4 / 17.7, of 60000 59.0 / 61.3, 4 x 32 of 2000 26.6 / 24.5, 32 x 32 of 4000 114 / 106; 1 x 64 of 2000 18.2 / 23.4, of 16000 40.3 / 39.2; 32/4 heads 16 x 8 of 6000 34.3 / 52.0.
+    if (four && !f32) r.chunk = sh.group > 32 || want > (heads > 8 ? 64 : sh.max_kv > 4096 ? 128 : 256);
     // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.1 / 7.8, after 509 10.2 / 10.1, after 999 10.2 / 14.7;
     // fp32 (steps of half as many keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760
     // 13.0 / 12.5, of 1000 15.6 / 15.9, 32 x 1 of 760 26.0 / 19.5, 8 bits 8 x 1 of 760 12.6 / 10.7, of 1000 14.0 / 12.3, of 1500 14.2 / 16.4, 32 x 1 of 1000 22.2 / 15.8 (a single long
@@ -514,6 +517,16 @@ PagedRoute paged_route(const CacheShape& sh) {
     r.least = 1;
     r.setup = 1;
     r.whole = sh.max_kv <= brief;
+    if (four) {
+        // What a unit takes beside its steps, in bf16: 64 x 1 of up to 32769 keys 64.7 us with 1, 62.4 with 2, 63.4 with 3; 30 x 2 of up to 20000 32.4, 30.6, 31.4; fp32 (4/2 heads) 3 x 200 of up
+        // to 3200 20.4, 21.0, 21.0.
+        r.setup = f32 ? 1 : 2;
+        // Short sequences by the number of units, cut / whole.  Fewer than 64: 1 x 1 of 768 9.9 / 8.8, 1 x 4 of 900 9.9 / 10.6, 1 x 16 of 900 11.7 / 13.0.  64 to 127: 8 x 1 of 1024 12.2 / 10.8, of 1536
+        // 12.4 / 14.0, 8 x 4 of 1500 15.4 / 14.6.  128 to 255: 8 x 16 of 1500 23.5 / 17.7.  More: 32 x 1 of 2048 21.9 / 18.7, of 3072 26.9 / 25.4, 32 x 4 of 2000 31.7 / 19.1, 64 x 1 of up to 2000 16.0 / 16.8.
+        // fp32, 4/2 and 8/2 heads: 1 x 1 of 512 10.7 / 8.2, 1 x 50 of 600 10.9 / 11.2; 8 x 50 of 700 16.7 / 12.0, 64 x 1 of 1024 14.8 / 13.4, of 1500 16.3 / 17.9; 8 x 200 of 800 33.0 / 18.6.
+        const double units = heads * (((long long)sh.max_q + (1 << r.tile_shift) - 1) >> r.tile_shift);
+        r.whole = sh.max_kv <= (units < 64 ? (f32 ? 512 : 768) : units < 128 || (f32 && units < 256) ? 1024 : units < 256 ? 1536 : 2048);
+    }
     return r;
 }
 
