@@ -144,11 +144,20 @@ __device__ __forceinline__ unsigned quantise8_to_4(const float (&x)[8], int& exp
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
+// Rows of 4 bits are half a line of L2, 64 bytes, and a token's scales of a head 4 of a line that 32 tokens share.  They are written and read by ordinary accesses, which bring a line together, whatever the
+// tensors do, and lines' tokens come to one XCD.  32/8 heads, us, past the caches and tokens dealt over the XCDs / ordinary / and together: 65536 tokens back 72.1 / 54.1 / 49.8, written and
+// back 148.9 / 130.5 / 123.4, 8192 back 9.3 / 9.2 / 8.8.
+// Of 8 * kTogether neighbouring workgroups the first kTogether on an XCD, whichever these are: 32 tokens, whose scales of a head fill a line of its L2.  What is left over stays as it is.
+constexpr unsigned kTogether = 8;
+__device__ __forceinline__ unsigned by_xcd(unsigned b, unsigned blocks) {
+    return b < blocks / (8 * kTogether) * (8 * kTogether) ? b / (8 * kTogether) * (8 * kTogether) + (b & 7) * kTogether + (b >> 3) % kTogether : b;
+}
+
 template <typename T, int TURN, int TO, bool STREAM>
 __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
     __shared__ f32x2 turns[4][64];                                 // (cos, sin) of the wave's token
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15;
-    const unsigned index = blockIdx.x * 4u + wave;
+    const unsigned index = (TO == TO_MXFP4 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x) * 4u + wave;
     const int token = __builtin_amdgcn_readfirstlane((int)(index / (unsigned)a.waves));
     const int part = (int)index - token * a.waves;
     if (token >= a.tokens) return;                                 // no barrier below: a wave's exchange is its own
@@ -189,7 +198,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
         const T* from = kind == 0 ? (const T*)a.q + token * a.qs0 + h * a.qs1
                                   : (kind == 1 ? (const T*)a.k + token * a.ks0 + h * a.ks1 : (const T*)a.v + token * a.vs0 + h * a.vs1);
         float x[8];
-        load8<STREAM>(from + 8 * c16, x);
+        // fp32 for 4 bits: two instructions share a line.  8/2 heads: 16000 tokens with norms 37.7 us past the caches, 35.5 by ordinary loads; 60000 tokens of 8 heads written 121 and 115
+        load8<STREAM && (TO != TO_MXFP4 || sizeof(T) == 2)>(from + 8 * c16, x);
         if (TURN != TURN_NONE || TO == TO_TENSOR) {
             if (kind < 2 && (kind ? a.kw : a.qw)) {
                 float sq = 0.f;
@@ -236,7 +246,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
                 int e;
                 const unsigned w = quantise8_to_4(x, e);
                 if (kept) {
-                    put<STREAM>((uint8_t*)(kind == 1 ? a.cache.k : a.cache.v) + row * (kHeadDim / 2) + 4 * c16, w);
+                    put<false>((uint8_t*)(kind == 1 ? a.cache.k : a.cache.v) + row * (kHeadDim / 2) + 4 * c16, w);
                     if ((c16 & 3) == 0) (kind == 1 ? a.cache.ks : a.cache.vs)[row * 4 + (c16 >> 2)] = (uint8_t)e;
                 }
             } else {
@@ -254,7 +264,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(RopeArgs a) {
 template <typename T, int HELD, bool STREAM>
 __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15;
-    const unsigned index = blockIdx.x * 4u + wave;
+    const unsigned index = (HELD == HELD_MXFP4 ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x) * 4u + wave;
     const int token = __builtin_amdgcn_readfirstlane((int)(index / (unsigned)a.waves));
     const int part = (int)index - token * a.waves;
     if (token >= a.tokens) return;
@@ -269,10 +279,19 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
         for (int e = 0; e < 8; ++e) x[e] = 0.f;                    // a token without a place in the cache
         if (held) {
             if (HELD == HELD_MXFP4) {
-                const unsigned w = get<STREAM, unsigned>((const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * (kHeadDim / 2) + 4 * c16);
-                const float scale = __uint_as_float((unsigned)(is_v ? a.cache.vs : a.cache.ks)[row * 4 + (c16 >> 2)] << 23);       // of 255: NaN
-                const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1),
-                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3)};
+                // of fp32 channels 4 c16 .. and 64 + 4 c16 .., so that a store writes whole lines: 20000 tokens of 8 heads 48.9 us with 8 c16 .., now 31
+                const uint8_t* from = (const uint8_t*)(is_v ? a.cache.v : a.cache.k) + row * (kHeadDim / 2);
+                const uint8_t* scales = (is_v ? a.cache.vs : a.cache.ks) + row * 4;
+                unsigned w; float s0, s1;
+                if (sizeof(T) == 4) {
+                    w = *(const uint16_t*)(from + 2 * c16) | (unsigned)*(const uint16_t*)(from + 32 + 2 * c16) << 16;
+                    s0 = __uint_as_float((unsigned)scales[c16 >> 3] << 23); s1 = __uint_as_float((unsigned)scales[2 + (c16 >> 3)] << 23);
+                } else {
+                    w = *(const unsigned*)(from + 4 * c16);
+                    s0 = s1 = __uint_as_float((unsigned)scales[c16 >> 2] << 23);                   // of 255: NaN
+                }
+                const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s0, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s0, 1),
+                                    __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s1, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s1, 3)};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = y[e >> 1][e & 1];
             } else if (HELD == HELD_MXFP8) {
@@ -287,7 +306,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RopeArgs a) {
                 load8<STREAM>((const T*)(is_v ? a.cache.v : a.cache.k) + row * kHeadDim + 8 * c16, x);
             }
         }
-        store8<STREAM>((T*)(is_v ? a.q_out : a.k_out) + token * (is_v ? a.vs0 : a.ks0) + h * (is_v ? a.vs1 : a.ks1) + 8 * c16, x);
+        T* const to = (T*)(is_v ? a.q_out : a.k_out) + token * (is_v ? a.vs0 : a.ks0) + h * (is_v ? a.vs1 : a.ks1);
+        if (HELD == HELD_MXFP4 && sizeof(T) == 4) {
+            put<STREAM>(to + 4 * c16, f32x4{x[0], x[1], x[2], x[3]});
+            put<STREAM>(to + 64 + 4 * c16, f32x4{x[4], x[5], x[6], x[7]});
+        } else store8<STREAM>(to + 8 * c16, x);
     }
 }
 
@@ -334,7 +357,11 @@ hipError_t launch_write(const RopeArgs& a, int held, bool stream, hipStream_t st
 }
 template <typename T>
 hipError_t launch_back(const RopeArgs& a, int held, bool stream, hipStream_t st) {
-    return held == HELD_MXFP4 ? launch_read<T, HELD_MXFP4>(a, stream, st) : held == HELD_MXFP8 ? launch_read<T, HELD_MXFP8>(a, stream, st) : launch_read<T, HELD_PLAIN>(a, stream, st);
+    if (held == HELD_MXFP4) {
+        hipLaunchKernelGGL((cache_read_kernel<T, HELD_MXFP4, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
+    return held == HELD_MXFP8 ? launch_read<T, HELD_MXFP8>(a, stream, st) : launch_read<T, HELD_PLAIN>(a, stream, st);
 }
 
 }  // namespace
@@ -366,7 +393,8 @@ hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v
 hipError_t launch_cache_read(const CacheShape& sh, const int32_t* slots, const CachePtr& cache, void* k, void* v, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.slots = slots; a.k_out = k; a.q_out = v;
-    const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
+    // From 4 bits the tensors are nearly all that moves, and go past the caches at any size: 8 heads in bf16, 4000 tokens 8.5 / 6.8 us, 8000 12.1 / 8.5, 30000 36.6 / 24.1, in fp32 4000 12.6 / 8.9.
+    const bool stream = sh.held == HELD_MXFP4 || cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
     return sh.dtype == 1 ? launch_back<__bf16>(a, sh.held, stream, st) : launch_back<float>(a, sh.held, stream, st);
 }
 
