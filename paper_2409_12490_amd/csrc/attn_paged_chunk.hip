@@ -20,12 +20,9 @@
 #include "paged.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace cp {
 namespace {
-
-typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 
 constexpr int kChunkRows = 256, WQ = 32, TK = 64, NBUF = 4;
 constexpr int kTileBytes = TK * 256;
@@ -43,11 +40,13 @@ __device__ __forceinline__ u32x4 widen8(unsigned w0, unsigned w1, float scale) {
     return r;
 }
 
-// half h of 16 channels as a thread has them of a row, to bf16: e4m3, e2m1 (a scale of 255 makes them NaN)
-__device__ __forceinline__ u32x4 widen_half(u32x4 x, int h, float scale) { return widen8(x[2 * h], x[2 * h + 1], scale); }
-__device__ __forceinline__ u32x4 widen_half(u32x2 x, int h, float scale) {
-    return u32x4{packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 0)), packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 1)),
-                 packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 2)), packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[h], scale, 3))};
+__device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {                    // eight e2m1 to bf16; a scale of 255 makes them NaN
+    u32x4 r;
+    r[0] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+    r[1] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+    r[2] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+    r[3] = packed(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    return r;
 }
 
 // All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
@@ -58,7 +57,7 @@ __device__ __forceinline__ u32x4 widen_half(u32x2 x, int h, float scale) {
 template <int HELD, int RUNS, bool ROTATED>
 __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
     constexpr bool MX = HELD != HELD_PLAIN, MX4 = HELD == HELD_MXFP4;
-    constexpr int kRowBytes = row_bytes(HELD, 2);
+    constexpr int kRowBytes = row_bytes(HELD, 2);                  // of 4 bits
     const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
     if (thread_id() == 0) *LDS_PTR(unsigned, lds0 + kOddOff) = 0;
     __syncthreads();
@@ -77,8 +76,9 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
             v_addr[dt] = lds0 + kVOff + (4 * hh + (i16 >> 2)) * 256 + ((((unsigned)(dt ^ (i16 >> 2)) << 2) + 2 * gbit + ((i16 & 3) >> 1)) << 4) + (i16 & 1) * 8;
         // copies: wave w fills rows 4 w .. 4 w + 3 and 32 + 4 w .. of a tile; physical chunk pch of row r4
         const unsigned lane_k = (unsigned)r4 * 256 + (unsigned)(pch ^ ((4 * wave + r4) & 15)) * 16, lane_v = (unsigned)r4 * 256 + (unsigned)(pch ^ (4 * r4)) * 16;
-        // 8 and 4 bits: thread tid has 16 channels 16 * (tid & 7) of row tid >> 3
-        const int xrow = tid >> 3, xpiece = tid & 7;
+        // 8 bits: thread tid has 16 channels 16 * (tid & 7) of row tid >> 3 of K and V.  4 bits: the 32 channels 32 * (tid & 3), those of a scale, of row tid / 4, of K (waves 0-3) or V (4-7).
+        const int xrow = MX4 ? (tid & 255) >> 2 : tid >> 3, xpiece = MX4 ? tid & 3 : tid & 7;
+        const unsigned turned = (unsigned)(xrow & 3) * 4;            // 4 bits: V's words are taken in the order w ^ (row & 3), and so are K's, by their swizzle: eight lanes write to all banks
 
         const Sequence seq = run.now;
         const int t0 = run.tile << a.tile_shift, live = min(1 << a.tile_shift, seq.tokens - t0), head = run.head;
@@ -127,7 +127,12 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
                 page[g] = there ? entry[g] : 0;                      // keys that are not there are read from page 0 and hidden
             }
             // the wave's rows: 4 * wave .. + 3 and 32 + 4 * wave .. + 3, or 8 * wave .. + 7
-            if (MX) {
+            if constexpr (MX4) {                                     // rows 16 * (wave & 3) .. + 15
+                int p = page[0];
+#pragma unroll
+                for (int g = 1; g < RUNS; ++g) p = (wave & 3) / (4 / RUNS) == g ? page[g] : p;
+                at[0] = (((int64_t)p * a.hkv + head) << a.page_shift) + ((base0 + x * TK + 16 * (wave & 3)) & mask);
+            } else if (MX) {
                 int p = page[0];
 #pragma unroll
                 for (int g = 1; g < RUNS; ++g) p = wave / (8 / RUNS) == g ? page[g] : p;
@@ -183,24 +188,46 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
                 *LDS_PTR(u32x4, at) = clean(*LDS_PTR(const u32x4, at), base(x) + row, (bits >> (row >> 4)) & 1);
             }
         };
-        // 8 and 4 bits: the tile in flight
-        typedef typename std::conditional<MX4, u32x2, u32x4>::type raw_row;
-        raw_row raw_k, raw_v; unsigned scale_k = 0, scale_v = 0;
+        // 8 and 4 bits: the tile in flight; of 4 bits K or V are in raw_k
+        u32x4 raw_k, raw_v; unsigned scale_k = 0, scale_v = 0;
         auto load_raw = [&]() __attribute__((always_inline)) {       // of the tile described last
-            const unsigned in_rows = (unsigned)lane * (kRowBytes / 8), in_scales = (unsigned)(lane >> 3) * 4 + (unsigned)((lane & 7) >> 1);   // eight rows of a wave
-            raw_k = *(const raw_row*)(uniform_ptr((const char*)a.cache.k + at[0] * kRowBytes) + in_rows);
-            raw_v = *(const raw_row*)(uniform_ptr((const char*)a.cache.v + at[0] * kRowBytes) + in_rows);
+            if constexpr (MX4) {
+                const char* from = uniform_ptr((const char*)(ROTATED ? a.cache.v : a.cache.k) + at[0] * kRowBytes);
+                const unsigned in_rows = (unsigned)lane * 16;
+                if constexpr (!ROTATED) raw_k = *(const u32x4*)(from + in_rows);
+                else {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) raw_k[w] = *(const unsigned*)(from + (in_rows + (turned ^ 4 * w)));
+                }
+                scale_k = (uniform_ptr((ROTATED ? a.cache.vs : a.cache.ks) + at[0] * 4))[(unsigned)lane];
+                return;
+            }
+            const unsigned in_rows = (unsigned)lane * 16, in_scales = (unsigned)(lane >> 3) * 4 + (unsigned)((lane & 7) >> 1);   // eight rows of a wave
+            raw_k = *(const u32x4*)(uniform_ptr((const char*)a.cache.k + at[0] * 128) + in_rows);
+            raw_v = *(const u32x4*)(uniform_ptr((const char*)a.cache.v + at[0] * 128) + in_rows);
             scale_k = (uniform_ptr(a.cache.ks + at[0] * 4))[in_scales];
             scale_v = (uniform_ptr(a.cache.vs + at[0] * 4))[in_scales];
         };
         auto store_raw = [&](int x, int bits, int slot) __attribute__((always_inline)) {
+            if constexpr (MX4) {
+                const float scale = __uint_as_float(scale_k << 23);
+                const unsigned to = lds0 + (ROTATED ? kVOff : kKOff) + slot * kTileBytes + xrow * 256 + (((unsigned)(4 * xpiece) ^ (ROTATED ? 5u * (xrow & 3) : (unsigned)(xrow & 15))) << 4);
+                const bool part = ROTATED && partly(x, bits), there = ROTATED && ((bits >> (xrow >> 4)) & 1);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    u32x4 v = widen8(raw_k[w], scale);
+                    if (part) v = clean(v, base(x) + xrow, there);
+                    *LDS_PTR(u32x4, to ^ (w << 4)) = v;
+                }
+                return;
+            }
             const float sk = __uint_as_float(scale_k << 23), sv = __uint_as_float(scale_v << 23);
             const unsigned row = lds0 + slot * kTileBytes + xrow * 256;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                *LDS_PTR(u32x4, row + kKOff + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = widen_half(raw_k, h, sk);
+                *LDS_PTR(u32x4, row + kKOff + (((2 * xpiece + h) ^ (xrow & 15)) << 4)) = widen8(raw_k[2 * h], raw_k[2 * h + 1], sk);
             __builtin_amdgcn_sched_barrier(0);                       // registers of one at a time
-            u32x4 v2[2] = {widen_half(raw_v, 0, sv), widen_half(raw_v, 1, sv)};
+            u32x4 v2[2] = {widen8(raw_v[0], raw_v[1], sv), widen8(raw_v[2], raw_v[3], sv)};
             if (partly(x, bits)) {
                 const bool there = (bits >> (xrow >> 4)) & 1;
                 v2[0] = clean(v2[0], base(x) + xrow, there); v2[1] = clean(v2[1], base(x) + xrow, there);
@@ -381,11 +408,11 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigne
         const int bits0 = ok[3];
         if (MX) {
             load_raw();
-            const raw_row k0 = raw_k, v0 = raw_v;
+            const u32x4 k0 = raw_k, v0 = raw_v;
             const unsigned sk0 = scale_k, sv0 = scale_v;
             describe_first(1);
             load_raw();
-            const raw_row k1 = raw_k, v1 = raw_v;
+            const u32x4 k1 = raw_k, v1 = raw_v;
             const unsigned sk1 = scale_k, sv1 = scale_v;
             raw_k = k0; raw_v = v0; scale_k = sk0; scale_v = sv0;
             store_raw(0, bits0, 0);
