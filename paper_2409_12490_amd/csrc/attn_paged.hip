@@ -492,7 +492,8 @@ PagedRoute paged_route(const CacheShape& sh) {
     // (Eight waves to a workgroup, half as many steps: no faster; a unit's 56 GB/s are what one compute unit reads.)
     const int brief = f32 ? 128 : heads < 64 ? 512 : scaled ? 1024 : 768;
     if (r.chunk) {
-        r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2; r.setup = 5;
+        r.rows = 256; r.tile_shift = log2_of(256 / sh.group); r.step_shift = 6; r.workgroups = 256; r.least = 2;
+        r.setup = four ? 4 : 5;                                     // 4 bits: 20 sequences of 1 to 300 new tokens (32/4 heads) 133.2 with 3, 134.4, 135.9; 10 of 1 to 200 (32/8) 65.9, 65.2, 66.9; 8 141.0 and 68.6
         const double units = heads * (((long long)sh.max_q + (1 << r.tile_shift) - 1) >> r.tile_shift);
         r.whole = sh.max_kv <= (units < 16 ? 256 : units < 64 ? 512 : 768);
         return r;

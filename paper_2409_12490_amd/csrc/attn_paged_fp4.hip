@@ -174,28 +174,30 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
         const int r = 16 * nq + c16, of = (int)a.by_group.div((unsigned)r), t = min(of, n.live - 1), g = r - of * a.group;
         return (const T*)a.q + (int64_t)(n.row + t) * a.qs0 + (int64_t)(n.head * a.group + g) * a.qs1 + 32 * kg + 8 * ks;
     };
+    f32x4 q_raw[F32 ? NQ : 1][2];
     auto load_q = [&](const Unit& n) __attribute__((always_inline)) {
-        if constexpr (F32) {
-            f32x4 x[NQ][2];
 #pragma unroll
-            for (int nq = 0; nq < NQ; ++nq) {
+        for (int nq = 0; nq < NQ; ++nq) {
+            if constexpr (F32) {                                               // a quarter of the channels to a wave
                 const T* from = q_part(n, nq, wave);
-                x[nq][0] = *(const f32x4*)from; x[nq][1] = *(const f32x4*)(from + 4);
+                q_raw[nq][0] = *(const f32x4*)from; q_raw[nq][1] = *(const f32x4*)(from + 4);
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)q_part(n, nq, ks);
             }
+        }
+    };
+    auto place_q = [&]() __attribute__((always_inline)) {
+        if constexpr (F32) {
             __syncthreads();                                                   // the unit before has been read
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
                 bf16x8 piece[3];
-                split8(x[nq][0], x[nq][1], piece);
+                split8(q_raw[nq][0], q_raw[nq][1], piece);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) q_pieces[((nq * 4 + wave) * 3 + i) * 64] = piece[i];
             }
             __syncthreads();
-        } else {
-#pragma unroll
-            for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks) qf[nq][ks] = *(const bf16x8*)q_part(n, nq, ks);
         }
     };
     auto begin = [&](const Unit& n) __attribute__((always_inline)) {
@@ -206,6 +208,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
         __builtin_amdgcn_sched_barrier(0);
         load_v();
         __builtin_amdgcn_sched_barrier(0);
+        place_q();
         look_up(n, 1);
     };
     // The first step of the next unit is asked for in this one's last: what a unit begins and ends with, some 3 us, passes meanwhile (64 single tokens of up to 32769 keys 73.7 us, now 66.9).
