@@ -6,8 +6,9 @@ import torch
 from oracle import cache_oracle as O
 from paper_2409_12490_amd import binding as B
 from tests.cache4_helpers import Pool4, attend4
-from tests.cache_helpers import DEV, check_attention, f64, randn
+from tests.cache_helpers import DEV, HALF_STEP, check_attention, dealing, f64, randn, route
 from tests.test_gpu_paged import CASES, DEALT, _starts
+from tests.test_gpu_paged_dealing import _plain
 
 pytestmark = pytest.mark.gpu
 
@@ -199,3 +200,77 @@ def test_blocks_of_nan_at_any_key(dtype, hq, hkv, page, seqs, before):
                 pool.spoil(1, slot // page, h, slot % page, u % 3)
     out, lse = attend4(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
     _compare(pool, q, start, total, out, lse, dtype)
+
+
+# Tiles of 256 rows, in every way that their units are dealt out: rounds that leave nothing, that leave some to be cut, or whole; whole as the lengths turn out or as the host says; cut.
+TILES = [(32, 8, 64, [(512, 812)] * 8), (64, 4, 16, [(48, 1000)] * 64), (28, 4, 32, [(512, 812)] * 17), (64, 1, 32, [(3100, 3311)]), (28, 4, 64, [(257, 900)] * 17),
+         (32, 8, 32, [(130, 900)] * 4), (32, 8, 64, [(200 + 37 * i, 820 + 50 * i) for i in range(5)]), (32, 8, 64, [(300, 600)] * 4),
+         (32, 8, 64, [(70, 4000), (300, 900), (0, 0), (1, 1700)]), (16, 4, 16, [(130, 1300)] * 70)]
+
+
+def _width(seqs, page):
+    return max(-(-t // page) for _, t in seqs) + 1                  # of Pool's page table
+
+
+def tiles_route(case):
+    hq, hkv, page, seqs = case
+    return dealing("bf16", 2, hq, hkv, seqs, _width(seqs, page) * page)
+
+
+@pytest.mark.parametrize("case", TILES, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}x{len(c[3])}x{c[3][0][0]}x{c[3][0][1]}")
+def test_dealt_tiles(case):
+    hq, hkv, page, seqs = case
+    gen = torch.Generator().manual_seed(len(seqs) + hq)
+    new, total = zip(*seqs)
+    pool = Pool4(gen, total, hkv, page)
+    assert pool.table.shape[1] == _width(seqs, page)
+    q, start = randn(gen, sum(new), hq, 128).to(DEV), _starts(new)
+    out, lse = attend4(pool, q, start, total, max_q_len=max(new))
+    want, want_lse, size, logit = _plain(pool, q, start, total, 128 ** -0.5)
+    # the bound of cache_helpers.check_attention
+    delta = 2.0 ** -20 * (logit + want_lse.abs().clamp(min=1.0)) + 2.0 ** -20
+    bound = HALF_STEP["bf16"] * (size + want.abs()) * 1.01 + 4 * delta[..., None] * size.amax(-1, keepdim=True) + 1e-30
+    worst = float(((out.double() - want).abs() / bound).max())
+    assert torch.isfinite(out).all() and worst <= 1.0, f"out: {worst:.2f} of the bound"
+    assert ((lse.double() - want_lse).abs() <= 2 * delta).all()
+
+
+# Both sides of the lines between the kernels, their tiles and units cut or whole: dtype, heads, page, sequences.
+AROUND = [("bf16", 8, 2, 16, [(16, 700), (3, 90)] * 3), ("bf16", 8, 2, 16, [(17, 700), (3, 90)] * 3), ("bf16", 8, 2, 64, [(32, 5000)]), ("bf16", 8, 2, 64, [(33, 5000)]), ("bf16", 8, 2, 64, [(64, 3900)]),
+          ("bf16", 8, 2, 64, [(65, 3900)]), ("bf16", 32, 1, 32, [(2, 300), (1, 40)]), ("bf16", 32, 1, 16, [(1, 800)]), ("bf16", 33, 1, 32, [(1, 300)]), ("bf16", 33, 1, 32, [(1, 200), (1, 31)]), ("bf16", 32, 8, 64, [(1, 700)] * 3),
+          ("bf16", 32, 8, 64, [(1, 800)] * 3), ("bf16", 32, 8, 16, [(1, 1000)] * 8), ("bf16", 32, 8, 64, [(2, 1900 - 50 * i) for i in range(33)]), ("bf16", 4, 2, 16, [(1, 2100), (1, 5)] * 70),
+          ("fp32", 8, 2, 16, [(1, 480)] * 3), ("fp32", 8, 2, 64, [(1, 700), (3, 90)]), ("fp32", 8, 2, 32, [(4, 1000 - 20 * i) for i in range(33)]), ("fp32", 17, 1, 16, [(2, 300), (1, 1)]),
+          ("fp32", 40, 1, 64, [(3, 900), (1, 64)]), ("fp32", 64, 1, 16, [(2, 130)]), ("fp32", 4, 2, 16, [(200, 1500)])]
+
+
+def around_route(case):
+    dtype, hq, hkv, page, seqs = case
+    return route(dtype, 2, hq, hkv, len(seqs), max(n for n, _ in seqs), _width(seqs, page) * page)
+
+
+@pytest.mark.parametrize("case", AROUND, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}x{c[3]}x{len(c[4])}x{c[4][0][0]}x{c[4][0][1]}")
+def test_around_the_lines(case):
+    dtype, hq, hkv, page, seqs = case
+    pool, q, start, total = _case(dtype, hq, hkv, page, seqs)
+    assert pool.table.shape[1] == _width(seqs, page)
+    out, lse = attend4(pool, q, start, total, max_q_len=max(n for n, _ in seqs))
+    check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_units_of_one_step_one_after_another(dtype):
+    """Workgroups that go through many units of one step each, empty ones and ones that see nothing among them, and of two and three steps: the next unit's keys are asked for in the last step."""
+    seqs = [(1, (1, 128, 0, 129, 37, 257, 1, 384)[i % 8]) if i % 11 else (0, 0) for i in range(700)]
+    pool, q, start, total = _case(dtype, 4, 2, 16, seqs)
+    for max_kv in (0, 400):
+        out, lse = attend4(pool, q, start, total, max_q_len=1, max_kv_len=max_kv)
+        check_attention(pool, q, start, total, out, lse)
+
+
+def test_fp32_queries_of_any_size():
+    """Queries and keys from far apart ranges: three bf16 pieces hold all of an fp32 number, so that a logit is as exact as its sum."""
+    pool, q, start, total = _case("fp32", 8, 2, 16, [(1, 300), (5, 90)], scale=2.0 ** -60)
+    q = q * 2.0 ** 60 * (1 + torch.arange(128, device=DEV) * 2.0 ** -17)
+    q[0, 0, 5], q[1, 1] = 3.4028234e38 * 2.0 ** -64, 0.0
+    out, lse = attend4(pool, q, start, total, max_q_len=5)
+    check_attention(pool, q, start, total, out, lse)
