@@ -533,9 +533,11 @@ PagedRoute paged_route(const CacheShape& sh) {
 
 // No more workgroups than there can be runs, from what the host knows of the lengths: any number is right, and those without a run take time to begin and end, in the
 // join above all.  A multiple of 8, see Run.
-static double most_units(const CacheShape& sh, const PagedRoute& r) { return (double)sh.hkv * ((sh.tokens >> r.tile_shift) + (double)sh.n_seqs); }
-static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r) {
-    const double units = most_units(sh, r), steps = (double)(sh.max_kv >> r.step_shift) + 2 + r.setup;
+static double most_units(const CacheShape& sh, const PagedRoute& r, int most = 1 << 30) {
+    return (double)sh.hkv * ((most <= 1 << r.tile_shift ? 0 : sh.tokens >> r.tile_shift) + (double)sh.n_seqs);      // most: of new tokens that a sequence of the launch has
+}
+static unsigned useful_workgroups(const CacheShape& sh, const PagedRoute& r, int most) {
+    const double units = most_units(sh, r, most), steps = (double)(sh.max_kv >> r.step_shift) + 2 + r.setup;
     const double runs = r.whole ? units : units * steps / r.least;
     return (unsigned)std::min<double>(r.workgroups, 8.0 * std::ceil(runs / 8));
 }
@@ -559,17 +561,25 @@ hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, cons
     return launch<false, false, 1>(a, st);
 }
 
-hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
-                             float* lse, void* workspace, hipStream_t st) {
+// Over pages of 4 bits a batch of single tokens with a chunk or two among them goes to both kernels, one after the other: sequences of up to so many new tokens, 16 rows, to the one whose
+// waves split the keys, where 256 rows' worth of time passes for each of their steps otherwise.  0: one kernel for all.  The host does not see the lengths, so it goes by how long the others are
+// on the average if one is as long as is said, and by how much there can be to gain: two launches more are 7 to 12 us.  us, one kernel / both: 63 single tokens of 8000 keys and 512 of 4512
+// (32/8 heads) 504 / 166, 15 and 2048 161 / 104, 3 and 300 of 2300 (32/4) 42 / 52; 20 sequences of 1 to 300 of up to 12300 (32/4), 67 on the average, 134 / 146; 50 of 1 to 100, 20 on the average, 71 / 80.
+int few_tokens(const CacheShape& sh) {
+    if (sh.held != HELD_MXFP4 || sh.n_seqs < 2 || sh.group > 32 || !paged_route(sh).chunk) return 0;
+    const double others = (double)std::max(sh.tokens - sh.max_q, 0) / (sh.n_seqs - 1), steps = (double)(sh.n_seqs - 1) * sh.hkv * (double)(sh.max_kv >> 6);
+    return others <= 12 && steps >= 6000 ? std::max(1, 16 / sh.group) : 0;
+}
+
+// One kernel, and what joins the parts that it leaves; of `a` the caller's arrays and which sequences are this launch's are set.
+static hipError_t launch_route(const CacheShape& sh, PagedArgs a, void* workspace, hipStream_t st) {
     const PagedRoute route = paged_route(sh);
-    PagedArgs a;
-    a.q = q; a.cache = cache; a.table = sh.max_pages ? table : kv_len; a.q_start = q_start; a.kv_len = kv_len; a.out = out; a.lse = lse;
     a.parts = (float*)workspace;
     a.stats = a.parts + (size_t)route.workgroups * 2 * route.rows * kHeadDim;
     a.record = (int32_t*)(a.stats + (size_t)route.workgroups * 2 * route.rows * 2);
     a.tokens = sh.tokens; a.n_seqs = sh.n_seqs; a.max_pages = sh.max_pages; a.n_pages = sh.n_pages; a.hq = sh.hq; a.hkv = sh.hkv; a.group = sh.group;
     a.page_shift = sh.page_shift; a.tile_shift = route.tile_shift; a.step_shift = route.step_shift;
-    a.workgroups = useful_workgroups(sh, route); a.cut_units = (unsigned)std::min<double>(a.workgroups, most_units(sh, route)); a.least = route.least; a.setup = route.setup; a.whole = route.whole; a.held = sh.held;
+    a.workgroups = useful_workgroups(sh, route, a.most); a.cut_units = (unsigned)std::min<double>(a.workgroups, most_units(sh, route, a.most)); a.least = route.least; a.setup = route.setup; a.whole = route.whole; a.held = sh.held;
     a.by_group = FastDiv(sh.group);
     a.scale = sh.scale; a.scale_log2e = sh.scale * 1.4426950408889634f;
     a.qs0 = sh.qs[0]; a.qs1 = sh.qs[1]; a.os0 = sh.os[0]; a.os1 = sh.os[1];
@@ -589,6 +599,22 @@ hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr
         else hipLaunchKernelGGL((join_kernel<__bf16, false, 4>), grid, dim3(256), 0, st, a, route.rows, grid.y);
     }
     return hipGetLastError();
+}
+
+hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
+                             float* lse, void* workspace, hipStream_t st) {
+    PagedArgs a;
+    a.q = q; a.cache = cache; a.table = sh.max_pages ? table : kv_len; a.q_start = q_start; a.kv_len = kv_len; a.out = out; a.lse = lse;
+    a.fewest = 0; a.most = 1 << 30;
+    const int few = few_tokens(sh);
+    if (few) {
+        CacheShape small = sh;
+        small.max_q = a.most = few;                                // and a tile holds them
+        const hipError_t e = launch_route(small, a, workspace, st);
+        if (e != hipSuccess) return e;
+        a.fewest = few + 1; a.most = 1 << 30;
+    }
+    return launch_route(sh, a, workspace, st);
 }
 
 }  // namespace cp

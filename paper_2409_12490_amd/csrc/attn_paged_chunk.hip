@@ -55,7 +55,7 @@ __device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {              
 // RUNS: pages that a tile of 64 keys lies in: 1 (pages of 64 and more), 2 or 4 (of 16).  Four look-ups and what follows from them are 80 scalar instructions a step more than one:
 // 8192 new tokens of 32768 (32/8 heads), pages of 64, 3571 us with four and 3310 with one.
 template <int HELD, int RUNS, bool ROTATED>
-__device__ __forceinline__ void work(const PagedArgs& a, Run<true>& run, unsigned home, unsigned lds0) {
+__device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_MXFP4>& run, unsigned home, unsigned lds0) {
     constexpr bool MX = HELD != HELD_PLAIN, MX4 = HELD == HELD_MXFP4;
     constexpr int kRowBytes = row_bytes(HELD, 2);                  // of 4 bits
     const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
@@ -577,7 +577,7 @@ template <int HELD, int RUNS>
 __global__ __launch_bounds__(512, 1) void paged_chunk_kernel(PagedArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    Run<true> run;
+    Run<true, HELD == HELD_MXFP4> run;
     const bool any = run.find(a, workgroup_id(), thread_id() & 63);
     if (workgroup_id() == 0 && thread_id() == 0) a.record[0] = run.whole ? 0 : (int)run.used;   // whole: nothing to join
     if (run.logical < run.used && thread_id() == 0) a.record[4 + 4 * run.logical + 3] = 0;

@@ -72,6 +72,8 @@ __device__ __forceinline__ V get(const char* p) { return __builtin_nontemporal_l
 
 constexpr int kWaveKeys = 32;                 // of a step, to each wave
 
+typedef Run<false, true> Share;
+
 // One unit, or the piece of it that lies in a workgroup's run.  All the same for a workgroup.
 struct Unit {
     int seq, head, row, live;                 // row: its first token's, live: its tokens
@@ -80,7 +82,7 @@ struct Unit {
     // the first key of a wave's r-th 16 (of pages of 16), in step x of the piece
     __device__ __forceinline__ int key(const PagedArgs& a, unsigned x, int wave, int r) const { return (int)((first + x) << a.step_shift) + wave * kWaveKeys + 16 * r; }
 };
-__device__ __forceinline__ Unit unit_of(const PagedArgs& a, const Run<false>& run) {
+__device__ __forceinline__ Unit unit_of(const PagedArgs& a, const Share& run) {
     Unit n;
     const int t0 = run.tile << a.tile_shift;
     n.seq = run.seq; n.head = run.head; n.row = run.now.start + t0; n.live = min(1 << a.tile_shift, run.now.tokens - t0);
@@ -90,7 +92,7 @@ __device__ __forceinline__ Unit unit_of(const PagedArgs& a, const Run<false>& ru
     return n;
 }
 // Run::next_steps with scalar loads: a vector load's wait would be one for all keys and values that are under way.
-__device__ __forceinline__ bool next_unit(const PagedArgs& a, Run<false>& run) {
+__device__ __forceinline__ bool next_unit(const PagedArgs& a, Share& run) {
     const unsigned rest = run.whole ? 1u : a.setup + run.now.steps_of(a, run.tile) - run.at;
     if (run.left <= rest) return false;
     run.left -= rest;
@@ -101,7 +103,7 @@ __device__ __forceinline__ bool next_unit(const PagedArgs& a, Run<false>& run) {
             run.head = 0;
             do {
                 if (++run.seq >= a.n_seqs) return false;
-                run.now.load_uniform(a, run.seq, run.whole);
+                run.now.load_uniform<true>(a, run.seq, run.whole);
             } while (run.now.tiles == 0);
         }
     }
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
 
     const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, kg = lane >> 4;
     const int wave = first_lane(tid >> 6);
-    Run<false> run;
+    Share run;
     const bool any = run.find(a, blockIdx.x, lane);
     if (blockIdx.x == 0 && tid == 0) a.record[0] = (int)run.used;
     if (run.logical < run.used && tid == 0) a.record[4 + 4 * run.logical + 3] = 0;

@@ -47,6 +47,7 @@ struct PagedRoute {
     int whole;                                // units are not cut: sequences are known to be short, and there is nothing to join
 };
 PagedRoute paged_route(const CacheShape& sh);
+int few_tokens(const CacheShape& sh);
 size_t paged_workspace(const CacheShape& sh);
 hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
                              float* lse, void* workspace, hipStream_t st);

@@ -34,6 +34,7 @@ struct PagedArgs {
     FastDiv by_group;
     float scale, scale_log2e;
     int64_t qs0, qs1, os0, os1;
+    int fewest, most;                         // 4 bits: new tokens of the sequences that are the launch's; the others are another's
 };
 
 // A unit that begins in a workgroup's run and ends in a later one's: parts of it are in slot 1 of this workgroup and slot 0 of `parts - 1` that follow.
@@ -55,18 +56,22 @@ struct Sequence {                             // one sequence, checked: whatever
     __device__ __forceinline__ unsigned steps_of(const PagedArgs& a, int j) const {    // without setup
         return TileSteps(tokens, keys, a.step_shift).of((unsigned)j, a.tile_shift, a.step_shift);
     }
+    template <bool SPLIT>
     __device__ __forceinline__ bool load(const PagedArgs& a, int s, int whole) {       // whether its rows ascend
-        return set(a, a.q_start[s], a.q_start[s + 1], a.kv_len[s], whole);
+        return set<SPLIT>(a, a.q_start[s], a.q_start[s + 1], a.kv_len[s], whole);
     }
     // the same for a number that all lanes share, through scalar loads
+    template <bool SPLIT>
     __device__ __forceinline__ void load_uniform(const PagedArgs& a, int s, int whole) {
         typedef const __attribute__((address_space(4))) int32_t* list;
         const list starts = (list)(unsigned long long)a.q_start, lengths = (list)(unsigned long long)a.kv_len;
-        set(a, starts[s], starts[s + 1], lengths[s], whole);
+        set<SPLIT>(a, starts[s], starts[s + 1], lengths[s], whole);
     }
+    template <bool SPLIT>
     __device__ __forceinline__ bool set(const PagedArgs& a, int from, int to, int held, int whole) {
         start = min(max(from, 0), a.tokens);
         tokens = min(max(to, start), a.tokens) - start;
+        if (SPLIT && (tokens < a.fewest || tokens > a.most)) tokens = 0;
         keys = (int)min((long long)max(held, 0), (long long)a.max_pages << a.page_shift);
         tiles = (int)(((unsigned)tokens + (1u << a.tile_shift) - 1) >> a.tile_shift);
         length = before(a, tiles, whole);
@@ -80,8 +85,8 @@ struct Sequence {                             // one sequence, checked: whatever
     }
 };
 
-// What a workgroup works on: whole units first (rounds), then its run.  Every wave works it out by itself.
-template <bool ROUNDS>
+// What a workgroup works on: whole units first (rounds), then its run.  Every wave works it out by itself.  SPLIT: of the sequences that are this launch's.
+template <bool ROUNDS, bool SPLIT = false>
 struct Run {
     unsigned logical, used, share, left;      // its number among those that share, these, steps of each, steps left to it
     int seq, head, tile; unsigned at;         // at: inside the unit, setup first
@@ -97,7 +102,7 @@ struct Run {
         Sequence s;
         unsigned long long wrong = 0;
         for (int base = 0; base < a.n_seqs; base += 64) {
-            wrong |= __builtin_amdgcn_ballot_w64(!s.load(a, min(base + lane, a.n_seqs - 1), whole));
+            wrong |= __builtin_amdgcn_ballot_w64(!s.template load<SPLIT>(a, min(base + lane, a.n_seqs - 1), whole));
             mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
             upto = mine;
 #pragma unroll
@@ -157,7 +162,7 @@ struct Run {
             unsigned past = 0;
             for (int base = 0; base < a.n_seqs; base += 64) {
                 if (again) {
-                    s.load(a, min(base + lane, a.n_seqs - 1), whole);
+                    s.template load<SPLIT>(a, min(base + lane, a.n_seqs - 1), whole);
                     mine = base + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
                     upto = mine;
 #pragma unroll
@@ -198,13 +203,13 @@ struct Run {
     // the unit of the present round; false where a round that is not full has none for this workgroup
     __device__ __forceinline__ bool whole_unit(const PagedArgs& a) {
         const unsigned unit = (unsigned)round * a.workgroups + (round & 1 ? a.workgroups - 1 - place : place);
-        now.load(a, 0, whole);                                            // all are alike but for their start
+        now.template load<SPLIT>(a, 0, whole);                                            // all are alike but for their start
         const unsigned tiles = (unsigned)first_lane(now.tiles), heads = (unsigned)first_lane((int)(unit / tiles));
         tile = (int)(unit - heads * tiles);
         seq = first_lane((int)(heads / (unsigned)a.hkv));
         if (seq >= a.n_seqs) return false;
         head = (int)(heads - (unsigned)seq * (unsigned)a.hkv);
-        now.load(a, seq, whole);
+        now.template load<SPLIT>(a, seq, whole);
         now = now.of_lane(0);
         at = 0;
         left = a.setup + now.steps_of(a, tile);
@@ -231,7 +236,7 @@ struct Run {
         head = 0;
         do {
             if (++seq >= a.n_seqs) return false;
-            now.load(a, seq, whole);
+            now.template load<SPLIT>(a, seq, whole);
             now = now.of_lane(0);
         } while (now.tiles == 0);
         return true;
@@ -242,7 +247,7 @@ struct Run {
             round = rounds;
             left = run_left; at = run_at; seq = run_seq; head = run_head; tile = run_tile;
             if (left == 0) return false;
-            now.load(a, seq, whole);
+            now.template load<SPLIT>(a, seq, whole);
             now = now.of_lane(0);
             return has_steps(a);
         }

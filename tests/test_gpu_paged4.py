@@ -1,4 +1,6 @@
 """Attention of new tokens over pages of 4 bits against fp64: the cases of the other formats, what hidden places hold, arrays that say nonsense, captured calls."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -6,7 +8,7 @@ import torch
 from oracle import cache_oracle as O
 from paper_2409_12490_amd import binding as B
 from tests.cache4_helpers import Pool4, attend4
-from tests.cache_helpers import DEV, HALF_STEP, check_attention, dealing, f64, randn, route
+from tests.cache_helpers import DEV, HALF_STEP, Shape, check_attention, dealing, f64, randn, route
 from tests.test_gpu_paged import CASES, DEALT, _starts
 from tests.test_gpu_paged_dealing import _plain
 
@@ -274,3 +276,70 @@ def test_fp32_queries_of_any_size():
     q[0, 0, 5], q[1, 1] = 3.4028234e38 * 2.0 ** -64, 0.0
     out, lse = attend4(pool, q, start, total, max_q_len=5)
     check_attention(pool, q, start, total, out, lse)
+
+
+# Single tokens with a chunk or two among them: both kernels, each with its own sequences.  Of up to so many new tokens, and of more; none at all; keys that none of them sees.
+MIXED = [(32, 8, 64, [(1, 100 + 30 * i) for i in range(38)] + [(300, 1400), (4, 700), (5, 710), (0, 500), (2, 1), (0, 0)], 4), (28, 4, 16, [(2, 1500 - 9 * i) for i in range(80)] + [(60, 60), (3, 900)], 2),
+         (32, 1, 32, [(1, 5600 - 70 * i) for i in range(72)] + [(9, 300)], 1), (5, 1, 16, [(3, 4100), (1, 90)] * 50 + [(120, 700)], 3), (32, 8, 64, [(1, 1400)] * 40, 4)]
+
+
+def few_of(case):
+    hq, hkv, page, seqs, _ = case
+    f = B.load()._ZN2cp10few_tokensERKNS_10CacheShapeE
+    f.argtypes, f.restype = [ctypes.POINTER(Shape)], ctypes.c_int
+    max_q = max(n for n, _ in seqs)
+    return f(Shape(dtype=1, mxfp8=2, hq=hq, hkv=hkv, group=hq // hkv, n_seqs=len(seqs), max_q=max_q if max_q > 1 else 100, max_kv=_width(seqs, page) * page, tokens=sum(n for n, _ in seqs)))
+
+
+@pytest.mark.parametrize("case", MIXED, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}x{len(c[3])}")
+def test_single_tokens_beside_a_chunk(case):
+    hq, hkv, page, seqs, few = case
+    assert few_of(case) == few
+    pool, q, start, total = _case("bf16", hq, hkv, page, seqs)
+    assert pool.table.shape[1] == _width(seqs, page)
+    longest = max(n for n, _ in seqs)
+    out, lse = attend4(pool, q, start, total, max_q_len=longest if longest > 1 else 100)     # the last: a bound that no sequence comes near to
+    check_attention(pool, q, start, total, out, lse)
+
+
+def test_single_tokens_beside_a_chunk_captured_and_out_of_order():
+    """Replays follow the lengths, sequences change sides; rows that do not ascend are nobody's, in either kernel; rows behind the last sequence stay as they are."""
+    gen = torch.Generator().manual_seed(8)
+    seqs = [(1, 1400 - 11 * i) for i in range(40)] + [(90, 700)]
+    pool = Pool4(gen, [t for _, t in seqs], 8, 64)
+    table, q = pool.table.to(DEV), randn(gen, 140, 32, 128).to(DEV)
+    out, lse = torch.full((140, 32, 128), 5.0, dtype=q.dtype, device=DEV), torch.full((140, 32), 5.0, device=DEV)
+    p = B.make_cache_params(32, 8, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp4=True, page_table=table, max_q_len=100)
+    ws = B.alloc_paged_workspace(p)
+    start, lens = torch.zeros(42, dtype=torch.int32, device=DEV), torch.zeros(41, dtype=torch.int32, device=DEV)
+
+    def call():
+        B.critiprefill_paged_attn(p, q, *pool.cache, table, start, lens, out, lse, ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for new, held in (([1] * 40 + [90], [t for _, t in seqs]), ([3] * 20 + [0] * 20 + [70], [900 - i for i in range(40)] + [700]), ([1] * 40 + [1], [5] * 41), ([0] * 40 + [100], [0] * 40 + [700])):
+        start.copy_(torch.tensor(_starts(new), dtype=torch.int32))
+        lens.copy_(torch.tensor(held, dtype=torch.int32))
+        out.fill_(5.0); lse.fill_(5.0)
+        call()
+        torch.cuda.synchronize()
+        eager = out.clone(), lse.clone()
+        out.fill_(5.0); lse.fill_(5.0); ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        n = sum(new)
+        check_attention(pool, q[:n], _starts(new), held, out[:n], lse[:n])
+        assert (out[n:] == 5).all() and (lse[n:] == 5).all()
+    start.copy_(torch.tensor(list(range(20)) + [18] + list(range(21, 42)), dtype=torch.int32))
+    out.fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert (out == 7).all()

@@ -1,10 +1,12 @@
 """Attention over pages of 4 bits on the CPU: which kernel and which way to cut the work the library's own rules choose, on both sides of their lines, and that the lines of the other formats
 are where they were."""
+import ctypes
+
 import pytest
 
 from paper_2409_12490_amd import binding as B
 from tests import test_cache_abi as A
-from tests.cache_helpers import dealing, route
+from tests.cache_helpers import Shape, dealing, route
 
 FOUR = 2                                           # HELD_MXFP4 of csrc/cache.h
 
@@ -54,6 +56,29 @@ def test_the_gpu_cases_around_the_lines_are_on_both_sides():
     from tests.test_gpu_paged4 import AROUND, around_route
     routes = [around_route(c) for c in AROUND]
     assert {(r.chunk, r.rows) for r in routes} == {(0, 16), (0, 32), (0, 64), (1, 256)} and {(r.chunk, r.whole) for r in routes} == {(0, 0), (0, 1), (1, 0), (1, 1)}
+
+
+def _few(held, heads, seqs, max_q, max_kv, tokens, dtype=1):
+    f = B.load()._ZN2cp10few_tokensERKNS_10CacheShapeE
+    f.argtypes, f.restype = [ctypes.POINTER(Shape)], ctypes.c_int
+    return f(Shape(dtype=dtype, mxfp8=held, hq=heads[0], hkv=heads[1], group=heads[0] // heads[1], n_seqs=seqs, max_q=max_q, max_kv=max_kv, tokens=tokens))
+
+
+@pytest.mark.parametrize("heads,seqs,max_q,max_kv,tokens,few", [
+    ((32, 8), 64, 512, 8192, 575, 4), ((32, 4), 64, 512, 8192, 575, 2), ((32, 1), 64, 512, 4096, 575, 0), ((32, 1), 64, 512, 8192, 575, 1), ((33, 1), 64, 512, 8192 * 2, 575, 0),
+    # the others 12 tokens on the average, and more; 6000 steps of 64 keys for all but one, and fewer
+    ((32, 8), 11, 100, 8192, 220, 4), ((32, 8), 11, 100, 8192, 221, 0), ((32, 8), 11, 100, 4800, 200, 4), ((32, 8), 11, 100, 4736, 200, 0),
+    # one sequence; no tiles of 256 rows; nothing known of the longest
+    ((32, 8), 1, 512, 80000, 512, 0), ((32, 8), 64, 16, 8192, 64, 0), ((32, 8), 64, 64, 8192, 64, 4),
+])
+def test_single_tokens_beside_a_chunk(heads, seqs, max_q, max_kv, tokens, few):
+    assert _few(FOUR, heads, seqs, max_q, max_kv, tokens) == few
+    assert _few(0, heads, seqs, max_q, max_kv, tokens) == _few(1, heads, seqs, max_q, max_kv, tokens) == _few(FOUR, heads, seqs, max_q, max_kv, tokens, dtype=0) == 0
+
+
+def test_the_gpu_cases_of_single_tokens_beside_a_chunk_go_to_both():
+    from tests.test_gpu_paged4 import MIXED, few_of
+    assert [few_of(c) for c in MIXED] == [c[4] for c in MIXED]
 
 
 @pytest.mark.parametrize("dtype", [B.CP_DTYPE_FP32, B.CP_DTYPE_BF16])
