@@ -49,6 +49,12 @@ __device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {              
     return r;
 }
 
+// 4 bits: a thread has the four 16-byte pieces of a scale's 32 channels, and neighbouring threads those of the next, so that piece w of 32-channel block b lies at 4 w + b of its row and not at
+// 4 b + w, swizzled by the row as below: eight lanes that write, two rows of four blocks, meet all 32 banks, and so do those that read (257 conflict cycles a step with the other
+// kernels' order).
+__device__ __forceinline__ unsigned k_turn(int row) { return (unsigned)((row & 1) << 2 | (row >> 1 & 3) | (row & 8)); }     // of row & 15
+__device__ __forceinline__ unsigned v_turn(int row) { return (unsigned)(row | (row & 1) << 2); }                           // of row & 3
+
 // All units of a workgroup's run, for waves 0-3 or (ROTATED, half a period behind) waves 4-7, each of which shares its SIMD with wave - 4.  The roles part here and not
 // around their key loops: with both loops inside the one over the units the compiler spills 60 to 80 registers.  Both meet the same barriers.
 // What is left of it: all forms keep 174 to 292 times a scalar in a lane of a vector register, and that over 8-bit pages of 16 one vector register in memory (8 bytes of scratch).
@@ -68,17 +74,17 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_
         const int lane = tid & 63, l32 = lane & 31, hh = lane >> 5, r4 = lane >> 4, pch = lane & 15;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         // ---- per-lane LDS addresses (bytes, ring slot 0), see attn_bf16.hip
-        const unsigned k_base = (lds0 + kKOff + l32 * 256) | (unsigned)(((l32 & 15) ^ hh) << 4);
+        const unsigned k_base = (lds0 + kKOff + l32 * 256) | (MX4 ? (k_turn(l32 & 15) ^ (unsigned)hh << 2) << 4 : (unsigned)(((l32 & 15) ^ hh) << 4));
         const int i16 = lane & 15, gbit = (lane >> 4) & 1;
         unsigned v_addr[4];
     #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
-            v_addr[dt] = lds0 + kVOff + (4 * hh + (i16 >> 2)) * 256 + ((((unsigned)(dt ^ (i16 >> 2)) << 2) + 2 * gbit + ((i16 & 3) >> 1)) << 4) + (i16 & 1) * 8;
+            v_addr[dt] = MX4 ? lds0 + kVOff + (4 * hh + (i16 >> 2)) * 256 + (((unsigned)(((2 * gbit + ((i16 & 3) >> 1)) << 2) + dt) ^ v_turn(i16 >> 2)) << 4) + (i16 & 1) * 8
+                             : lds0 + kVOff + (4 * hh + (i16 >> 2)) * 256 + ((((unsigned)(dt ^ (i16 >> 2)) << 2) + 2 * gbit + ((i16 & 3) >> 1)) << 4) + (i16 & 1) * 8;
         // copies: wave w fills rows 4 w .. 4 w + 3 and 32 + 4 w .. of a tile; physical chunk pch of row r4
         const unsigned lane_k = (unsigned)r4 * 256 + (unsigned)(pch ^ ((4 * wave + r4) & 15)) * 16, lane_v = (unsigned)r4 * 256 + (unsigned)(pch ^ (4 * r4)) * 16;
         // 8 bits: thread tid has 16 channels 16 * (tid & 7) of row tid >> 3 of K and V.  4 bits: the 32 channels 32 * (tid & 3), those of a scale, of row tid / 4, of K (waves 0-3) or V (4-7).
         const int xrow = MX4 ? (tid & 255) >> 2 : tid >> 3, xpiece = MX4 ? tid & 3 : tid & 7;
-        const unsigned turned = (unsigned)(xrow & 3) * 4;            // 4 bits: V's words are taken in the order w ^ (row & 3), and so are K's, by their swizzle: eight lanes write to all banks
 
         const Sequence seq = run.now;
         const int t0 = run.tile << a.tile_shift, live = min(1 << a.tile_shift, seq.tokens - t0), head = run.head;
@@ -194,11 +200,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_
             if constexpr (MX4) {
                 const char* from = uniform_ptr((const char*)(ROTATED ? a.cache.v : a.cache.k) + at[0] * kRowBytes);
                 const unsigned in_rows = (unsigned)lane * 16;
-                if constexpr (!ROTATED) raw_k = *(const u32x4*)(from + in_rows);
-                else {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) raw_k[w] = *(const unsigned*)(from + (in_rows + (turned ^ 4 * w)));
-                }
+                raw_k = *(const u32x4*)(from + in_rows);
                 scale_k = (uniform_ptr((ROTATED ? a.cache.vs : a.cache.ks) + at[0] * 4))[(unsigned)lane];
                 return;
             }
@@ -211,13 +213,13 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_
         auto store_raw = [&](int x, int bits, int slot) __attribute__((always_inline)) {
             if constexpr (MX4) {
                 const float scale = __uint_as_float(scale_k << 23);
-                const unsigned to = lds0 + (ROTATED ? kVOff : kKOff) + slot * kTileBytes + xrow * 256 + (((unsigned)(4 * xpiece) ^ (ROTATED ? 5u * (xrow & 3) : (unsigned)(xrow & 15))) << 4);
+                const unsigned to = lds0 + (ROTATED ? kVOff : kKOff) + slot * kTileBytes + xrow * 256 + (((unsigned)xpiece ^ (ROTATED ? v_turn(xrow & 3) : k_turn(xrow & 15))) << 4);
                 const bool part = ROTATED && partly(x, bits), there = ROTATED && ((bits >> (xrow >> 4)) & 1);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     u32x4 v = widen8(raw_k[w], scale);
                     if (part) v = clean(v, base(x) + xrow, there);
-                    *LDS_PTR(u32x4, to ^ (w << 4)) = v;
+                    *LDS_PTR(u32x4, to ^ (w << 6)) = v;
                 }
                 return;
             }
@@ -248,7 +250,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_
         unsigned ka[8], va[4];
         int ka_slot = 0, va_slot = 0;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) ka[ks] = k_base ^ (ks << 5);
+        for (int ks = 0; ks < 8; ++ks) ka[ks] = k_base ^ (MX4 ? ((ks & 1) << 3 | ks >> 1) << 4 : ks << 5);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) va[dt] = v_addr[dt];
         auto next_k_slot = [&]() {
