@@ -62,10 +62,10 @@ struct Sequence {                             // one sequence, checked: whatever
     }
     // the same for a number that all lanes share, through scalar loads
     template <bool SPLIT>
-    __device__ __forceinline__ void load_uniform(const PagedArgs& a, int s, int whole) {
+    __device__ __forceinline__ bool load_uniform(const PagedArgs& a, int s, int whole) {
         typedef const __attribute__((address_space(4))) int32_t* list;
         const list starts = (list)(unsigned long long)a.q_start, lengths = (list)(unsigned long long)a.kv_len;
-        set<SPLIT>(a, starts[s], starts[s + 1], lengths[s], whole);
+        return set<SPLIT>(a, starts[s], starts[s + 1], lengths[s], whole);
     }
     template <bool SPLIT>
     __device__ __forceinline__ bool set(const PagedArgs& a, int from, int to, int held, int whole) {
