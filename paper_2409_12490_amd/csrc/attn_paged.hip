@@ -561,6 +561,16 @@ hipError_t launch_paged_rows(const CacheShape& sh, const PagedRoute& route, cons
     return launch<false, false, 1>(a, st);
 }
 
+template <typename T>
+static hipError_t launch_join(int groups, int rows, int tile_rows, const PagedArgs& a, hipStream_t st) {
+    const int at_once = 8 / groups;
+    const dim3 grid(a.cut_units, (unsigned)((rows + at_once - 1) / at_once));
+    if (groups == 8) hipLaunchKernelGGL((join_kernel<T, false, 8>), grid, dim3(256), 0, st, a, tile_rows, grid.y);
+    else if (groups == 4) hipLaunchKernelGGL((join_kernel<T, false, 4>), grid, dim3(256), 0, st, a, tile_rows, grid.y);
+    else hipLaunchKernelGGL((join_kernel<T, false, 2>), grid, dim3(256), 0, st, a, tile_rows, grid.y);
+    return hipGetLastError();
+}
+
 // Over pages of 4 bits a batch of single tokens with a chunk or two among them goes to both kernels, one after the other: sequences of up to so many new tokens, 16 rows, to the one whose
 // waves split the keys, where 256 rows' worth of time passes for each of their steps otherwise.  0: one kernel for all.  The host does not see the lengths, so it goes by how long the others are
 // on the average if one is as long as is said, and by how much there can be to gain: two launches more are 7 to 12 us.  us, one kernel / both: 63 single tokens of 8000 keys and 512 of 4512
@@ -590,15 +600,12 @@ static hipError_t launch_route(const CacheShape& sh, PagedArgs a, void* workspac
     // A workgroup of the join takes a row with eight groups of threads, or two with four; more rows than its grid has, where a chunk is longer than was said, come in
     // turn.  Eight and four: 1 x 4 tokens after 5000 (16 rows, 64 parts) 16.1 and 17.2 us; 8 x 8 after 16000 over 8-bit pages (32 rows) 70 and 67, fp32 4/2 heads 3 x 200 40.6 and 38.7.
     const int rows = (int)std::min<long long>(route.rows, (long long)std::min(sh.max_q, 1 << route.tile_shift) * sh.group);
-    const dim3 grid(a.cut_units, (unsigned)(rows <= 16 ? rows : (rows + 1) / 2));
-    if (sh.dtype == 0) {
-        if (rows <= 16) hipLaunchKernelGGL((join_kernel<float, false, 8>), grid, dim3(256), 0, st, a, route.rows, grid.y);
-        else hipLaunchKernelGGL((join_kernel<float, false, 4>), grid, dim3(256), 0, st, a, route.rows, grid.y);
-    } else {
-        if (rows <= 16) hipLaunchKernelGGL((join_kernel<__bf16, false, 8>), grid, dim3(256), 0, st, a, route.rows, grid.y);
-        else hipLaunchKernelGGL((join_kernel<__bf16, false, 4>), grid, dim3(256), 0, st, a, route.rows, grid.y);
-    }
-    return hipGetLastError();
+    // Where there are many units each was cut into few parts, and few groups are enough.  Over pages of 4 bits, us, eight groups / four / two: 8 units (1 x 1 of 131072, 32/8 heads) 30.5 / 31.6 / 33.4, 16
+    // (2 x 1 of 30000) 20.2 / 19.9 / 20.5, 32 (4 x 1) 29.0 / 28.9 / 29.3, 64 (8 x 4 of 16000) 33.9 / 32.7 / 31.7, 240 (30 x 2 of up to 20000) 30.5 / 29.4 / 28.7, 512 (64 x 1 of up to 32769) 62.5 / 61.5 /
+    // 60.7; of two tiles, 128 (8 x 16 of 16000), four and two 62.5 / 60.5; fp32 up to 150 (3 x 200, 4/2 heads) 20.1 / 19.2 / 18.7.
+    int groups = rows <= 16 ? 8 : 4;
+    if (sh.held == HELD_MXFP4) groups = a.cut_units >= 64 ? 2 : a.cut_units >= 32 ? 4 : groups;
+    return sh.dtype == 0 ? launch_join<float>(groups, rows, route.rows, a, st) : launch_join<__bf16>(groups, rows, route.rows, a, st);
 }
 
 hipError_t launch_paged_attn(const CacheShape& sh, const void* q, const CachePtr& cache, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,

@@ -343,3 +343,19 @@ def test_single_tokens_beside_a_chunk_captured_and_out_of_order():
     graph.replay()
     torch.cuda.synchronize()
     assert (out == 7).all()
+
+
+# Cut units by number, of rows that no group of the joining kernel divides: dtype, heads, page, sequences.
+JOINED = [(dtype, hq, hkv, 32, [(new, 2500 - 70 * i) for i in range(n)]) for dtype in ("bf16", "fp32")
+          for hq, hkv, new, n in ((32, 8, 1, 3), (32, 8, 1, 4), (24, 8, 1, 7), (24, 8, 1, 8), (40, 8, 1, 9), (8, 8, 1, 10), (28, 4, 3, 17))]
+
+
+@pytest.mark.parametrize("case", JOINED, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}x{len(c[4])}x{c[4][0][0]}")
+def test_parts_joined_by_few_and_many_groups(case):
+    """The call's hint of the longest chunk may be too small: the joining kernel's workgroups then take the rows behind those that they were launched for in turn."""
+    dtype, hq, hkv, page, seqs = case
+    assert not route(dtype, 2, hq, hkv, len(seqs), seqs[0][0], _width(seqs, page) * page).whole
+    pool, q, start, total = _case(dtype, hq, hkv, page, seqs)
+    for hint in (seqs[0][0], 1):
+        out, lse = attend4(pool, q, start, total, max_q_len=hint)
+        check_attention(pool, q, start, total, out, lse)
