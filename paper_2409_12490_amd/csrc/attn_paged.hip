@@ -523,7 +523,7 @@ PagedRoute paged_route(const CacheShape& sh) {
         // to 3200 20.4, 21.0, 21.0.
         r.setup = f32 ? 1 : 2;
         // Short sequences by the number of units, cut / whole.  Fewer than 64: 1 x 1 of 768 9.9 / 8.8, 1 x 4 of 900 9.9 / 10.6, 1 x 16 of 900 11.7 / 13.0.  64 to 127: 8 x 1 of 1024 12.2 / 10.8, of 1536
-        // 12.4 / 14.0, 8 x 4 of 1500 15.4 / 14.6.  128 to 255: 8 x 16 of 1500 23.5 / 17.7.  More: 32 x 1 of 2048 21.9 / 18.7, of 3072 26.9 / 25.4, 32 x 4 of 2000 31.7 / 19.1, 64 x 1 of up to 2000 16.0 / 16.8.
+        // 12.4 / 14.0, 8 x 4 of 1500 15.4 / 14.6.  128 to 255: 8 x 16 of 1500 23.5 / 17.7.  More: 32 x 1 of 2048 21.9 / 18.7, 32 x 4 of 2000 31.7 / 19.1, 64 x 1 of up to 2000 16.0 / 16.8.
         // fp32, 4/2 and 8/2 heads: 1 x 1 of 512 10.7 / 8.2, 1 x 50 of 600 10.9 / 11.2; 8 x 50 of 700 16.7 / 12.0, 64 x 1 of 1024 14.8 / 13.4, of 1500 16.3 / 17.9; 8 x 200 of 800 33.0 / 18.6.
         const double units = heads * (((long long)sh.max_q + (1 << r.tile_shift) - 1) >> r.tile_shift);
         r.whole = sh.max_kv <= (units < 64 ? (f32 ? 512 : 768) : units < 128 || (f32 && units < 256) ? 1024 : units < 256 ? 1536 : 2048);

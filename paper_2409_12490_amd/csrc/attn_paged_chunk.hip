@@ -7,13 +7,13 @@
 // four pages, looked up by scalar loads a step ahead (pages are whole multiples of 16 tokens, so the rows of one load lie together); rows past the sequence's end lie in
 // its last page and may hold anything, so rows of V that no row sees are zeroed in LDS; the row sum adds P before it is rounded, since the log-sum-exp is an
 // output in its own right here (32 additions a step for 16 dot products).
-// Pages of 8 and 4 bits: a thread takes 16 channels of a row of K and of V into registers, a step ahead, and writes them to LDS as bf16 (exact: the scales are powers of two).
-// Every wave converts an eighth of a tile, where conversion at the reads from LDS would have each wave convert all of it.
+// Pages of 8 and 4 bits: every thread takes an eighth of a wave's share of a tile into registers, a step ahead, and writes it to LDS as bf16 (exact: the scales are powers of two), where
+// conversion at the reads from LDS would have each wave convert all of it.  8 bits: 16 channels of a row of K and of V; 4 bits: the 32 channels of one scale, of K or of V.
 //
 // What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
 // library reaches 1.24; the MFMA pipe is busy for 55 % of the launch, the vector units for 43 %, 96 % of the reads come from L2.  Over 8-bit pages 3.38 ms: 14 % more vector
-// instructions.  512 after 16384: 138 us, 1.01 PFLOP/s, 64 units in 314 pieces and 10 us to join them.  Mixed batches and short follow-ups: the beginnings and ends of pieces, 5 steps' worth each
-// (12 sequences of 1 to 300 new tokens, 32/4 heads, 8 bits: 388 pieces for 156 units, 98 us and 9.5 to join; 1 x 64 of 2000 21 us in all, MFMA busy for a twentieth of it).
+// instructions; over pages of 4 bits 3.23 ms, and 4096 of 32768 1.73 ms, 1.19 PFLOP/s.  512 after 16384: 138 us, 1.01 PFLOP/s, 64 units in 314 pieces and 10 us to join them.  Mixed batches and short follow-ups: the beginnings and ends of pieces, 5 steps' worth each
+// (12 sequences of 1 to 300 new tokens, 32/4 heads, 8 bits: 388 pieces for 156 units, 98 us and 9.5 to join; 20 of these, 4 bits: 478 pieces for 232 units, 121 us and 11 to join; 1 x 64 of 2000 21 us in all, MFMA busy for a twentieth of it).
 // Not kept: 8-bit bytes by way of LDS, three tiles in flight (no faster at 109 us for 8 x 4 tokens after 16000, 4 % slower in mixed batches); conversion that writes to LDS without bank
 // conflicts at the price of selections (257 conflict cycles a step less, 3 % slower); the places of the key loops within 32 bytes (1 % between the best and the worst).
 #include "attn_bf16.h"
