@@ -359,3 +359,91 @@ def test_parts_joined_by_few_and_many_groups(case):
     for hint in (seqs[0][0], 1):
         out, lse = attend4(pool, q, start, total, max_q_len=hint)
         check_attention(pool, q, start, total, out, lse)
+
+
+@pytest.mark.parametrize("dtype,hint", [("bf16", 4), ("bf16", 0), ("fp32", 4)])
+def test_nonsense_of_a_single_sequence(dtype, hint):
+    """The share of a single sequence is found by loads of its own."""
+    pool, q, start, total = _case(dtype, 8, 2, 16, [(4, 600)])
+    rows = torch.full((12, 8, 128), 5.0, dtype=q.dtype, device=DEV)
+    out = rows[4:-4]
+    table = pool.table.clone()
+    for start_, held in (([-5, 2 ** 31 - 1], 2 ** 31 - 1), ([-2 ** 31, 4], -1), ([1, 2 ** 30], -2 ** 31), ([0, 4], 2 ** 31 - 1)):
+        attend4(pool, q, start_, [held], table=table, max_q_len=hint, out=out)
+    out.fill_(5.0)
+    for start_ in ([4, 0], [2 ** 31 - 1, -1], [4, 4], [0, 0], [9, 9]):
+        attend4(pool, q, start_, total, max_q_len=hint, out=out)
+    assert bool((rows == 5.0).all())
+    table[0, :] = -1                                                 # no page is there: nothing to see
+    got, lse = attend4(pool, q, start, total, table=table, max_q_len=hint)
+    assert not got.any() and bool((lse == -float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 5), ("fp32", 3)])
+def test_a_captured_single_sequence_follows_its_length(dtype, new):
+    pool, q, start, total = _case(dtype, 8, 2, 32, [(new, 2100)])
+    table = pool.table.to(DEV)
+    out, lse = torch.empty((new, 8, 128), dtype=q.dtype, device=DEV), torch.empty((new, 8), device=DEV)
+    starts, lens = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (start, total))
+    p = B.make_cache_params(8, 2, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp4=True, page_table=table, max_q_len=new)
+    ws = B.alloc_paged_workspace(p)
+    call = lambda: B.critiprefill_paged_attn(p, q, *pool.cache, table, starts, lens, out, lse, ws)      # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for held in (2100, new, 0, 1, 129, 1500, 2100):
+        lens.fill_(held)
+        out.zero_(); lse.zero_(); ws.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(pool, q, start, [held], out, lse)
+
+
+@pytest.mark.parametrize("dtype,seqs", [("bf16", [(1, 900), (1, 40)]), ("bf16", [(90, 900), (1, 40), (70, 70)]), ("fp32", [(3, 700)])])
+def test_outputs_with_gaps_and_no_sum(dtype, seqs):
+    pool, q, start, total = _case(dtype, 8, 2, 16, seqs)
+    room = torch.full((2 * q.shape[0], 9, 136), 7.0, dtype=q.dtype, device=DEV)
+    out = room[::2, 1:, :128]
+    table = pool.table.to(DEV)
+    p = B.make_cache_params(8, 2, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp4=True, page_table=table)
+    starts, lens = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (start, total))
+    B.critiprefill_paged_attn(p, q, *pool.cache, table, starts, lens, out, None, B.alloc_paged_workspace(p))
+    torch.cuda.synchronize()
+    want, lse = attend4(pool, q, start, total)
+    assert torch.equal(out, want)
+    check_attention(pool, q, start, total, want, lse)
+    out.fill_(7.0)
+    assert bool((room == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,hint", [("bf16", 1), ("bf16", 300), ("fp32", 2)])
+def test_a_table_without_pages(dtype, hint):
+    pool, q, start, total = _case(dtype, 8, 2, 16, [(2, 90), (1, 30)])
+    out, lse = attend4(pool, q, start, total, table=torch.empty((2, 0), dtype=torch.int32), max_q_len=hint)
+    assert not out.any() and bool((lse == -float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 100), ("fp32", 5)])
+def test_two_calls_at_once(dtype, new):
+    """On two streams, each with outputs and a workspace of its own."""
+    cases = [_case(dtype, 8, 2, 16, [(new, 2000 - 90 * i) for i in range(n)], seed=n) for n in (1, 9)]
+    want = [attend4(*c, max_q_len=new) for c in cases]
+    calls = []
+    for pool, q, start, total in cases:
+        table, out, lse = pool.table.to(DEV), torch.zeros((q.shape[0], 8, 128), dtype=q.dtype, device=DEV), torch.zeros((q.shape[0], 8), device=DEV)
+        p = B.make_cache_params(8, 2, q.dtype, q=q, out=out, k_cache=pool.cache[0], mxfp4=True, page_table=table, max_q_len=new)
+        calls.append((p, q, *pool.cache, table, *(torch.tensor(x, dtype=torch.int32, device=DEV) for x in (start, total)), out, lse, B.alloc_paged_workspace(p)))
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                B.critiprefill_paged_attn(*c)
+    torch.cuda.synchronize()
+    for w, c in zip(want, calls):
+        assert torch.equal(w[0], c[-3]) and torch.equal(w[1], c[-2])
