@@ -91,6 +91,19 @@ __device__ __forceinline__ Unit unit_of(const PagedArgs& a, const Share& run) {
     run.piece(a, n.first, n.count, n.steps);
     return n;
 }
+// Head and tile of step `rest` of a sequence.
+__device__ __forceinline__ bool place_in(const PagedArgs& a, Share& run, unsigned rest) {
+    run.head = first_lane((int)(rest / run.now.length));
+    rest -= (unsigned)run.head * run.now.length;
+    int lo = 0, hi = run.now.tiles - 1;                                        // the last tile that begins at or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (run.now.before(a, mid, run.whole) <= rest) lo = mid; else hi = mid - 1;
+    }
+    run.tile = lo;
+    run.at = rest - run.now.before(a, lo, run.whole);
+    return run.has_steps(a);
+}
 // Run::find for a single sequence, whose arrays all lanes share: without the sums over lanes, and by scalar loads (one token of 300 keys, in a graph, 6.4 us, now 5.6; of 2000 8.8 and 8.1).
 __device__ __forceinline__ bool find_one(const PagedArgs& a, Share& run, unsigned workgroup) {
     run.whole = a.whole; run.logical = ~0u; run.used = run.left = 0; run.seq = run.head = run.tile = 0; run.at = 0;
@@ -103,17 +116,50 @@ __device__ __forceinline__ bool find_one(const PagedArgs& a, Share& run, unsigne
     if ((workgroup >> 3) >= (run.used + 7) / 8 || logical >= run.used) return false;
     run.logical = logical;
     run.left = min(run.share, total - logical * run.share);
-    unsigned rest = logical * run.share;
-    run.head = (int)(rest / run.now.length);
-    rest -= (unsigned)run.head * run.now.length;
-    int lo = 0, hi = run.now.tiles - 1;                                        // the last tile that begins at or before it
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (run.now.before(a, mid, run.whole) <= rest) lo = mid; else hi = mid - 1;
+    return place_in(a, run, logical * run.share);
+}
+// Run::find for 65 to 4096 sequences: the waves sum up 64 of them in turn, and look into those alone where the run begins.  us, with Run::find and so, 32/8 heads in a graph: 128 x 1 of 8000 keys 176.2 /
+// 175.4, 256 of 4000 182.3 / 180.2, 512 of 2100 202.1 / 198.7, of up to 4000 82.7 / 77.3.
+constexpr int kMany = 64 * 64;
+__device__ __forceinline__ unsigned up_to(unsigned x, int lane) {              // of all lanes before and its own
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const unsigned o = __shfl_up(x, d); if (lane >= d) x += o; }
+    return x;
+}
+__device__ __forceinline__ bool find_many(const PagedArgs& a, Share& run, unsigned workgroup, int lane, int wave, unsigned* shared) {
+    run.whole = a.whole; run.logical = ~0u; run.used = run.left = 0; run.seq = run.head = run.tile = 0; run.at = 0; run.now = Sequence{};
+    const int groups = (a.n_seqs + 63) >> 6;
+    unsigned long long wrong = 0;
+    Sequence s;
+    auto load = [&](int g) __attribute__((always_inline)) {
+        wrong |= __builtin_amdgcn_ballot_w64(!s.load<true>(a, min(64 * g + lane, a.n_seqs - 1), run.whole));
+        return 64 * g + lane < a.n_seqs ? s.length * (unsigned)a.hkv : 0u;
+    };
+    for (int g = wave; g < groups; g += 4) {
+        unsigned sum = load(g);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) shared[g] = sum;
     }
-    run.tile = lo;
-    run.at = rest - run.now.before(a, lo, run.whole);
-    return run.has_steps(a);
+    if (lane == 0) shared[64 + wave] = wrong != 0;
+    __syncthreads();
+    const unsigned of = lane < groups ? shared[lane] : 0u, upto = up_to(of, lane);
+    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    if (first_lane((int)(shared[64] | shared[65] | shared[66] | shared[67])) || total == 0) return false;
+    run.share = max(run.whole ? 1u : a.least, (unsigned)first_lane((int)((total + a.workgroups - 1) / a.workgroups)));
+    run.used = (unsigned)first_lane((int)((total + run.share - 1) / run.share));
+    const unsigned logical = (workgroup & 7) * ((run.used + 7) / 8) + (workgroup >> 3);
+    if ((workgroup >> 3) >= (run.used + 7) / 8 || logical >= run.used) return false;
+    run.logical = logical;
+    const unsigned begin = logical * run.share;
+    run.left = min(run.share, total - begin);
+    const int g = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > begin));
+    const unsigned past = (unsigned)__builtin_amdgcn_readlane((int)(upto - of), g), mine = load(g), within = up_to(mine, lane);
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(past + within > begin));
+    unsigned rest = begin - past - (unsigned)__builtin_amdgcn_readlane((int)(within - mine), l);
+    run.seq = 64 * g + l;
+    run.now = s.of_lane(l);
+    return place_in(a, run, rest);
 }
 // Run::next_steps with scalar loads: a vector load's wait would be one for all keys and values that are under way.
 __device__ __forceinline__ bool next_unit(const PagedArgs& a, Share& run) {
@@ -148,7 +194,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
     const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, kg = lane >> 4;
     const int wave = first_lane(tid >> 6);
     Share run;
-    const bool any = a.n_seqs == 1 ? find_one(a, run, blockIdx.x) : run.find(a, blockIdx.x, lane);
+    const bool any = a.n_seqs == 1 ? find_one(a, run, blockIdx.x)
+                   : a.n_seqs > 64 && a.n_seqs <= kMany ? find_many(a, run, blockIdx.x, lane, wave, (unsigned*)merge) : run.find(a, blockIdx.x, lane);
     if (blockIdx.x == 0 && tid == 0) a.record[0] = (int)run.used;
     if (run.logical < run.used && tid == 0) a.record[4 + 4 * run.logical + 3] = 0;
     if (!any) return;

@@ -447,3 +447,21 @@ def test_two_calls_at_once(dtype, new):
     torch.cuda.synchronize()
     for w, c in zip(want, calls):
         assert torch.equal(w[0], c[-3]) and torch.equal(w[1], c[-2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [64, 65, 128, 129, 4096, 4097])
+def test_many_sequences(dtype, n):
+    """On both sides of the numbers up to which a run's beginning is found in one look, by the waves in turn, and by all of them."""
+    lengths = [(1, 3000) if i % 997 == 5 else (1, 300) if i % 97 == 6 else ((0, 0), (1, 1 + 13 * i % 40), (1, 0), (2, 1), (1, 17))[i % 5] for i in range(n)]
+    pool, q, start, total = _case(dtype, 4, 2, 16, lengths)
+    for keys in (0, 200):                                            # cut, as the table is wide, and not cut
+        assert route(dtype, 2, 4, 2, n, 1, keys or pool.table.shape[1] * 16).whole == (keys > 0)
+        out, lse = attend4(pool, q, start, total, max_q_len=1, max_kv_len=keys)
+        check_attention(pool, q, start, total, out, lse)
+    rows = torch.full_like(q, 5.0, memory_format=torch.contiguous_format)
+    for at in (1, n // 2, n):                                        # not ascending there: nothing is done
+        wrong = list(start)
+        wrong[at] = wrong[at - 1] - 1
+        attend4(pool, q, wrong, total, max_q_len=1, out=rows)
+    assert bool((rows == 5.0).all())
