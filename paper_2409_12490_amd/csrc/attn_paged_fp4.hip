@@ -44,6 +44,8 @@ __device__ __forceinline__ float column_sum(float x) {
     r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// of the four neighbouring lanes that share c16 >> 2 the I-th's
+template <int I> __device__ __forceinline__ unsigned quad_lane(unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x55 * I, 0xf, 0xf, true); }
 // eight neighbouring e2m1 to bf16
 __device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {
     return u32x4{as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
@@ -202,7 +204,11 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
     const unsigned home = run.logical;
     const float c = a.scale_log2e, lazy_raw = fminf(kLazyLog2 / c, 3e38f);      // not infinite, whatever the scale: no maximum would be taken over then
     const int page_mask = (1 << a.page_shift) - 1;
-    const unsigned in_k = (unsigned)c16 * 64 + (unsigned)kg * 16, in_v = (unsigned)kg * 256 + (unsigned)c16 * 4, in_ks = (unsigned)c16 * 4, in_vs = (unsigned)kg * 16;
+    // An operand's row 4 a + b is key a + 4 b of its 16, so that the accumulators of S^T, four rows to a lane, hold keys kg + 4 i, and a load instruction of V has four neighbouring tokens, two
+    // whole lines, where keys 4 kg + i make it half of four.  Scales of V: a lane asks for the word of one of its four tokens and has the others from its neighbours.  us, keys 4 kg + i with a
+    // lane's four words in one load / so, 32/8 heads in a graph: one token of 10^6 170.8 / 165.2, 64 of up to 32769 60.9 / 58.9, 16 of 20000 (pages of 16) 63.8 / 60.8, 8 x 4 of 16000 31.7 / 30.9.
+    const unsigned of_row = (unsigned)(c16 >> 2 | (c16 & 3) << 2);
+    const unsigned in_k = of_row * 64 + (unsigned)kg * 16, in_v = (unsigned)kg * 64 + (unsigned)c16 * 4, in_ks = of_row * 4, in_vs = (unsigned)(kg + 4 * (c16 & 3)) * 4;
     // rotations to the right that bring a block's byte to the exponent's bits: the lane's 32 channels of K, its 8 of V.  What else is in the word is not looked at.
     const unsigned turn_k = 8u * (unsigned)kg + 9, turn_v = 8u * ((unsigned)c16 >> 2) + 9;
 
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
     };
     int seen[RUNS], seen_next[RUNS];                                           // keys of a run that exist, of this step and the next
     int64_t at[RUNS];                                                          // first row of the runs asked for last
-    u32x4 rk[kGroups], rvs[kGroups]; unsigned rks[kGroups], rv[4 * kGroups];
+    u32x4 rk[kGroups]; unsigned rks[kGroups], rv[4 * kGroups], rvs[kGroups];
     auto load_k = [&](const Unit& n, unsigned x) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < RUNS; ++r) {                                       // a page that is not in the pool holds nothing: its keys are hidden, and read from page 0
@@ -236,8 +242,8 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
         for (int g = 0; g < kGroups; ++g) {
             const int r = g / kRunGroups, more = g % kRunGroups;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) rv[4 * g + i] = get<unsigned>((const char*)a.cache.v + at[r] * 64 + 1024 * more + 64 * i + in_v);
-            rvs[g] = *(const u32x4*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
+            for (int i = 0; i < 4; ++i) rv[4 * g + i] = get<unsigned>((const char*)a.cache.v + at[r] * 64 + 1024 * more + 256 * i + in_v);
+            rvs[g] = *(const unsigned*)(a.cache.vs + at[r] * 4 + 64 * more + in_vs);
         }
     };
     // Lane's column is a row, 8 channels at 32 kg + 8 ks: of bf16 in registers; the pieces of fp32, three times as many, in LDS, once for the four waves, where the merge comes later.
@@ -342,12 +348,12 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
             if (!whole) {
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + 4 * kg;
+                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + kg;
 #pragma unroll
                     for (int nq = 0; nq < NQ; ++nq) {
                         const int lim = seen[r] > 0 ? last[nq] - u : -1;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[nq][g][i] = i > lim ? -INFINITY : s[nq][g][i];
+                        for (int i = 0; i < 4; ++i) s[nq][g][i] = 4 * i > lim ? -INFINITY : s[nq][g][i];
                     }
                 }
             }
@@ -386,18 +392,19 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
             // `odd` says that some rows see such a key and others do not; the unit's end makes it NaN for those that do.
             unsigned scales[kGroups][4];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) scales[g][i] = __builtin_amdgcn_alignbit(rvs[g][i], rvs[g][i], turn_v);
+            for (int g = 0; g < kGroups; ++g) {
+                const unsigned turned = __builtin_amdgcn_alignbit(rvs[g], rvs[g], turn_v);
+                scales[g][0] = quad_lane<0>(turned); scales[g][1] = quad_lane<1>(turned); scales[g][2] = quad_lane<2>(turned); scales[g][3] = quad_lane<3>(turned);
+            }
             if (!whole) {
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + 4 * kg;
+                    const int r = g / kRunGroups, u = now.key(a, x, wave, r) + 16 * (g % kRunGroups) + kg;
                     const int lim = seen[r] > 0 ? high - u : -1, sure = seen[r] > 0 ? low - u : -1;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const bool far = (scales[g][i] & 0x7f800000u) >= kFarScale << 23;
-                        if (i > sure && far) { scales[g][i] = 0x3f800000u; if (i <= lim) odd = true; }
+                        if (4 * i > sure && far) { scales[g][i] = 0x3f800000u; if (4 * i <= lim) odd = true; }
                     }
                 }
             }
