@@ -10,7 +10,7 @@
 // PV has, and neither by a branch.  Where the loads stand behind a branch the compiler has to wait for all of them at the first use of any (one token of 10^6 keys 203 us, 64 of 8000 108; without
 // 195 and 103, past the caches 170 and 91, and with whole lines of V in an instruction 165 and 88).  Not kept: two steps at a time (64 single tokens of all lengths up to 32769: 90 us for 72, units are short), three workgroups to a
 // compute unit (64 of 8000: 101 us for 91), K and V two steps ahead in registers of their own (fp32: 20 x 200 after 8000 249 us for 232, 8 x 1 of 20000 21.1 for 18.8),
-// the merge's rows that are not there left out (no difference), K as 4-bit operand of a scaled MFMA with Q in two e4m3 pieces (its sums are good to 2^-17 of their terms only).
+// the merge's rows that are not there left out (no difference), waves that go on to the next unit without a barrier while the last of the four adds up (64 of up to 32769 67.6 us for 59.7), K as 4-bit operand of a scaled MFMA with Q in two e4m3 pieces (its sums are good to 2^-17 of their terms only).
 // fp32 with its own MFMAs, 4/2 heads: 3 x up to 200 tokens after 3000 34.5 us, with pieces 20.9; 20 x 200 after 8000 682 and 256; 8/2 heads: 8 x 1 of 20000 37.0 and 19.5.
 #include "paged.h"
 
