@@ -220,7 +220,8 @@ size_t critiprefill_paged_workspace_bytes(const critiprefill_cache_params *p);
  * Whatever they hold, nothing outside the tensors is touched: rows and lengths are cut to the tensors' sizes, tokens of a page outside the pool are seen
  * by no row, and with a q_start that does not ascend nothing is done.  Rows of no sequence are not written.  out must not overlap q or the cache.  At most 64
  * query heads for a KV head.
- * Logits, maxima and sums are fp32.  With dtype bf16 a weight is rounded to bf16 for its product with V (not for the sum of weights), and out once at the end.
+ * Logits, maxima and sums are fp32.  Over pages of 4 bits fp32 queries and weights go into their products as bf16 numbers that add up to them: of one below 2^-110 what lies below
+ * 2^-133 is lost.  With dtype bf16 a weight is rounded to bf16 for its product with V (not for the sum of weights), and out once at the end.
  * The same call on the same contents gives the same bits.  Where a row's sum over keys is cut depends on the other sequences of the call, max_q_len and max_kv_len, and so do its last bits.
  */
 int critiprefill_paged_attn(const critiprefill_cache_params *p, const void *q, const void *k_cache, const void *v_cache, const uint8_t *k_scale,

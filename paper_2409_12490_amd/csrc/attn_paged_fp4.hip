@@ -4,7 +4,7 @@
 //   K   a lane takes one key's 32 channels of one scale, 16 bytes, and makes them bf16 (exact) by 16 conversions that apply the scale
 //   V   a lane takes 8 channels of 8 tokens, 4 bytes each; 32 conversions, and 32 v_perm that bring two tokens' together
 //   e2m1 has no infinity or NaN: what may become one is seen in the scales alone, and a key that no row sees needs no zeros in place of its V
-//   fp32: Q and P as three bf16 pieces of 8 bits, exactly, so that a product is three bf16 MFMAs where one in fp32 takes the time of 16, with sums in fp32 as there
+//   fp32: Q and P as three bf16 pieces of 8 bits, exactly from 2^-110 on (split8), so that a product is three bf16 MFMAs where one in fp32 takes the time of 16, with sums in fp32 as there
 //
 // A step's loads are half as many bytes as over 8-bit pages for as much work, so what a wave waits for counts: K of the next step is asked for when QK has read this one's, V when
 // PV has, and neither by a branch.  Where the loads stand behind a branch the compiler has to wait for all of them at the first use of any (one token of 10^6 keys 203 us, 64 of 8000 108; without
@@ -52,7 +52,9 @@ __device__ __forceinline__ u32x4 widen8(unsigned w, float scale) {
     return u32x4{as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
                  as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), as_u32(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
 }
-// Eight fp32 as sums of three bf16 each, exactly: 8 of the 24 bits to a piece, cut off and not rounded, so that the largest stay finite.
+// Eight fp32 as sums of three bf16 each: 8 of the 24 bits to a piece, cut off and not rounded, so that the largest stay finite.  Exact from 2^-110 on; of a smaller number what lies below
+// bf16's last bit, 2^-133, is lost.  A logit is then off by 2^-133 sum_c |k_c| scale at most, which keys above 2^100
+// alone make felt, and an output, whose largest weight is 1 or more, by 2^-133 sum_u |v_u|: values above 2^100 whose weights are next to nothing.
 __device__ __forceinline__ void split8(f32x4 lo, f32x4 hi, bf16x8* piece) {
     u32x4 w[3];
 #pragma unroll

@@ -465,3 +465,18 @@ def test_many_sequences(dtype, n):
         wrong[at] = wrong[at - 1] - 1
         attend4(pool, q, wrong, total, max_q_len=1, out=rows)
     assert bool((rows == 5.0).all())
+
+
+@pytest.mark.parametrize("power", [-100, -110, -118, -124])
+def test_fp32_queries_next_to_nothing(power):
+    """Queries of 2^power under keys as much larger: the third piece of an element below 2^-110 is a bf16 number of fewer bits, and what lies below the last of them, 2^-133, is cut off.  A logit is off by
+    that much of each of its key's channels beside what cache_helpers.check_attention has."""
+    scale = 128 ** -0.5
+    pool, q, start, total = _case("fp32", 8, 2, 16, [(1, 300), (5, 90)], scale=2.0 ** -power)
+    q = q * 2.0 ** power
+    out, lse = attend4(pool, q, start, total, max_q_len=5)
+    want, want_lse, size, logit = O.paged_attention(f64(q), pool.held_k, pool.held_v, pool.page, pool.table.numpy(), start, total, scale)
+    lost = 2.0 ** -133 * np.nanmax(np.abs(pool.held_k).sum(-1)) * scale
+    delta = 2.0 ** -20 * (logit + np.maximum(np.abs(want_lse), 1.0)) + 2.0 ** -20 + lost
+    bound = 2.0 ** -24 * np.abs(want) * 1.01 + 4 * delta[..., None] * size.max(-1, keepdims=True)
+    assert (np.abs(f64(out) - want) <= bound).all() and (np.abs(f64(lse) - want_lse) <= 2 * delta).all()
