@@ -332,7 +332,8 @@ unsigned grid_of(const RopeArgs& a) { return (unsigned)(((long long)a.tokens * a
 
 template <typename T, int TURN, int TO>
 hipError_t launch(const RopeArgs& a, bool stream, hipStream_t st) {
-    if (stream) hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    constexpr bool kCan = !(sizeof(T) == 4 && TURN == TURN_NONE && TO == TO_MXFP4);   // of fp32 as it is into 4 bits all accesses are ordinary ones
+    if (kCan && stream) hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, kCan>), dim3(grid_of(a)), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((norm_rope_kernel<T, TURN, TO, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
@@ -340,10 +341,12 @@ template <typename T, int TO>
 hipError_t launch_turn(const RopeArgs& a, int turn, bool stream, hipStream_t st) {
     return turn == TURN_WHOLE ? launch<T, TURN_WHOLE, TO>(a, stream, st) : turn == TURN_HALVES ? launch<T, TURN_HALVES, TO>(a, stream, st) : launch<T, TURN_PAIRS, TO>(a, stream, st);
 }
+// From 4 bits the tensors are nearly all that moves, and go past the caches at any size: 8 heads in bf16, 4000 tokens 8.5 / 6.8 us, 8000 12.1 / 8.5, 30000 36.6 / 24.1, in fp32 4000 12.6 / 8.9.
 template <typename T, int HELD>
 hipError_t launch_read(const RopeArgs& a, bool stream, hipStream_t st) {
-    if (stream) hipLaunchKernelGGL((cache_read_kernel<T, HELD, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((cache_read_kernel<T, HELD, false>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    constexpr bool kAlways = HELD == HELD_MXFP4;
+    if (kAlways || stream) hipLaunchKernelGGL((cache_read_kernel<T, HELD, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((cache_read_kernel<T, HELD, kAlways>), dim3(grid_of(a)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 // a kernel for each way that the cache may hold rows
@@ -357,11 +360,7 @@ hipError_t launch_write(const RopeArgs& a, int held, bool stream, hipStream_t st
 }
 template <typename T>
 hipError_t launch_back(const RopeArgs& a, int held, bool stream, hipStream_t st) {
-    if (held == HELD_MXFP4) {
-        hipLaunchKernelGGL((cache_read_kernel<T, HELD_MXFP4, true>), dim3(grid_of(a)), dim3(256), 0, st, a);
-        return hipGetLastError();
-    }
-    return held == HELD_MXFP8 ? launch_read<T, HELD_MXFP8>(a, stream, st) : launch_read<T, HELD_PLAIN>(a, stream, st);
+    return held == HELD_MXFP4 ? launch_read<T, HELD_MXFP4>(a, stream, st) : held == HELD_MXFP8 ? launch_read<T, HELD_MXFP8>(a, stream, st) : launch_read<T, HELD_PLAIN>(a, stream, st);
 }
 
 }  // namespace
@@ -393,8 +392,7 @@ hipError_t launch_cache_write(const CacheShape& sh, const void* k, const void* v
 hipError_t launch_cache_read(const CacheShape& sh, const int32_t* slots, const CachePtr& cache, void* k, void* v, hipStream_t st) {
     RopeArgs a = common(sh, 2 * sh.hkv, &cache);
     a.slots = slots; a.k_out = k; a.q_out = v;
-    // From 4 bits the tensors are nearly all that moves, and go past the caches at any size: 8 heads in bf16, 4000 tokens 8.5 / 6.8 us, 8000 12.1 / 8.5, 30000 36.6 / 24.1, in fp32 4000 12.6 / 8.9.
-    const bool stream = sh.held == HELD_MXFP4 || cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
+    const bool stream = cache_call_streams(sh, 2 * sh.hkv, 2 * sh.hkv);
     return sh.dtype == 1 ? launch_back<__bf16>(a, sh.held, stream, st) : launch_back<float>(a, sh.held, stream, st);
 }
 

@@ -1,5 +1,6 @@
 """CPU-side checks of the cache of 4 bits: the oracle's own format, the refusals of the library before any launch, and of the binding."""
 import ctypes
+import re
 import types
 
 import numpy as np
@@ -114,3 +115,13 @@ def test_binding_refuses_pages_that_do_not_fit():
         with pytest.raises(B.CritiPrefillError) as e:
             call([cache[0], cache[1], None, cache[3]])
         assert e.value.status == -1
+
+
+def test_no_two_kernels_that_differ_in_nothing():
+    """The last argument of both kernels says whether tensors go past the caches.  fp32 written into 4 bits never does, what is read back from there always; the other forms are not built."""
+    with open(B.lib_path(), "rb") as f:
+        built = f.read()
+    # a kernel's name in the library: <element type, TURN_NONE, TO_MXFP4, past the caches>, <element type, HELD_MXFP4, past the caches>
+    forms = lambda name: {m.group(1).decode() for m in re.finditer(name.encode() + rb"ELb([01])EEE", built)}                                                       # noqa: E731
+    assert forms("norm_rope_kernelIfLi0ELi3") == {"0"} and forms("norm_rope_kernelIDF16bLi0ELi3") == {"0", "1"}
+    assert forms("cache_read_kernelIfLi2") == {"1"} and forms("cache_read_kernelIDF16bLi2") == {"1"}
