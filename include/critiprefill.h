@@ -179,7 +179,8 @@ typedef struct critiprefill_cache_params {
                                                  (16 rows or more each) by the steps over max_pages * page_size keys (64 or more each) by n_kv_heads < 2^31 */
     int32_t max_q_len, max_kv_len;            /* paged_attn: new tokens, and tokens in all, that a sequence has at most, 0: not known (tokens, and
                                                  max_pages * page_size).  They choose the kernel and the way the work is cut; more are right too.  A table much
-                                                 wider than the sequences are long hides that these are short: 32 single tokens of 760 keys 26 us, with max_kv_len 20 */
+                                                 wider than the sequences are long hides that these are short: 32 single tokens of 760 keys 26 us, with max_kv_len 20;
+                                                 over pages of 4 bits 3 single tokens and a chunk of 300 of 2300 keys in a table of 131072 49 us, with max_kv_len 39 */
     int32_t rotary_dim, rotary_interleaved;   /* norm_rope: channels that turn (0 .. 128, a multiple of 16), and how they pair */
     float norm_eps, attn_scale;               /* attn_scale: 0 -> 1/sqrt(head_dim) */
     int64_t q_stride[2], k_stride[2], v_stride[2]; /* token, head.  cache_read: k_stride, v_stride are the outputs' */

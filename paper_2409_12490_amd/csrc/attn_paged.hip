@@ -482,7 +482,9 @@ PagedRoute paged_route(const CacheShape& sh) {
     const double heads = (double)sh.n_seqs * sh.hkv;
     r.chunk = !f32 && want > (scaled ? 32 : 16) && !(sh.group <= 16 && want <= 32 && heads <= 8 && sh.max_kv <= 24576);
     // Over pages of 4 bits tiles of 32 rows, as many as it takes, pay further: 1 x 16 tokens of 2000 13.4 / 15.7, of 60000 37.5 / 59.1, 8 x 16 of 8000 40.2 / 63.8, 32 x 16 of 4000 63.7 / 106; 1 x 32
-    // of 2000 15.4 / 17.7, of 60000 59.0 / 61.3, 4 x 32 of 2000 26.6 / 24.5, 32 x 32 of 4000 114 / 106; 1 x 64 of 2000 18.2 / 23.4, of 16000 40.3 / 39.2; 32/4 heads 16 x 8 of 6000 34.3 / 52.0.
+    // of 2000 15.4 / 17.7, of 60000 59.0 / 61.3, 4 x 32 of 2000 26.6 / 24.5, 32 x 32 of 4000 114 / 106; 1 x 64 of 2000 18.2 / 23.4, of 16000 40.3 / 39.2; 32/4 heads 16 x 8 of 6000 34.3 / 52.0.  Other heads: 28/4 8 x 9 of
+    // 16000 51 / 64, 8 x 13 62 / 60, 40/8 8 x 12 91 / 109, 8 x 19 150 / 106, 8/8 8 x 64 64 / 103, 8 x 96 98 / 105; a single sequence of few KV heads and many keys would have tiles of 32 rows further, 16/1 1 x 12 of 16000 18.8 /
+    // 24.6, 28/4 1 x 36 28.4 / 34.2, where 40/8 1 x 25 takes 34.0 / 27.3.
     if (four && !f32) r.chunk = sh.group > 32 || want > (heads > 8 ? 64 : sh.max_kv > 4096 ? 128 : 256);
     // Sequences known to be short: units are not cut, and nothing is joined.  us, cut / whole, 32/8 heads: 1 token after 255 10.1 / 7.8, after 509 10.2 / 10.1, after 999 10.2 / 14.7;
     // fp32 (steps of half as many keys, and slower) 8 x 1 of up to 512 12.2 / 17.1.  With units for a quarter of the chip the join has more to read and longer units pay: 8 x 1 of 760
@@ -501,7 +503,8 @@ PagedRoute paged_route(const CacheShape& sh) {
     // The smallest tile that holds a sequence's new tokens, up to 16 rows, in bf16 over 8-bit pages (K and V converted once) and fp32 over plain ones (K and V read once) 32.  Of fp32
     // with 32 rows one workgroup has room on a compute unit, and few steps are better shared by twice as many of 16: us, 32 / 16 rows (4/2 heads): 1 x 9 tokens after 3000
     // 16.2 / 13.0, 1 x 16 after 8000 26.4 / 21.1, 1 x 50 after 600 15.5 / 13.2, after 3000 20.4 / 21.6, 8 x 16 after 3000 28.7 / 36.2, 1 x 500 after 8000 99 / 117; 8-bit pages 1 x 50 after
-    // 600 15.3 / 12.8, 3 x 200 after 3000 56 / 52, 20 x 200 after 8000 720 / 645.
+    // 600 15.3 / 12.8, 3 x 200 after 3000 56 / 52, 20 x 200 after 8000 720 / 645.  Over pages of 4 bits (bf16 products, and K and V converted for each tile) 32 rows pay with more steps still, and 16 stay: 1 x 50 of 3000
+    // 11.9 / 12.6, 8 x 16 of 3000 16.0 / 15.4, 1 x 500 of 8000 38.9 / 36.5, 3 x 200 of 3200 28.8 / 27.4, 20 x 200 of 8200 249 / 248; 8/2 heads 4 x 9 of 9000 20.5 / 18.2; 32/8 10 x 100 of 20000 1060 / 1160.
     int most = scaled ? 2 : 1;
     if (f32) {
         const int shift = log2_of(std::max(1, 32 / sh.group));
@@ -575,6 +578,10 @@ static hipError_t launch_join(int groups, int rows, int tile_rows, const PagedAr
 // waves split the keys, where 256 rows' worth of time passes for each of their steps otherwise.  0: one kernel for all.  The host does not see the lengths, so it goes by how long the others are
 // on the average if one is as long as is said, and by how much there can be to gain: two launches more are 7 to 12 us.  us, one kernel / both: 63 single tokens of 8000 keys and 512 of 4512
 // (32/8 heads) 504 / 166, 15 and 2048 161 / 104, 3 and 300 of 2300 (32/4) 42 / 52; 20 sequences of 1 to 300 of up to 12300 (32/4), 67 on the average, 134 / 146; 50 of 1 to 100, 20 on the average, 71 / 80.
+// Where nothing is said of the longest, it may be all tokens, and the others none: both kernels.  A batch of chunks that are alike then has nothing for the first, and loses its two launches: us, one / both, 20 x 100
+// tokens of 4000 169 / 175, 64 x 20 of 8000 362 / 369, 16 x 129 of 8000 360 / 366; one that is not has more to gain: 15 single tokens and 2048 of 8000 339 / 293, 20 and 1000 277 / 178, 30 and 300 of 4000 151 / 75.  The
+// average of all (129, 49 and 11 for these three) would not tell the first two from the even ones.  Nor does the host know how far a wide table is filled: 3 and 300 of 2300 in one of 131072 39 / 49, 31 and 200 of 800
+// 50 / 43; max_kv_len says it.
 int few_tokens(const CacheShape& sh) {
     if (sh.held != HELD_MXFP4 || sh.n_seqs < 2 || sh.group > 32 || !paged_route(sh).chunk) return 0;
     const double others = (double)std::max(sh.tokens - sh.max_q, 0) / (sh.n_seqs - 1), steps = (double)(sh.n_seqs - 1) * sh.hkv * (double)(sh.max_kv >> 6);

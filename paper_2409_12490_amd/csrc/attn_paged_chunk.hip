@@ -7,7 +7,7 @@
 // four pages, looked up by scalar loads a step ahead (pages are whole multiples of 16 tokens, so the rows of one load lie together); rows past the sequence's end lie in
 // its last page and may hold anything, so rows of V that no row sees are zeroed in LDS; the row sum adds P before it is rounded, since the log-sum-exp is an
 // output in its own right here (32 additions a step for 16 dot products).
-// Pages of 8 and 4 bits: every thread takes an eighth of a wave's share of a tile into registers, a step ahead, and writes it to LDS as bf16 (exact: the scales are powers of two), where
+// Pages of 8 and 4 bits: the 512 threads share a tile out, take their 16 bytes of it into registers a step ahead, and write them to LDS as bf16 (exact: the scales are powers of two), where
 // conversion at the reads from LDS would have each wave convert all of it.  8 bits: 16 channels of a row of K and of V; 4 bits: the 32 channels of one scale, of K or of V.
 //
 // What bounds it, 32/8 heads: the matrix units under the clock that they leave, as in attn_bf16.hip: 8192 new tokens of 32768 3.16 ms, 1.22 PFLOP/s, where a large product of the
@@ -356,7 +356,7 @@ __device__ __forceinline__ void work(const PagedArgs& a, Run<true, HELD == HELD_
                 for (int r = 0; r < 16; ++r) {
                     const float p = __builtin_amdgcn_exp2f(fmaf(s[kt][r], c, -ms));
                     if (r & 1) rs1 += p; else rs0 += p;
-                    pf[2 * kt + (r >> 3)][r & 7] = (__bf16)p;
+                    pf[2 * kt + (r >> 3)][r & 7] = (__bf16)p;         // off by 2^-8 of a term or less; in two pieces PV would take twice the matrix time
                 }
             l_run = l_run * alpha + (rs0 + rs1);
             if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {

@@ -11,6 +11,8 @@
 // 195 and 103, past the caches 170 and 91, and with whole lines of V in an instruction 165 and 88).  Not kept: two steps at a time (64 single tokens of all lengths up to 32769: 90 us for 72, units are short), three workgroups to a
 // compute unit (64 of 8000: 101 us for 91), K and V two steps ahead in registers of their own (fp32: 20 x 200 after 8000 249 us for 232, 8 x 1 of 20000 21.1 for 18.8),
 // the merge's rows that are not there left out (no difference), waves that go on to the next unit without a barrier while the last of the four adds up (64 of up to 32769 67.6 us for 59.7), K as 4-bit operand of a scaled MFMA with Q in two e4m3 pieces (its sums are good to 2^-17 of their terms only).
+// Scalars do not fit: every form keeps 22 to 82 of them in lanes of vector registers.  In bf16 with 16 rows a step that asks for another of its unit reads none of them, the last of a unit, which asks for the next unit's, 43
+// for pages of 16 and 2 for larger ones.  No vector register is spilled.
 // fp32 with its own MFMAs, 4/2 heads: 3 x up to 200 tokens after 3000 34.5 us, with pieces 20.9; 20 x 200 after 8000 682 and 256; 8/2 heads: 8 x 1 of 20000 37.0 and 19.5.
 #include "paged.h"
 
@@ -70,8 +72,10 @@ __device__ __forceinline__ void split8(f32x4 lo, f32x4 hi, bf16x8* piece) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) piece[i] = as_bf16x8(w[i]);
 }
-// Elements go past the caches: a call reads them once.  us, ordinary loads / past the caches (32/8 heads, pages of 64, caches that no other call has left in the chip): one token of 8000 keys
-// 12.5 / 11.4, of 131072 34.6 / 31.2, of 10^6 194.9 / 170.0; 8 of 2000 15.1 / 14.1, 64 of 8000 102.6 / 91.5.  Scales, 16 tokens' to 64 bytes, by ordinary loads.
+// Elements go past the caches: where a sequence's new tokens fit a tile a call reads them once.  us, ordinary loads / past the caches (32/8 heads, pages of 64, caches that no other call has left in the
+// chip): one token of 8000 keys 12.5 / 11.4, of 131072 34.6 / 31.2, of 10^6 194.9 / 170.0; 8 of 2000 15.1 / 14.1, 64 of 8000 102.6 / 91.5.  Sequences of several tiles, which read them again for each, take these loads too
+// though ordinary ones are faster there: 8 x 16 tokens of 16000 60.7 / 64.0, 1 x 64 of 16000 37.4 / 39.1, 1 x 32 of 60000 56.7 / 61.8, 32 x 16 of 4000 59.8 / 60.4; fp32, 4/2 heads 3 x 200 of 3200 27.2 / 27.4, 20 x 200 of
+// 8200 228 / 249, 32/8 heads 10 x 100 of 20000 1012 / 1156.  Scales, 16 tokens' to 64 bytes, by ordinary loads.
 template <typename V>
 __device__ __forceinline__ V get(const char* p) { return __builtin_nontemporal_load((const V*)p); }
 
@@ -293,7 +297,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
         place_q();
         look_up(n, 1);
     };
-    // The first step of the next unit is asked for in this one's last: what a unit begins and ends with, some 3 us, passes meanwhile (64 single tokens of up to 32769 keys 73.7 us, now 66.9).
+    // The first step of the next unit is asked for in this one's last: what a unit begins and ends with, some 3 us, passes meanwhile (64 single tokens of up to 32769 keys 73.7 us without and 66.9 with it, before other steps that brought them to 59).
     // With 32 rows there are no registers for it, and with fp32 the queries' place is the merge's (with a place of their own: 20 x 200 after 8000 1 % faster, 3 x 200 after 3000 2 % slower).
     constexpr bool kAcross = NQ == 1 && !F32;
     Unit now = unit_of(a, run);
@@ -382,7 +386,7 @@ __global__ __launch_bounds__(kThreads, NQ == 1 || sizeof(T) == 2 ? 2 : 1) void p
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[nq][g][i], c, -ms));
                         sum += p;                                              // before P is rounded for the product: lse is as exact as fp32 allows
                         if constexpr (F32) p4[g][i] = p;
-                        else pf[nq][0][4 * g + i] = (__bf16)p;
+                        else pf[nq][0][4 * g + i] = (__bf16)p;                 // off by 2^-8 of a term or less; out's error against 64 bits stays that of its own rounding, 0.0016 of its size
                     }
                 if constexpr (F32) split8(p4[0], p4[1], pf[nq]);
                 l_run[nq] = l_run[nq] * alpha + sum;

@@ -147,7 +147,8 @@ __device__ __forceinline__ unsigned quantise8_to_4(const float (&x)[8], int& exp
 // Rows of 4 bits are half a line of L2, 64 bytes, and a token's scales of a head 4 of a line that 32 tokens share.  They are written and read by ordinary accesses, which bring a line together, whatever the
 // tensors do, and lines' tokens come to one XCD.  32/8 heads, us, past the caches and tokens dealt over the XCDs / ordinary / and together: 65536 tokens back 72.1 / 54.1 / 49.8, written and
 // back 148.9 / 130.5 / 123.4, 8192 back 9.3 / 9.2 / 8.8.
-// Of 8 * kTogether neighbouring workgroups the first kTogether on an XCD, whichever these are: 32 tokens, whose scales of a head fill a line of its L2.  What is left over stays as it is.
+// Of 8 * kTogether neighbouring workgroups the first kTogether on an XCD, whichever these are: 32 tokens where a wave has one to itself (from 2049 on), whose scales of a head fill a line of its L2; with fewer
+// tokens, which waves share, as many fewer, and a part of a line.  What is left over stays as it is.
 constexpr unsigned kTogether = 8;
 __device__ __forceinline__ unsigned by_xcd(unsigned b, unsigned blocks) {
     return b < blocks / (8 * kTogether) * (8 * kTogether) ? b / (8 * kTogether) * (8 * kTogether) + (b & 7) * kTogether + (b >> 3) % kTogether : b;

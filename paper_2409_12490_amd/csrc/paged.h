@@ -1,4 +1,4 @@
-// What the two kernels of attention over pages share: how the work is cut, and what is left for the join.
+// What the three kernels of attention over pages (attn_paged.hip, attn_paged_fp4.hip, attn_paged_chunk.hip) share: how the work is cut, and what is left for the join.
 //
 // A unit is (sequence, KV head, tile of the sequence's new tokens); its rows are the tile's tokens times the KV head's query heads.  A unit takes as many
 // steps over its keys as its last token sees, and `setup` more for what a workgroup does around them (with none, workgroups whose run held twenty units of two steps each

@@ -43,9 +43,10 @@ __host__ __device__ __forceinline__ unsigned whole_rounds(unsigned units, unsign
 // Cutting evens the work out but is not free: what is left for the join is written and read again, 9 steps' worth where every workgroup leaves some and 4 in
 // any case, and in plain pages a step of a run takes a quarter longer than one of a whole unit.  us, cut / whole (32/8 heads, the only layout that this was measured at): 4 x 300 new
 // tokens of 600 40.5 / 29.6, of 1000 47.8 / 38.9, of 4000 102 / 106; 16 x 64 of 600 43.2 / 30.9, of 2000 59.9 / 63.2; 1 x 2000 of 2400 78.3 / 74.6; 16 x 300 of 600 (two rounds and
-// a half) 78.1 / 72.3; 8 bits 4 x 300 of 1000 50.7 / 42.7, of 2000 67.7 / 68.6.
-__host__ __device__ __forceinline__ bool uncut_pays(unsigned turns, unsigned longest, unsigned used, unsigned share, bool mxfp8) {
-    const unsigned cut = 4 + 9 * used / 256 + share + (turns == 1 && !mxfp8 ? share / 4 : 0);
+// a half) 78.1 / 72.3; 8 bits 4 x 300 of 1000 50.7 / 42.7, of 2000 67.7 / 68.6; 4 bits, which go by the same line (`scaled`), 46.9 / 43.1, 64.5 / 70.7, of 4000 97.8 / 125, 1 x 2000 of 2400 76.5 / 83.4, 16 x 300 of 1000
+// 107 / 110 (taken whole), five of 200 to 350 of 820 to 1020 49.4 / 43.5.
+__host__ __device__ __forceinline__ bool uncut_pays(unsigned turns, unsigned longest, unsigned used, unsigned share, bool scaled) {
+    const unsigned cut = 4 + 9 * used / 256 + share + (turns == 1 && !scaled ? share / 4 : 0);
     return turns * longest <= cut;
 }
 
